@@ -356,6 +356,65 @@ int innerq_decode_step_ragged(const innerq_config_t *cfg, const innerq_cache_t *
                               void *out, int out_is_fp32, void *workspace, size_t workspace_bytes,
                               void *hip_stream);
 
+/* ---- Several new tokens of a sequence at once: chunks of a prompt, drafts of a few tokens, batches that mix
+ * both (no counterpart in the paper, whose path decodes one token a step).  The calls below take rows where they
+ * lie, in the output of a projection: a tensor is named by its first element and the strides of batch, head and
+ * token in ELEMENTS; the head_dim channels of a row are contiguous.  Strides are multiples of 8 (rows start on 16
+ * bytes) and not negative; a stride of 0 (the same row for all) is fine for what is read.  They serve inner-grouped
+ * caches (INNERQ_E_UNSUPPORTED for the other kinds) of at most 2^24 capacity_tokens. */
+typedef struct {
+  int64_t batch, head, token;
+} innerq_strides_t;
+
+/* Rotary positions.  rot_dim / 2 pairs of channels are turned, pair i by the angle whose cosine and sine stand in
+ * column i of row p of the tables, p being the token's position on the pair's axis:
+ *   y1 = fp16(fl(x1 * cos) - fl(x2 * sin)),  y2 = fp16(fl(x2 * cos) + fl(x1 * sin))   (every fp32 operation rounded)
+ * Pair i is channels (i, i + rot_dim / 2), or (2 i, 2 i + 1) if interleaved; channels from rot_dim on pass through.
+ * The inverse rotation (which is also the gradient) is the same call with the sines negated. */
+typedef struct {
+  const float *cos_table, *sin_table; /* device, fp32 [table_positions][rot_dim / 2], 16-byte aligned */
+  int64_t table_positions;            /* 1 .. 2^31 - 1; a position outside [0, table_positions) is clamped into the table */
+  int32_t rot_dim;                    /* 16, 32, .. 128 (INNERQ_E_UNSUPPORTED: another even number) */
+  int32_t interleaved;                /* 0 or 1 */
+  int32_t n_axes;                     /* 1 to 3 (time, height, width) */
+  uint8_t pair_axis[64];              /* axis of every pair, below n_axes; entries from rot_dim / 2 on are ignored */
+} innerq_rotation_t;
+
+/* y = x rotated, for n_heads heads (queries and keys together where they lie next to each other).
+ *   positions     device, int32 [n_axes][B][t_new], or NULL: token t of sequence b stands at n_b + t on every axis,
+ *                 with n_b = n_tokens_dev[b] (device, int32 [B]) or, where that is NULL, n_tokens
+ *   t_new_dev     device, int32 [B], or NULL: rows of y from t_new_dev[b] on are left as they were
+ *   x, y          device, fp16 rows; y may be x (same pointer and strides), else they must not overlap */
+int innerq_rotate(const innerq_config_t *cfg, const innerq_rotation_t *rotation, const int32_t *positions,
+                  int64_t n_tokens, const int32_t *n_tokens_dev, const int32_t *t_new_dev, const void *x,
+                  const innerq_strides_t *x_strides, void *y, const innerq_strides_t *y_strides, int32_t n_heads,
+                  int64_t t_new, void *hip_stream);
+
+/* innerq_quantize_append of rows where they lie, the keys rotated on their way in (rotation may be NULL: as they
+ * are) and then, if k_inv_norm is given, multiplied by the factors; the cache is bit for bit the one that
+ * innerq_rotate followed by innerq_quantize_append leaves.  positions as for innerq_rotate (NULL: token t stands at
+ * cache->n_tokens + t).  One launch where no new token enters a ring slot that leaves it in the same call (a first
+ * prompt, a single token), else two. */
+int innerq_append_rotated(const innerq_config_t *cfg, innerq_cache_t *cache, const innerq_rotation_t *rotation,
+                          const int32_t *positions, const void *k_new, const innerq_strides_t *k_strides,
+                          const void *v_new, const innerq_strides_t *v_strides, int64_t t_new,
+                          const float *k_inv_norm, void *hip_stream);
+
+/* The same for a batch whose sequences bring different numbers of tokens to different numbers of cached ones, both
+ * in DEVICE memory; no host decision depends on them, so the call can be recorded in a HIP graph.
+ *   n_tokens_dev  int32 [B]: tokens cached before the call; the call advances every entry by what it appended.
+ *                 cache->n_tokens and store_ahead_tokens (host) are neither read nor written.
+ *   t_new_dev     int32 [B]: new tokens of every sequence, 0 .. t_new; rows of k_new, v_new beyond them are not read.
+ *   t_new         host: the bound that sizes the launch
+ * Every store is left one step ahead of its sequence (as innerq_decode_step_ragged wants and keeps it).  Counts
+ * outside their bounds are clamped on the device (a sequence that would pass capacity_tokens takes the tokens that
+ * fit); no buffer is overrun. */
+int innerq_append_rotated_ragged(const innerq_config_t *cfg, const innerq_cache_t *cache,
+                                 const innerq_rotation_t *rotation, const int32_t *positions, int32_t *n_tokens_dev,
+                                 const int32_t *t_new_dev, const void *k_new, const innerq_strides_t *k_strides,
+                                 const void *v_new, const innerq_strides_t *v_strides, int64_t t_new,
+                                 const float *k_inv_norm, void *hip_stream);
+
 /* Measurement hook (no counterpart in the paper; its Section "Latency" times the fused
  * dequantise-and-multiply kernels on their own, and this lets a benchmark do the same).
  * The next attention call made by the calling host thread (innerq_decode_attention,

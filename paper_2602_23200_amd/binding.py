@@ -39,6 +39,15 @@ class innerq_cache_t(C.Structure):
                                                            ("page_table", C.c_void_p)]
 
 
+class innerq_strides_t(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("head", C.c_int64), ("token", C.c_int64)]
+
+
+class innerq_rotation_t(C.Structure):
+    _fields_ = [("cos_table", C.c_void_p), ("sin_table", C.c_void_p), ("table_positions", C.c_int64),
+                ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("n_axes", C.c_int32), ("pair_axis", C.c_uint8 * 64)]
+
+
 class InnerQError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -95,6 +104,16 @@ def lib() -> C.CDLL:
         L.innerq_decode_step_ragged.restype = C.c_int
         L.innerq_append_deferred.argtypes = [cfgp, cachep, C.c_void_p, C.c_void_p, C.c_void_p]
         L.innerq_append_deferred.restype = C.c_int
+        rotp, strp = C.POINTER(innerq_rotation_t), C.POINTER(innerq_strides_t)
+        L.innerq_rotate.argtypes = [cfgp, rotp, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, strp, C.c_void_p, strp,
+                                    C.c_int32, C.c_int64, C.c_void_p]
+        L.innerq_rotate.restype = C.c_int
+        L.innerq_append_rotated.argtypes = [cfgp, cachep, rotp, C.c_void_p, C.c_void_p, strp, C.c_void_p, strp, C.c_int64, C.c_void_p,
+                                            C.c_void_p]
+        L.innerq_append_rotated.restype = C.c_int
+        L.innerq_append_rotated_ragged.argtypes = [cfgp, cachep, rotp, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, strp, C.c_void_p,
+                                                   strp, C.c_int64, C.c_void_p, C.c_void_p]
+        L.innerq_append_rotated_ragged.restype = C.c_int
         L.innerq_profile_next_attention.argtypes = [C.c_void_p, C.c_void_p]
         L.innerq_profile_next_attention.restype = C.c_int
         L.innerq_select_inner_kernel.argtypes = [C.c_int]
@@ -358,6 +377,106 @@ def innerq_append_deferred(cache: Cache, k_new, v_new, stream=None) -> None:
                                       _stream(stream))
     if st != OK:
         raise InnerQError(st, "innerq_append_deferred")
+
+
+# ---- several new tokens of a sequence at once: rows [B, H, T, d] fp16 wherever they lie (a projection's output [B, T, H, d]
+# transposed, say); channels contiguous, strides multiples of eight elements.
+
+@dataclass
+class Rotation:
+    """Rotary positions: the caller's tables (kept alive here) and the C struct that names them."""
+    c: innerq_rotation_t
+    tables: tuple
+
+
+def make_rotation(cos, sin, interleaved: bool = False, pair_axis=None) -> Rotation:
+    """cos, sin: fp32 CUDA tensors [positions, rot_dim / 2]; pair_axis: the axis (0 to 2) of every pair, or None: one axis."""
+    import torch
+    for t in (cos, sin):
+        assert t.dtype == torch.float32 and t.is_contiguous() and t.is_cuda and t.dim() == 2
+    assert cos.shape == sin.shape and 1 <= cos.shape[1] <= 64
+    axes = [0] * cos.shape[1] if pair_axis is None else [int(a) for a in pair_axis]
+    assert len(axes) == cos.shape[1] and all(0 <= a <= 2 for a in axes)
+    c = innerq_rotation_t(cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], int(interleaved), max(axes) + 1)
+    c.pair_axis[:len(axes)] = axes
+    return Rotation(c, (cos, sin))
+
+
+def _rows(t, cfg: innerq_config_t, heads: int, tokens: int, dtype=None):
+    """Pointer and strides of rows [B, H, T, d]."""
+    import torch
+    assert t.is_cuda and t.dtype == (dtype or torch.float16) and tuple(t.shape) == (cfg.batch, heads, tokens, cfg.head_dim)
+    assert t.stride(3) == 1
+    # (a dimension of one has no stride to speak of)
+    return t.data_ptr(), C.byref(innerq_strides_t(*(t.stride(i) if t.shape[i] > 1 else 0 for i in range(3))))
+
+
+def _positions(positions, rotation: Optional[Rotation], cfg: innerq_config_t, tokens: int) -> Optional[int]:
+    import torch
+    if positions is None or rotation is None:
+        return None
+    assert positions.is_cuda and positions.dtype == torch.int32 and positions.is_contiguous()
+    axes = rotation.c.n_axes
+    assert tuple(positions.shape) == (axes, cfg.batch, tokens) or (axes == 1 and tuple(positions.shape) == (cfg.batch, tokens))
+    return positions.data_ptr()
+
+
+def _counts(t, cfg: innerq_config_t) -> Optional[int]:
+    import torch
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == (cfg.batch,)
+    return t.data_ptr()
+
+
+def innerq_rotate(cfg: innerq_config_t, rotation: Rotation, x, out=None, positions=None, n_tokens: int = 0, n_tokens_dev=None,
+                  t_new_dev=None, stream=None):
+    """x [B, H, T, d] rotated into out (x itself for in place; a new tensor of x's layout if None).  positions int32 [axes, B, T], or
+    None: token t stands at n_tokens (n_tokens_dev[b]) + t."""
+    import torch
+    if out is None:
+        out = torch.empty_like(x)
+    xp, xs = _rows(x, cfg, x.shape[1], x.shape[2])
+    yp, ys = _rows(out, cfg, x.shape[1], x.shape[2])
+    st = lib().innerq_rotate(C.byref(cfg), C.byref(rotation.c), _positions(positions, rotation, cfg, x.shape[2]), n_tokens,
+                             _counts(n_tokens_dev, cfg), _counts(t_new_dev, cfg), xp, xs, yp, ys, x.shape[1], x.shape[2], _stream(stream))
+    if st != OK:
+        raise InnerQError(st, "innerq_rotate")
+    return out
+
+
+def _factors(f, cfg: innerq_config_t) -> Optional[int]:
+    import torch
+    if f is None:
+        return None
+    assert f.is_cuda and f.dtype == torch.float32 and f.is_contiguous() and tuple(f.shape) == (cfg.n_kv_heads, cfg.head_dim)
+    return f.data_ptr()
+
+
+def innerq_append_rotated(cache: Cache, k_new, v_new, rotation: Optional[Rotation] = None, positions=None, k_inv_norm=None,
+                          stream=None) -> None:
+    """innerq_quantize_append of k_new, v_new [B, Hk, T, d] where they lie, the keys rotated on their way in."""
+    cfg, T = cache.cfg, k_new.shape[2]
+    kp, ks = _rows(k_new, cfg, cfg.n_kv_heads, T)
+    vp, vs = _rows(v_new, cfg, cfg.n_kv_heads, T)
+    st = lib().innerq_append_rotated(C.byref(cfg), C.byref(cache.c), None if rotation is None else C.byref(rotation.c),
+                                     _positions(positions, rotation, cfg, T), kp, ks, vp, vs, T, _factors(k_inv_norm, cfg), _stream(stream))
+    if st != OK:
+        raise InnerQError(st, "innerq_append_rotated")
+
+
+def innerq_append_rotated_ragged(cache: Cache, n_tokens_dev, t_new_dev, k_new, v_new, rotation: Optional[Rotation] = None,
+                                 positions=None, k_inv_norm=None, stream=None) -> None:
+    """innerq_append_rotated with the counts of every sequence in device memory (int32 CUDA tensors [B]): n_tokens_dev cached,
+    advanced by the call, t_new_dev new ones, at most T; every store is left one step ahead."""
+    cfg, T = cache.cfg, k_new.shape[2]
+    kp, ks = _rows(k_new, cfg, cfg.n_kv_heads, T)
+    vp, vs = _rows(v_new, cfg, cfg.n_kv_heads, T)
+    st = lib().innerq_append_rotated_ragged(C.byref(cfg), C.byref(cache.c), None if rotation is None else C.byref(rotation.c),
+                                            _positions(positions, rotation, cfg, T), _counts(n_tokens_dev, cfg), _counts(t_new_dev, cfg),
+                                            kp, ks, vp, vs, T, _factors(k_inv_norm, cfg), _stream(stream))
+    if st != OK:
+        raise InnerQError(st, "innerq_append_rotated_ragged")
 
 
 def innerq_profile_next_attention(ev_start: Optional[int], ev_stop: Optional[int]) -> None:

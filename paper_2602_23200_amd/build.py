@@ -18,6 +18,8 @@ SOURCES = {
     "quantize.hip": ["-ffp-contract=off"],
     "quantize_owners.hip": ["-ffp-contract=off"],
     "quantize_owners_g64.hip": ["-ffp-contract=off"],
+    # (rotated values feed the quantiser: the same holds for them)
+    "rotate_append.hip": ["-ffp-contract=off"],
     "attention_generic.hip": [],
     "stream_probe.hip": [],
     "attention_fp16.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],

@@ -8,6 +8,7 @@
 
 #include "innerq_dev.h"
 #include "plan.h"
+#include "rows.h"
 
 using namespace innerq;
 
@@ -611,6 +612,155 @@ int innerq_decode_step(const innerq_config_t* cfg, innerq_cache_t* cache, const 
   cache->n_tokens = n + 1;
   cache->store_ahead_tokens = to;
   return INNERQ_OK;
+}
+
+}  // extern "C"
+
+// ---- several new tokens of a sequence at once (rows named by strides)
+
+namespace {
+
+constexpr long long kMostCapacity = 1LL << 24;           // token indices of these calls are 32-bit, their products with head_dim too
+
+int check_rows(const void* p, const innerq_strides_t* s, int unit = 8) {
+  if (!p || !s) return INNERQ_E_NULL;
+  if (misaligned(p)) return INNERQ_E_ALIGN;
+  for (const int64_t x : {s->batch, s->head, s->token}) {
+    if (x < 0) return INNERQ_E_ARG;
+    if (x % unit != 0) return INNERQ_E_ALIGN;
+  }
+  return INNERQ_OK;
+}
+// Rows that are written: no two of them the same.
+int check_rows_out(const void* p, const innerq_strides_t* s, long long batch, long long heads, long long tokens, int unit = 8) {
+  const int st = check_rows(p, s, unit);
+  if (st != INNERQ_OK) return st;
+  const struct { int64_t stride; long long n; } dims[3] = {{s->batch, batch}, {s->head, heads}, {s->token, tokens}};
+  for (const auto& d : dims)
+    if (d.n > 1 && d.stride < kHeadDim) return INNERQ_E_ARG;
+  return INNERQ_OK;
+}
+RowView rows_of(const void* p, const innerq_strides_t& s) { return {static_cast<const __half*>(p), s.batch, s.head, s.token}; }
+
+// positions: [n_axes][batch][t_new]
+int rotation_args(const innerq_rotation_t* r, const int32_t* positions, long long batch, long long t_new, RotArgs& a) {
+  if (!r || !r->cos_table || !r->sin_table) return INNERQ_E_NULL;
+  if (r->rot_dim < 2 || r->rot_dim > kHeadDim || r->rot_dim % 2 != 0) return INNERQ_E_ARG;
+  if (r->table_positions < 1 || r->table_positions > 0x7fffffffLL) return INNERQ_E_ARG;
+  if ((r->interleaved != 0 && r->interleaved != 1) || r->n_axes < 1 || r->n_axes > 3) return INNERQ_E_ARG;
+  a.axis_low = a.axis_high = 0;
+  for (int i = 0; i < r->rot_dim / 2; ++i) {
+    if (r->pair_axis[i] >= r->n_axes) return INNERQ_E_ARG;
+    a.axis_low |= (unsigned long long)(r->pair_axis[i] & 1) << i;
+    a.axis_high |= (unsigned long long)(r->pair_axis[i] >> 1) << i;
+  }
+  if (r->rot_dim % 16 != 0) return INNERQ_E_UNSUPPORTED;
+  if (misaligned(r->cos_table) || misaligned(r->sin_table) || (reinterpret_cast<uintptr_t>(positions) & 3u)) return INNERQ_E_ALIGN;
+  a.cos = r->cos_table; a.sin = r->sin_table;
+  a.positions = positions;
+  a.axis_stride = batch * t_new;
+  a.last_position = (int)(r->table_positions - 1);
+  a.pairs = r->rot_dim / 2;
+  a.interleaved = r->interleaved;
+  return INNERQ_OK;
+}
+
+int check_counts(const int32_t* n_tokens_dev, const int32_t* t_new_dev) {
+  if (!n_tokens_dev || !t_new_dev) return INNERQ_E_NULL;
+  return ((reinterpret_cast<uintptr_t>(n_tokens_dev) | reinterpret_cast<uintptr_t>(t_new_dev)) & 3u) ? INNERQ_E_ALIGN : INNERQ_OK;
+}
+
+// Config, cache and kind of a call over several tokens.
+int check_chunk_call(const innerq_config_t* cfg, const innerq_cache_t* cache) {
+  int st = check_config(cfg);
+  if (st != INNERQ_OK) return st;
+  st = check_cache(*cfg, cache);
+  if (st != INNERQ_OK) return st;
+  return cfg->kind != INNERQ_KIND_INNER || cfg->capacity_tokens > kMostCapacity ? INNERQ_E_UNSUPPORTED : INNERQ_OK;
+}
+
+int append_rows(const innerq_config_t* cfg, const innerq_cache_t* cache, const innerq_rotation_t* rotation, const int32_t* positions,
+                int32_t* n_tokens_dev, const int32_t* t_new_dev, const void* k_new, const innerq_strides_t* k_strides, const void* v_new,
+                const innerq_strides_t* v_strides, int64_t t_new, const float* k_inv_norm, void* hip_stream) {
+  int st = check_rows(k_new, k_strides);
+  if (st == INNERQ_OK) st = check_rows(v_new, v_strides);
+  if (st != INNERQ_OK) return st;
+  if (k_inv_norm && misaligned(k_inv_norm)) return INNERQ_E_ALIGN;
+  AppendArgs a;
+  a.rot = RotArgs{};
+  if (rotation) {
+    st = rotation_args(rotation, positions, cfg->batch, t_new, a.rot);
+    if (st != INNERQ_OK) return st;
+  }
+  a.q = quant_args(cfg, cache, nullptr, nullptr, t_new, k_inv_norm, cache->n_tokens, cache->n_tokens);
+  a.q.job[0].normalise = 0;                              // (keys are scaled where they are rotated)
+  a.q.n_dev = n_tokens_dev;
+  a.k = rows_of(k_new, *k_strides);
+  a.v = rows_of(v_new, *v_strides);
+  a.t_dev = t_new_dev;
+  a.t_new = (int)t_new;
+  a.ahead = n_tokens_dev ? 1 : 0;
+  return launch_append_rows(a, n_tokens_dev, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? INNERQ_OK : INNERQ_E_HIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+int innerq_rotate(const innerq_config_t* cfg, const innerq_rotation_t* rotation, const int32_t* positions, int64_t n_tokens,
+                  const int32_t* n_tokens_dev, const int32_t* t_new_dev, const void* x, const innerq_strides_t* x_strides, void* y,
+                  const innerq_strides_t* y_strides, int32_t n_heads, int64_t t_new, void* hip_stream) {
+  int st = check_config(cfg);
+  if (st != INNERQ_OK) return st;
+  if (t_new < 0 || n_heads < 1 || n_heads > 65535 || (long long)cfg->batch * t_new > 0x7fffffffLL || t_new > 0x7fffffffLL) return INNERQ_E_ARG;
+  if (n_tokens < 0 || n_tokens > 0x7fffffffLL - t_new) return INNERQ_E_ARG;
+  RotateArgs a;
+  st = rotation_args(rotation, positions, cfg->batch, t_new, a.rot);
+  if (st != INNERQ_OK) return st;
+  if (t_new == 0) return INNERQ_OK;
+  st = check_rows(x, x_strides);
+  if (st == INNERQ_OK) st = check_rows_out(y, y_strides, cfg->batch, n_heads, t_new);
+  if (st != INNERQ_OK) return st;
+  if (((reinterpret_cast<uintptr_t>(n_tokens_dev) | reinterpret_cast<uintptr_t>(t_new_dev)) & 3u)) return INNERQ_E_ALIGN;
+  a.x = rows_of(x, *x_strides);
+  a.y = static_cast<__half*>(y);
+  a.y_batch = y_strides->batch; a.y_head = y_strides->head; a.y_token = y_strides->token;
+  a.batch = cfg->batch; a.n_heads = n_heads; a.t_new = (int)t_new;
+  a.heads_per_block = 1;
+  a.n_tokens = (int)n_tokens;
+  a.n_dev = n_tokens_dev;
+  a.t_dev = t_new_dev;
+  return launch_rotate(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? INNERQ_OK : INNERQ_E_HIP;
+}
+
+int innerq_append_rotated(const innerq_config_t* cfg, innerq_cache_t* cache, const innerq_rotation_t* rotation, const int32_t* positions,
+                          const void* k_new, const innerq_strides_t* k_strides, const void* v_new, const innerq_strides_t* v_strides,
+                          int64_t t_new, const float* k_inv_norm, void* hip_stream) {
+  int st = check_chunk_call(cfg, cache);
+  if (st != INNERQ_OK) return st;
+  if (t_new < 0) return INNERQ_E_ARG;
+  if (t_new == 0) return INNERQ_OK;
+  if (t_new > cfg->capacity_tokens - cache->n_tokens) return INNERQ_E_CAPACITY;
+  st = append_rows(cfg, cache, rotation, positions, nullptr, nullptr, k_new, k_strides, v_new, v_strides, t_new, k_inv_norm, hip_stream);
+  if (st != INNERQ_OK) return st;
+  cache->n_tokens += t_new;
+  cache->store_ahead_tokens = cache->n_tokens;
+  return INNERQ_OK;
+}
+
+int innerq_append_rotated_ragged(const innerq_config_t* cfg, const innerq_cache_t* cache, const innerq_rotation_t* rotation,
+                                 const int32_t* positions, int32_t* n_tokens_dev, const int32_t* t_new_dev, const void* k_new,
+                                 const innerq_strides_t* k_strides, const void* v_new, const innerq_strides_t* v_strides, int64_t t_new,
+                                 const float* k_inv_norm, void* hip_stream) {
+  innerq_cache_t view = cache ? *cache : innerq_cache_t{};
+  view.n_tokens = 0;                                    // (the host counter is not used on this path)
+  int st = check_chunk_call(cfg, cache ? &view : nullptr);
+  if (st == INNERQ_OK) st = check_counts(n_tokens_dev, t_new_dev);
+  if (st != INNERQ_OK) return st;
+  if (t_new < 0) return INNERQ_E_ARG;
+  if (t_new == 0) return INNERQ_OK;
+  if (t_new > cfg->capacity_tokens) return INNERQ_E_CAPACITY;
+  return append_rows(cfg, &view, rotation, positions, n_tokens_dev, t_new_dev, k_new, k_strides, v_new, v_strides, t_new, k_inv_norm, hip_stream);
 }
 
 }  // extern "C"
