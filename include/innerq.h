@@ -415,6 +415,37 @@ int innerq_append_rotated_ragged(const innerq_config_t *cfg, const innerq_cache_
                                  const void *v_new, const innerq_strides_t *v_strides, int64_t t_new,
                                  const float *k_inv_norm, void *hip_stream);
 
+/* Attention of the next t_new tokens of every sequence: query i stands behind the n cached tokens and the new tokens
+ * 0 .. i - 1 and attends to all of them and to its own,
+ *   out_i = softmax(q_i [K_cached; k_new_0 .. k_new_i]^T / sqrt(d)) [V_cached; v_new_0 .. v_new_i],
+ * the cached tokens as the cache holds them (windows fp16, store dequantised), the new ones as they are given
+ * (rotated, and divided by the key-norm factors if the cached ones are).  The cache is not modified: a program
+ * appends afterwards what it keeps of the chunk or the draft.  Any number of query heads per kv head; n may be 0.
+ *   q, out      fp16 rows; out fp32 rows if out_is_fp32 (strides then multiples of 4), not overlapping an input
+ *   q_scale     device, fp32 [Hk][d] or NULL: as for innerq_decode_attention
+ *   workspace   device scratch of innerq_chunk_workspace_bytes(cfg, t_new) bytes, content undefined; calls that may
+ *               run at the same time need one each
+ * Products are taken of fp16 operands on the matrix cores, accumulated in fp32: dequantised keys and values and the
+ * softmax weights are rounded to fp16 (relative 2^-12 rms each), statistics and sums are fp32.  Cached values up to
+ * 65000 in magnitude; inputs finite (rows beyond a sequence's count are not read). */
+size_t innerq_chunk_workspace_bytes(const innerq_config_t *cfg, int64_t t_new);
+int innerq_chunk_attention(const innerq_config_t *cfg, const innerq_cache_t *cache, const void *k_new,
+                           const innerq_strides_t *k_strides, const void *v_new, const innerq_strides_t *v_strides,
+                           const void *q, const innerq_strides_t *q_strides, int64_t t_new, const float *q_scale,
+                           void *out, const innerq_strides_t *out_strides, int out_is_fp32, void *workspace,
+                           size_t workspace_bytes, void *hip_stream);
+
+/* The same with the counts of every sequence in DEVICE memory (innerq_append_rotated_ragged): n_tokens_dev cached
+ * (read only here), t_new_dev new tokens, 0 .. t_new.  max_tokens (host) bounds n_tokens_dev[b] + t_new_dev[b] and
+ * only sizes the launch.  Rows of out beyond a sequence's count are left as they were. */
+int innerq_chunk_attention_ragged(const innerq_config_t *cfg, const innerq_cache_t *cache,
+                                  const int32_t *n_tokens_dev, const int32_t *t_new_dev, int64_t max_tokens,
+                                  const void *k_new, const innerq_strides_t *k_strides, const void *v_new,
+                                  const innerq_strides_t *v_strides, const void *q,
+                                  const innerq_strides_t *q_strides, int64_t t_new, const float *q_scale, void *out,
+                                  const innerq_strides_t *out_strides, int out_is_fp32, void *workspace,
+                                  size_t workspace_bytes, void *hip_stream);
+
 /* Measurement hook (no counterpart in the paper; its Section "Latency" times the fused
  * dequantise-and-multiply kernels on their own, and this lets a benchmark do the same).
  * The next attention call made by the calling host thread (innerq_decode_attention,

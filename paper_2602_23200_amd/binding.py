@@ -114,6 +114,15 @@ def lib() -> C.CDLL:
         L.innerq_append_rotated_ragged.argtypes = [cfgp, cachep, rotp, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, strp, C.c_void_p,
                                                    strp, C.c_int64, C.c_void_p, C.c_void_p]
         L.innerq_append_rotated_ragged.restype = C.c_int
+        L.innerq_chunk_workspace_bytes.argtypes = [cfgp, C.c_int64]
+        L.innerq_chunk_workspace_bytes.restype = C.c_size_t
+        L.innerq_chunk_attention.argtypes = [cfgp, cachep, C.c_void_p, strp, C.c_void_p, strp, C.c_void_p, strp, C.c_int64, C.c_void_p,
+                                             C.c_void_p, strp, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.innerq_chunk_attention.restype = C.c_int
+        L.innerq_chunk_attention_ragged.argtypes = [cfgp, cachep, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, strp, C.c_void_p, strp,
+                                                    C.c_void_p, strp, C.c_int64, C.c_void_p, C.c_void_p, strp, C.c_int, C.c_void_p,
+                                                    C.c_size_t, C.c_void_p]
+        L.innerq_chunk_attention_ragged.restype = C.c_int
         L.innerq_profile_next_attention.argtypes = [C.c_void_p, C.c_void_p]
         L.innerq_profile_next_attention.restype = C.c_int
         L.innerq_select_inner_kernel.argtypes = [C.c_int]
@@ -477,6 +486,60 @@ def innerq_append_rotated_ragged(cache: Cache, n_tokens_dev, t_new_dev, k_new, v
                                             kp, ks, vp, vs, T, _factors(k_inv_norm, cfg), _stream(stream))
     if st != OK:
         raise InnerQError(st, "innerq_append_rotated_ragged")
+
+
+def innerq_chunk_workspace_bytes(cfg: innerq_config_t, t_new: int) -> int:
+    return lib().innerq_chunk_workspace_bytes(C.byref(cfg), t_new)
+
+
+def allocate_chunk_workspace(cfg: innerq_config_t, t_new: int, device="cuda"):
+    import torch
+    return torch.empty(innerq_chunk_workspace_bytes(cfg, t_new), dtype=torch.uint8, device=device)
+
+
+def _chunk_out(out, q):
+    """The output rows: a new fp32 tensor [B, T, Hq, d] seen as [B, Hq, T, d] where none is given."""
+    import torch
+    if out is None:
+        B, H, T, d = q.shape
+        out = torch.empty(B, T, H, d, dtype=torch.float32, device=q.device).transpose(1, 2)
+    assert out.dtype in (torch.float32, torch.float16)
+    return out
+
+
+def innerq_chunk_attention(cache: Cache, k_new, v_new, q, workspace, out=None, q_scale=None, stream=None):
+    """q [B, Hq, T, d] attends to the cache and causally to the new rows k_new, v_new [B, Hk, T, d] (not appended by this call)
+    -> out [B, Hq, T, d] (fp32 unless an fp16 `out` is passed)."""
+    cfg, T = cache.cfg, q.shape[2]
+    out = _chunk_out(out, q)
+    kp, ks = _rows(k_new, cfg, cfg.n_kv_heads, T)
+    vp, vs = _rows(v_new, cfg, cfg.n_kv_heads, T)
+    qp, qs = _rows(q, cfg, cfg.n_q_heads, T)
+    op, os_ = _rows(out, cfg, cfg.n_q_heads, T, out.dtype)
+    st = lib().innerq_chunk_attention(C.byref(cfg), C.byref(cache.c), kp, ks, vp, vs, qp, qs, T, _factors(q_scale, cfg), op, os_,
+                                      int(out.element_size() == 4), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                      _stream(stream))
+    if st != OK:
+        raise InnerQError(st, "innerq_chunk_attention")
+    return out
+
+
+def innerq_chunk_attention_ragged(cache: Cache, n_tokens_dev, t_new_dev, max_tokens: int, k_new, v_new, q, workspace, out=None,
+                                  q_scale=None, stream=None):
+    """innerq_chunk_attention with the counts of every sequence in device memory (int32 CUDA tensors [B]): n_tokens_dev cached,
+    t_new_dev new ones, at most T; max_tokens bounds their sum.  Rows of `out` beyond a sequence's new tokens are left as they were."""
+    cfg, T = cache.cfg, q.shape[2]
+    out = _chunk_out(out, q)
+    kp, ks = _rows(k_new, cfg, cfg.n_kv_heads, T)
+    vp, vs = _rows(v_new, cfg, cfg.n_kv_heads, T)
+    qp, qs = _rows(q, cfg, cfg.n_q_heads, T)
+    op, os_ = _rows(out, cfg, cfg.n_q_heads, T, out.dtype)
+    st = lib().innerq_chunk_attention_ragged(C.byref(cfg), C.byref(cache.c), _counts(n_tokens_dev, cfg), _counts(t_new_dev, cfg), max_tokens,
+                                             kp, ks, vp, vs, qp, qs, T, _factors(q_scale, cfg), op, os_, int(out.element_size() == 4),
+                                             workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream))
+    if st != OK:
+        raise InnerQError(st, "innerq_chunk_attention_ragged")
+    return out
 
 
 def innerq_profile_next_attention(ev_start: Optional[int], ev_stop: Optional[int]) -> None:

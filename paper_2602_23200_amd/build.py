@@ -34,6 +34,8 @@ SOURCES = {
     "attention_join_g64.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "attention_join_paged.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "attention_join_paged_g64.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "attention_chunk.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "attention_chunk_g64.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],
     "attention_inner_f4.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 

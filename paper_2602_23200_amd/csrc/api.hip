@@ -7,6 +7,7 @@
 #include <mutex>
 
 #include "innerq_dev.h"
+#include "attention_chunk.h"
 #include "plan.h"
 #include "rows.h"
 
@@ -703,6 +704,57 @@ int append_rows(const innerq_config_t* cfg, const innerq_cache_t* cache, const i
   return launch_append_rows(a, n_tokens_dev, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? INNERQ_OK : INNERQ_E_HIP;
 }
 
+// Whether the rows of such a chunk can be counted in 31 bits.
+bool chunk_rows_fit(const innerq_config_t& c, long long t_new) { return t_new <= kMostCapacity && t_new * c.n_q_heads * c.batch < (1LL << 31); }
+
+ChunkTensor chunk_tensor(const innerq_config_t& c, const innerq_cache_t& k, int which, const void* fresh, const innerq_strides_t& s) {
+  const TensorView v = view_of(c, k, which, 0);
+  return {v.codes, v.scales, v.zeros, v.sink, v.ring, rows_of(fresh, s), v.slots};
+}
+
+// tokens: the most that a query attends to, cached and new ones.
+int chunk_attention(const innerq_config_t* cfg, const innerq_cache_t* cache, const int32_t* n_tokens_dev, const int32_t* t_new_dev, long long tokens,
+                    const void* k_new, const innerq_strides_t* k_strides, const void* v_new, const innerq_strides_t* v_strides, const void* q,
+                    const innerq_strides_t* q_strides, int64_t t_new, const float* q_scale, void* out, const innerq_strides_t* out_strides,
+                    int out_is_fp32, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const innerq_config_t& c = *cfg;
+  int st = check_rows(k_new, k_strides);
+  if (st == INNERQ_OK) st = check_rows(v_new, v_strides);
+  if (st == INNERQ_OK) st = check_rows(q, q_strides);
+  if (st == INNERQ_OK) st = check_rows_out(out, out_strides, c.batch, c.n_q_heads, t_new, out_is_fp32 ? 4 : 8);
+  if (st != INNERQ_OK) return st;
+  if (!workspace) return INNERQ_E_NULL;
+  if (misaligned(workspace) || (q_scale && misaligned(q_scale))) return INNERQ_E_ALIGN;
+  if (!chunk_rows_fit(c, t_new)) return INNERQ_E_UNSUPPORTED;
+  const ChunkSizes sizes = chunk_sizes(c, t_new);
+  if (workspace_bytes < sizes.bytes) return INNERQ_E_WORKSPACE;
+  ChunkArgs a;
+  a.k = chunk_tensor(c, *cache, 0, k_new, *k_strides);
+  a.v = chunk_tensor(c, *cache, 1, v_new, *v_strides);
+  a.q = rows_of(q, *q_strides);
+  a.q_scale = q_scale;
+  a.out = out;
+  a.out_batch = out_strides->batch; a.out_head = out_strides->head; a.out_token = out_strides->token;
+  a.out_is_fp32 = out_is_fp32;
+  a.batch = c.batch; a.n_q_heads = c.n_q_heads; a.n_kv_heads = c.n_kv_heads; a.heads_per_kv = c.n_q_heads / c.n_kv_heads;
+  a.w_sink = c.w_sink; a.w_recent = c.w_recent;
+  a.capacity = c.capacity_tokens;
+  a.t_new = (int)t_new;
+  a.n_tokens = (int)cache->n_tokens;
+  a.n_dev = n_tokens_dev;
+  a.t_dev = t_new_dev;
+  a.row_blocks = (int)sizes.row_blocks;
+  a.n_splits = chunk_splits(sizes, tokens);
+  a.ws_ml = static_cast<float*>(workspace);
+  a.ws_o = a.ws_ml + (sizes.heads * sizes.rows * a.n_splits * 2 + 3) / 4 * 4;
+  a.pages = pages_of(c, *cache);
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  hipError_t e = c.group == 32 ? launch_chunk_g32(a, bits_of(c, 0), bits_of(c, 1), sizes.form, stream)
+                               : launch_chunk_g64(a, bits_of(c, 0), bits_of(c, 1), sizes.form, stream);
+  if (e == hipSuccess && a.n_splits > 1) e = launch_chunk_merge(a, stream);
+  return e == hipSuccess ? INNERQ_OK : INNERQ_E_HIP;
+}
+
 }  // namespace
 
 extern "C" {
@@ -761,6 +813,41 @@ int innerq_append_rotated_ragged(const innerq_config_t* cfg, const innerq_cache_
   if (t_new == 0) return INNERQ_OK;
   if (t_new > cfg->capacity_tokens) return INNERQ_E_CAPACITY;
   return append_rows(cfg, &view, rotation, positions, n_tokens_dev, t_new_dev, k_new, k_strides, v_new, v_strides, t_new, k_inv_norm, hip_stream);
+}
+
+size_t innerq_chunk_workspace_bytes(const innerq_config_t* cfg, int64_t t_new) {
+  if (check_config(cfg) != INNERQ_OK || cfg->kind != INNERQ_KIND_INNER || t_new < 1 || !chunk_rows_fit(*cfg, t_new)) return 0;
+  return chunk_sizes(*cfg, t_new).bytes;
+}
+
+int innerq_chunk_attention(const innerq_config_t* cfg, const innerq_cache_t* cache, const void* k_new, const innerq_strides_t* k_strides,
+                           const void* v_new, const innerq_strides_t* v_strides, const void* q, const innerq_strides_t* q_strides, int64_t t_new,
+                           const float* q_scale, void* out, const innerq_strides_t* out_strides, int out_is_fp32, void* workspace,
+                           size_t workspace_bytes, void* hip_stream) {
+  const int st = check_chunk_call(cfg, cache);
+  if (st != INNERQ_OK) return st;
+  if (t_new < 0) return INNERQ_E_ARG;
+  if (t_new == 0) return INNERQ_OK;
+  if (t_new > cfg->capacity_tokens - cache->n_tokens) return INNERQ_E_CAPACITY;
+  return chunk_attention(cfg, cache, nullptr, nullptr, cache->n_tokens + t_new, k_new, k_strides, v_new, v_strides, q, q_strides, t_new, q_scale, out,
+                         out_strides, out_is_fp32, workspace, workspace_bytes, hip_stream);
+}
+
+int innerq_chunk_attention_ragged(const innerq_config_t* cfg, const innerq_cache_t* cache, const int32_t* n_tokens_dev, const int32_t* t_new_dev,
+                                  int64_t max_tokens, const void* k_new, const innerq_strides_t* k_strides, const void* v_new,
+                                  const innerq_strides_t* v_strides, const void* q, const innerq_strides_t* q_strides, int64_t t_new,
+                                  const float* q_scale, void* out, const innerq_strides_t* out_strides, int out_is_fp32, void* workspace,
+                                  size_t workspace_bytes, void* hip_stream) {
+  innerq_cache_t view = cache ? *cache : innerq_cache_t{};
+  view.n_tokens = 0;                                    // (the host counter is not used on this path)
+  int st = check_chunk_call(cfg, cache ? &view : nullptr);
+  if (st == INNERQ_OK) st = check_counts(n_tokens_dev, t_new_dev);
+  if (st != INNERQ_OK) return st;
+  if (t_new < 0 || max_tokens < 1) return INNERQ_E_ARG;
+  if (t_new == 0) return INNERQ_OK;
+  if (max_tokens > cfg->capacity_tokens || t_new > cfg->capacity_tokens) return INNERQ_E_CAPACITY;
+  return chunk_attention(cfg, &view, n_tokens_dev, t_new_dev, max_tokens, k_new, k_strides, v_new, v_strides, q, q_strides, t_new, q_scale, out,
+                         out_strides, out_is_fp32, workspace, workspace_bytes, hip_stream);
 }
 
 }  // extern "C"

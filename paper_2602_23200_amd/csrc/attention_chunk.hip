@@ -1,0 +1,607 @@
+// Attention of several new tokens of a sequence: query row (token i, head h) attends to the n cached tokens, as the cache holds
+// them, and to the new tokens 0 .. i.
+//
+// Rows of one kv head (its query heads x the new tokens) share every key and value, so keys and values are brought to fp16 once a
+// work-group, in LDS, and the products are matrix products:
+//   S^T = K Q^T   (32 x 32 x 16 instructions: rows are tokens, columns query rows)
+//   O^T = V^T P^T (rows are channels)
+// With the transposed products a lane holds sixteen scores of ONE query row, so the softmax statistics are the lane's own but for one
+// exchange of the two halves of a wavefront, and its weights are, rounded to fp16, the operand of the second product where they stand: the order of
+// the tokens inside a product does not matter as long as both operands agree, so V^T is laid out in LDS in the order in which the first
+// product leaves the tokens (16 tokens: 0 8 1 9 2 10 3 11 4 12 ...), which is also the order in which fields come out of packed words
+// two at a time.  Keys use the same order for channels, queries are brought into it once.
+//
+// Stored fields become fp16 exactly: masked in place under the exponent that gives their bits weight one (1024 + u, 256 + u, ..), that
+// constant subtracted (exact), then one fused |S| u + Z rounded to fp16 (relative 2^-12 rms, as the weights; scores, statistics and sums are fp32).
+//
+// The softmax reference level is raised only when a score passes it by 2^6 (weights up to 2^6 are far from fp16's end): the outputs
+// are scaled rarely.
+#include "attention_chunk.h"
+
+#ifndef INNERQ_CHUNK_G
+#define INNERQ_CHUNK_G 32
+#endif
+
+namespace innerq {
+namespace {
+
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef float float16_t __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int D = kHeadDim;
+constexpr int kKeyPitch = 2 * D + 16;                    // bytes of a key row in LDS (16 apart in the banks)
+constexpr float kRaise = 6.0f;                           // log2 of the largest weight before the level is raised
+
+__device__ __forceinline__ half2_t as_half2(uint32_t w) { return __builtin_bit_cast(half2_t, w); }
+__device__ __forceinline__ uint32_t as_u32(half2_t h) { return __builtin_bit_cast(uint32_t, h); }
+__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+__device__ __forceinline__ float other_half(float x) {   // lane ^ 32
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float((threadIdx.x & 32u) ? r[0] : r[1]);
+}
+
+// ---- packed fields
+
+// 32 fields of one group (a quarter of a key row, 32 tokens of a value channel) as they are loaded.
+template <int BITS>
+struct Piece {
+  static constexpr int BYTES = 32 * (BITS == 3 ? 2 : BITS) / 8;       // of the (low) plane
+  uint32_t w[BITS];
+  uint32_t scale, zero;
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < BITS; ++i) w[i] = 0u;
+    scale = zero = 0u;
+  }
+  // low: the fields (3-bit: their low two bits), high: the plane of high bits
+  __device__ __forceinline__ void load(const uint8_t* low, const uint8_t* high, const __half* s, const __half* z) {
+    if constexpr (BITS == 4) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(low);
+      w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+    } else {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(low);
+      w[0] = x.x; w[1] = x.y;
+      if constexpr (BITS == 3) w[2] = *reinterpret_cast<const uint32_t*>(high);
+    }
+    scale = *reinterpret_cast<const unsigned short*>(s);
+    zero = z ? *reinterpret_cast<const unsigned short*>(z) : 0u;
+  }
+};
+
+template <int BITS>
+struct Decoder {
+  half2_t s, z;
+  half2_t off[5];                                        // -(1024 + o), -(256 + o), -(64 + o), -(16 + o), -(4 + o), o = 2^(b-1) if symmetric
+  __device__ __forceinline__ void start(uint32_t scale, uint32_t zero) {
+    const bool asym = (scale & 0x8000u) != 0u;
+    const uint32_t a = scale & 0x7fffu, b = asym ? zero : 0u;
+    s = as_half2(a | a << 16);
+    z = as_half2(b | b << 16);
+    constexpr float H = (float)(1 << (BITS - 1));
+#pragma unroll
+    for (int i = 0; i < 5; ++i) {
+      const float base = (float)(1024 >> (2 * i));
+      const half2_t c0 = {(_Float16)-base, (_Float16)-base}, c1 = {(_Float16)(-base - H), (_Float16)(-base - H)};
+      off[i] = asym ? c0 : c1;
+    }
+  }
+  // the field at bit AT of each half (AT even, up to 8)
+  template <int AT>
+  __device__ __forceinline__ uint32_t value(uint32_t x) const {
+    constexpr uint32_t mask = ((1u << BITS) - 1u) << AT, base = (25u - AT) << 10;
+    const half2_t raw = as_half2((x & (mask * 0x10001u)) | (base * 0x10001u));
+    return as_u32(__builtin_elementwise_fma(raw + off[AT / 2], s, z));
+  }
+};
+
+// The piece's 32 values as fp16, in the order of the products: 16 words.
+template <int BITS>
+__device__ __forceinline__ void decode(const Piece<BITS>& p, uint32_t (&out)[16]) {
+  Decoder<BITS> d;
+  d.start(p.scale, p.zero);
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    uint32_t* o = out + 8 * b;
+    if constexpr (BITS == 4) {
+      const uint32_t lo = low_halves(p.w[2 * b], p.w[2 * b + 1]), hi = high_halves(p.w[2 * b], p.w[2 * b + 1]);
+      o[0] = d.template value<0>(lo); o[1] = d.template value<4>(lo);
+      o[2] = d.template value<0>(lo >> 8); o[3] = d.template value<4>(lo >> 8);
+      o[4] = d.template value<0>(hi); o[5] = d.template value<4>(hi);
+      o[6] = d.template value<0>(hi >> 8); o[7] = d.template value<4>(hi >> 8);
+    } else if constexpr (BITS == 2) {
+      const uint32_t x = p.w[b], y = x >> 10;
+      o[0] = d.template value<0>(x); o[1] = d.template value<2>(x); o[2] = d.template value<4>(x);
+      o[3] = d.template value<6>(x); o[4] = d.template value<8>(x);
+      o[5] = d.template value<0>(y); o[6] = d.template value<2>(y); o[7] = d.template value<4>(y);
+    } else {
+      // three-bit fields put together in place: low bits of fields k and 8 + k at bits 2 k of the halves, their high bits at bit k of h
+      const uint32_t x = p.w[b], n = p.w[2] >> (16 * b);
+      const uint32_t h = (n & 0xffu) | (n & 0xff00u) << 8;
+      auto field = [&](uint32_t low, uint32_t high, int at) { return (low & (0x00030003u << at)) | (high & (0x00040004u << at)); };
+      const uint32_t y = x >> 8;
+      o[0] = d.template value<0>(field(x, h << 2, 0)); o[1] = d.template value<2>(field(x, h << 3, 2));
+      o[2] = d.template value<4>(field(x, h << 4, 4)); o[3] = d.template value<6>(field(x, h << 5, 6));
+      o[4] = d.template value<0>(field(y, h >> 2, 0)); o[5] = d.template value<2>(field(y, h >> 1, 2));
+      o[6] = d.template value<4>(field(y, h, 4)); o[7] = d.template value<6>(field(y, h << 1, 6));
+    }
+  }
+}
+
+__device__ __forceinline__ void put_words(char* dst, const uint32_t (&w)[16]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4*>(dst + 16 * i) = u32x4{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
+}
+
+// ---- a sequence
+
+// Cached and new tokens; sink tokens; packed rows of keys and of values.  Keys of a row: the packed_v rows of the store, then the rest in
+// order of their tokens (number w of them is token w of the sink, else token w + packed_v).
+struct ChunkSeq { int n, t, sink, packed_k, packed_v; };
+__device__ __forceinline__ ChunkSeq chunk_seq(const ChunkArgs& a, int b, int group) {
+  const int cap = (int)a.capacity;
+  ChunkSeq s;
+  s.n = a.n_tokens;
+  s.t = a.t_new;
+  if (a.n_dev) {
+    s.n = a.n_dev[b];
+    s.n = s.n < 0 ? 0 : s.n > cap ? cap : s.n;
+    s.t = a.t_dev[b];
+    s.t = s.t < 0 ? 0 : s.t > a.t_new ? a.t_new : s.t;
+  }
+  s.sink = s.n < a.w_sink ? s.n : a.w_sink;
+  s.packed_k = (int)quantised_rows(a.w_sink, a.w_recent, group, kPerToken, s.n);
+  s.packed_v = (int)quantised_rows(a.w_sink, a.w_recent, group, kPerChannel, s.n);
+  return s;
+}
+
+template <int KB, int VB, int G, int RW, int TW>
+struct ChunkKernel {
+  static constexpr int KT = RW == 1 ? 32 : 64;           // tokens of a tile
+  static constexpr int NB = KT / 32;                     // blocks of 32 of them
+  static constexpr int NT = 64 * RW;                     // threads that bring a tile
+  static constexpr int P = KT * 4 / NT;                  // pieces of each tensor a thread brings
+  static constexpr int VPITCH = 2 * KT + 16;             // bytes of a channel of V^T
+  static constexpr int VALUES = KT * kKeyPitch;          // where they begin
+  static constexpr int BUF = VALUES + D * VPITCH;
+  static constexpr int NBUF = RW == 1 ? 1 : 2;           // (a wavefront by itself takes its LDS operations in order)
+  static constexpr int JOIN = TW > 1 ? TW * (64 * 64 + 128) * 4 : 0;
+  static constexpr int LDS = BUF * NBUF * TW > JOIN ? BUF * NBUF * TW : JOIN;
+
+  struct Packed { Piece<KB> k[P]; Piece<VB> v[P]; };
+  struct Plain { u32x4 k[P][4]; u32x4 v[P][4]; };
+
+  // Tile of store rows row0 .. : pieces in registers.  (row0 is a multiple of the tile, so one page holds it.)
+  static __device__ __forceinline__ void load_packed(const ChunkArgs& a, const ChunkSeq& s, long long bh, int row0, int tid, Packed& x) {
+    const long long lin = store_row(a.pages, a.n_kv_heads, a.capacity, bh, row0);
+#pragma unroll
+    for (int m = 0; m < P; ++m) {
+      const int p = tid + m * NT;
+      const int tok = p >> 2, quarter = p & 3;
+      if (row0 + tok < s.packed_v) {
+        const uint8_t* row = a.k.codes + (lin + tok) * (D * KB / 8);
+        const long long at = (lin + tok) * (D / G) + quarter * 32 / G;
+        x.k[m].load(row + quarter * Piece<KB>::BYTES, row + D * 2 / 8 + quarter * 4, a.k.scales + at, a.k.zeros ? a.k.zeros + at : nullptr);
+      } else {
+        x.k[m].clear();
+      }
+      const int c = p % D, sub = p / D;                  // channel, block of 32 tokens
+      const int row = row0 + 32 * sub;
+      if (row < s.packed_v) {
+        const long long at = (lin + 32 * sub) / G * D + c;
+        const uint8_t* run = a.v.codes + at * (G * VB / 8);
+        const int part = G == 64 ? (row & 63) / 32 : 0;
+        x.v[m].load(run + part * Piece<VB>::BYTES, run + G * 2 / 8 + part * 4, a.v.scales + at, a.v.zeros ? a.v.zeros + at : nullptr);
+      } else {
+        x.v[m].clear();
+      }
+    }
+  }
+  static __device__ __forceinline__ void put_packed(char* buf, int tid, const Packed& x) {
+#pragma unroll
+    for (int m = 0; m < P; ++m) {
+      const int p = tid + m * NT;
+      uint32_t w[16];
+      decode<KB>(x.k[m], w);
+      put_words(buf + (p >> 2) * kKeyPitch + (p & 3) * 64, w);
+      decode<VB>(x.v[m], w);
+      put_words(buf + VALUES + (p % D) * VPITCH + (p / D) * 64, w);
+    }
+  }
+
+  // fp16 row of the token of number w (which must exist); null for a key that is packed.
+  static __device__ __forceinline__ const __half* plain_row(const ChunkArgs& a, const ChunkSeq& s, const ChunkTensor& x, int packed, int b, int h, int w) {
+    const long long bh = (long long)b * a.n_kv_heads + h;
+    if (w < s.sink) return x.sink + (bh * a.w_sink + w) * D;
+    const int token = w + s.packed_v;
+    if (token >= s.n) return x.fresh.p + b * x.fresh.batch + h * x.fresh.head + (token - s.n) * x.fresh.token;
+    if (token - a.w_sink < packed) return nullptr;
+    return x.ring + (bh * x.slots + (uint32_t)token % (uint32_t)x.slots) * D;
+  }
+  // Numbers w0 .. of the rest; end: behind the last one.
+  static __device__ __forceinline__ void load_plain(const ChunkArgs& a, const ChunkSeq& s, int b, int h, int w0, int end, int tid, Plain& x) {
+#pragma unroll
+    for (int m = 0; m < P; ++m) {
+      const int p = tid + m * NT;
+      {
+        const int w = w0 + (p >> 2), quarter = p & 3;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x.k[m][i] = u32x4{0u, 0u, 0u, 0u};
+        if (w < end) {
+          const __half* row = plain_row(a, s, a.k, s.packed_k, b, h, w);
+          if (row) {
+            const __half* src = row + quarter * 32;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x.k[m][i] = *reinterpret_cast<const u32x4*>(src + 8 * i);
+#pragma unroll
+            for (int i = 0; i < 4; i += 2) {
+              const u32x4 f = x.k[m][i], g = x.k[m][i + 1];
+              x.k[m][i] = u32x4{low_halves(f.x, g.x), high_halves(f.x, g.x), low_halves(f.y, g.y), high_halves(f.y, g.y)};
+              x.k[m][i + 1] = u32x4{low_halves(f.z, g.z), high_halves(f.z, g.z), low_halves(f.w, g.w), high_halves(f.w, g.w)};
+            }
+          } else {
+            // (a key that has left its window before the values of its group have left theirs)
+            const long long lin = store_row(a.pages, a.n_kv_heads, a.capacity, (long long)b * a.n_kv_heads + h, w + s.packed_v - a.w_sink);
+            const uint8_t* codes = a.k.codes + lin * (D * KB / 8);
+            const long long at = lin * (D / G) + quarter * 32 / G;
+            Piece<KB> piece;
+            piece.load(codes + quarter * Piece<KB>::BYTES, codes + D * 2 / 8 + quarter * 4, a.k.scales + at, a.k.zeros ? a.k.zeros + at : nullptr);
+            uint32_t o[16];
+            decode<KB>(piece, o);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x.k[m][i] = u32x4{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
+          }
+        }
+      }
+      const int set = p % (KT / 4), chunk = p / (KT / 4);
+      const int first = w0 + 16 * (set >> 2) + 2 * (set & 3);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int w = first + (i & 1) * 8 + (i >> 1);
+        x.v[m][i] = u32x4{0u, 0u, 0u, 0u};
+        if (w < end) x.v[m][i] = *reinterpret_cast<const u32x4*>(plain_row(a, s, a.v, s.packed_v, b, h, w) + 8 * chunk);
+      }
+    }
+  }
+  static __device__ __forceinline__ void put_plain(char* buf, int tid, const Plain& x) {
+#pragma unroll
+    for (int m = 0; m < P; ++m) {
+      const int p = tid + m * NT;
+      char* k = buf + (p >> 2) * kKeyPitch + (p & 3) * 64;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4*>(k + 16 * i) = x.k[m][i];
+      const int set = p % (KT / 4), chunk = p / (KT / 4);
+      char* v = buf + VALUES + 8 * chunk * VPITCH + 8 * set;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const uint32_t r0 = x.v[m][0][c], r1 = x.v[m][1][c], r2 = x.v[m][2][c], r3 = x.v[m][3][c];
+        *reinterpret_cast<u32x2*>(v + 2 * c * VPITCH) = u32x2{low_halves(r0, r1), low_halves(r2, r3)};
+        *reinterpret_cast<u32x2*>(v + (2 * c + 1) * VPITCH) = u32x2{high_halves(r0, r1), high_halves(r2, r3)};
+      }
+    }
+  }
+
+  // A wavefront's 32 query rows: operand, outputs (lane: row lane % 32; channels 32 x + 8 (i / 4) + 4 (lane / 32) + i % 4), level, sum.
+  struct Rows {
+    half8_t q[8];
+    float16_t o[4];
+    float m, l;
+  };
+
+  // masked: some row does not attend to every token of the tile; limit: the last one that the lane's row attends to, counted from the tile's first.
+  static __device__ __forceinline__ void attend(const char* buf, Rows& r, int lane, bool masked, int limit, float scale) {
+    const int col = lane & 31, half = lane >> 5;
+    const char* keys = buf + col * kKeyPitch + 16 * half;
+    const char* values = buf + VALUES + col * VPITCH + 16 * half;
+    float16_t s[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      s[n] = float16_t{};
+#pragma unroll
+      for (int st = 0; st < 8; ++st)
+        s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8_t*>(keys + 32 * n * kKeyPitch + 32 * st), r.q[st], s[n], 0, 0, 0);
+    }
+    if (masked) {
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (32 * n + 8 * (i / 4) + 4 * half + i % 4 > limit) s[n][i] = -INFINITY;
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
+    top = fmaxf(top, other_half(top)) * scale;
+    const bool raise = top > r.m + kRaise || (r.m == -INFINITY && top > -INFINITY);
+    if (__builtin_amdgcn_ballot_w64(raise)) {
+      const float level = raise ? top : r.m;
+      const float f = raise ? __builtin_amdgcn_exp2f(r.m - level) : 1.f;       // (0 from the empty state)
+      r.l *= f;
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) r.o[x][i] *= f;
+      r.m = level;
+    }
+    const float level = r.m == -INFINITY ? 0.f : r.m;    // (a row that has met no token yet)
+    half8_t p[2 * NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i], scale, -level));
+        r.l += e;
+        p[2 * n + i / 8][2 * (i % 4) + (i / 4) % 2] = (_Float16)e;
+      }
+#pragma unroll
+    for (int st = 0; st < 2 * NB; ++st)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        r.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8_t*>(values + 32 * x * VPITCH + 32 * st), p[st], r.o[x], 0, 0, 0);
+  }
+
+  static __device__ __forceinline__ void load_queries(const ChunkArgs& a, int b, int h, int row, bool live, int half, Rows& r) {
+    const int i = row / a.heads_per_kv;
+    const __half* src = a.q.p + b * a.q.batch + (h * a.heads_per_kv + row - i * a.heads_per_kv) * a.q.head + i * a.q.token;
+#pragma unroll
+    for (int st = 0; st < 8; ++st) {
+      u32x2 x = {0u, 0u}, y = {0u, 0u};
+      if (live) {
+        x = *reinterpret_cast<const u32x2*>(src + 16 * st + 4 * half);
+        y = *reinterpret_cast<const u32x2*>(src + 16 * st + 8 + 4 * half);
+        if (a.q_scale) {
+          const float* f = a.q_scale + h * D + 16 * st + 4 * half;
+          __half* hx = reinterpret_cast<__half*>(&x);
+          __half* hy = reinterpret_cast<__half*>(&y);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            hx[e] = scaled_half(__half2float(hx[e]), f[e]);
+            hy[e] = scaled_half(__half2float(hy[e]), f[8 + e]);
+          }
+        }
+      }
+      r.q[st] = __builtin_bit_cast(half8_t, u32x4{low_halves(x.x, y.x), high_halves(x.x, y.x), low_halves(x.y, y.y), high_halves(x.y, y.y)});
+    }
+  }
+
+  // Channels 32 x .. of a row: the output itself, or the partial result of a split.
+  static __device__ __forceinline__ void store_channels(const ChunkArgs& a, int b, int h, int row, int split, int x, int half, const float16_t& o, float l) {
+    const int c0 = 32 * x + 4 * half;
+    if (a.n_splits > 1) {
+      float* dst = a.ws_o + ((((long long)b * a.n_kv_heads + h) * ((long long)a.t_new * a.heads_per_kv) + row) * a.n_splits + split) * D + c0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(dst + 8 * i) = float4{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
+      return;
+    }
+    const float f = 1.0f / l;
+    const int i = row / a.heads_per_kv;
+    const long long at = b * a.out_batch + (h * a.heads_per_kv + row - i * a.heads_per_kv) * a.out_head + i * a.out_token + c0;
+    if (a.out_is_fp32) {
+      float* dst = static_cast<float*>(a.out) + at;
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4)
+        *reinterpret_cast<float4*>(dst + 8 * i4) = float4{o[4 * i4] * f, o[4 * i4 + 1] * f, o[4 * i4 + 2] * f, o[4 * i4 + 3] * f};
+    } else {
+      __half* dst = static_cast<__half*>(a.out) + at;
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        const half2_t lo = {(_Float16)(o[4 * i4] * f), (_Float16)(o[4 * i4 + 1] * f)}, hi = {(_Float16)(o[4 * i4 + 2] * f), (_Float16)(o[4 * i4 + 3] * f)};
+        *reinterpret_cast<u32x2*>(dst + 8 * i4) = u32x2{as_u32(lo), as_u32(hi)};
+      }
+    }
+  }
+  static __device__ __forceinline__ void store_state(const ChunkArgs& a, int b, int h, int row, int split, float m, float l) {
+    float* ml = a.ws_ml + ((((long long)b * a.n_kv_heads + h) * ((long long)a.t_new * a.heads_per_kv) + row) * a.n_splits + split) * 2;
+    *reinterpret_cast<float2*>(ml) = float2{m, l};
+  }
+};
+
+// Work-groups: (sequence-head, split, block of rows), the rows of one sequence-head next to each other on one XCD (its L2 then brings every
+// tile from memory once), the last rows, which have the most keys, first.
+template <int KB, int VB, int G, int RW, int TW>
+__global__ void __launch_bounds__(64 * RW * TW, 2) attention_chunk_kernel(ChunkArgs a, unsigned items, unsigned per_xcd) {
+  using C = ChunkKernel<KB, VB, G, RW, TW>;
+  __shared__ __align__(16) char lds[C::LDS];
+  const unsigned slot = blockIdx.x / 8u, item = (blockIdx.x % 8u) * per_xcd + slot;
+  if (item >= items) return;
+  const unsigned rb = item % (unsigned)a.row_blocks, rest = item / (unsigned)a.row_blocks;
+  const unsigned split = rest % (unsigned)a.n_splits, bh = rest / (unsigned)a.n_splits;
+  const int b = (int)(bh / (unsigned)a.n_kv_heads), h = (int)(bh % (unsigned)a.n_kv_heads);
+  const ChunkSeq s = chunk_seq(a, b, G);
+  const int rows = s.t * a.heads_per_kv;
+  const int row_base = (a.row_blocks - 1 - (int)rb) * 32 * RW;
+  if (row_base >= rows) return;                          // (uniform)
+  const int wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63, half = lane >> 5;
+  const int group = wave / RW, tid = (int)threadIdx.x % C::NT;
+  const int first = row_base + (wave % RW) * 32, row = first + (lane & 31);
+  const bool live = row < rows;
+  typename C::Rows r;
+  C::load_queries(a, b, h, live ? row : 0, live, half, r);
+#pragma unroll
+  for (int x = 0; x < 4; ++x) r.o[x] = float16_t{};
+  r.m = -INFINITY;
+  r.l = 0.f;
+  const float scale = 0.08838834764831845f * 1.4426950408889634f;
+
+  // numbers of the rest that a row attends to: up to n - packed + its token
+  const int last_row = row_base + 32 * RW < rows ? row_base + 32 * RW : rows;
+  const int end = s.n - s.packed_v + (last_row - 1) / a.heads_per_kv + 1;
+  const int limit = s.n - s.packed_v + (live ? row : rows - 1) / a.heads_per_kv;
+  const int wave_last = first + 32 < rows ? first + 32 : rows;
+  const bool has_rows = first < rows;
+  const int least = s.n - s.packed_v + first / a.heads_per_kv, most = s.n - s.packed_v + (wave_last - 1) / a.heads_per_kv;
+
+  const int packed_tiles = (s.packed_v + C::KT - 1) / C::KT, tiles = packed_tiles + (end + C::KT - 1) / C::KT;
+  // this wavefront's share: of the split, of the work-group
+  const int parts = a.n_splits * TW, part = (int)split * TW + group;
+  const int per = tiles / parts, more = tiles % parts;
+  const int t0 = part * per + (part < more ? part : more), t1 = t0 + per + (part < more ? 1 : 0);
+  const int p1 = t1 < packed_tiles ? t1 : packed_tiles;
+  char* mine = lds + group * C::BUF * C::NBUF;
+  int buf = 0;
+  auto meet = [&] {
+    if constexpr (RW > 1) {
+      __syncthreads();
+    } else {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+  };
+  if (t0 < p1) {
+    typename C::Packed x;
+    C::load_packed(a, s, bh, t0 * C::KT, tid, x);
+    for (int t = t0; t < p1; ++t) {
+      char* at = mine + buf * C::BUF;
+      C::put_packed(at, tid, x);
+      if (t + 1 < p1) C::load_packed(a, s, bh, (t + 1) * C::KT, tid, x);
+      meet();
+      const int left = s.packed_v - t * C::KT;
+      if (has_rows) C::attend(at, r, lane, left < C::KT, left - 1, scale);
+      if constexpr (RW > 1) buf ^= 1;
+      else meet();
+    }
+  }
+  const int w1 = (t1 - packed_tiles) * C::KT;
+  int w = (t0 > packed_tiles ? t0 - packed_tiles : 0) * C::KT;
+  if (w < w1) {
+    typename C::Plain x;
+    C::load_plain(a, s, b, h, w, end, tid, x);
+    for (; w < w1; w += C::KT) {
+      char* at = mine + buf * C::BUF;
+      C::put_plain(at, tid, x);
+      if (w + C::KT < w1) C::load_plain(a, s, b, h, w + C::KT, end, tid, x);
+      meet();
+      if (has_rows && w <= most) C::attend(at, r, lane, w + C::KT - 1 > least, limit - w, scale);
+      if constexpr (RW > 1) buf ^= 1;
+      else meet();
+    }
+  }
+  r.l += other_half(r.l);
+
+  if constexpr (TW == 1) {
+    if (!live) return;
+    if (a.n_splits > 1 && half == 0) C::store_state(a, b, h, row, (int)split, r.m, r.l);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) C::store_channels(a, b, h, row, (int)split, x, half, r.o[x], r.l);
+  } else {
+    // the wavefronts' results meet in LDS, each joins the channels of its own number
+    static_assert(TW == 4 && RW == 1);
+    __syncthreads();
+    float* o = reinterpret_cast<float*>(lds);
+    float* ml = o + TW * 64 * 64;
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[(wave * 64 + x * 16 + i) * 64 + lane] = r.o[x][i];
+    ml[wave * 128 + lane] = r.m;
+    ml[wave * 128 + 64 + lane] = r.l;
+    __syncthreads();
+    float top = ml[lane];
+#pragma unroll
+    for (int n = 1; n < TW; ++n) top = fmaxf(top, ml[n * 128 + lane]);
+    float l = 0.f;
+    float16_t sum = {};
+#pragma unroll
+    for (int n = 0; n < TW; ++n) {
+      const float m = ml[n * 128 + lane];
+      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+      l = __builtin_fmaf(f, ml[n * 128 + 64 + lane], l);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum[i] = __builtin_fmaf(f, o[(n * 64 + wave * 16 + i) * 64 + lane], sum[i]);
+    }
+    if (!live) return;
+    if (a.n_splits > 1 && half == 0 && wave == 0) C::store_state(a, b, h, row, (int)split, top, l);
+    C::store_channels(a, b, h, row, (int)split, wave, half, sum, l);
+  }
+}
+
+template <int KB, int VB, int G, int RW, int TW>
+hipError_t launch_form(const ChunkArgs& a, hipStream_t stream) {
+  const long long items = (long long)a.batch * a.n_kv_heads * a.n_splits * a.row_blocks;
+  if (items >= (1LL << 30)) return hipErrorInvalidValue;
+  const unsigned per = (unsigned)ceil_div(items, 8);
+  attention_chunk_kernel<KB, VB, G, RW, TW><<<per * 8, 64 * RW * TW, 0, stream>>>(a, (unsigned)items, per);
+  return hipGetLastError();
+}
+template <int KB, int VB, int G>
+hipError_t launch_bits(const ChunkArgs& a, const ChunkForm& form, hipStream_t stream) {
+  return form.row_waves == 1 ? launch_form<KB, VB, G, 1, 4>(a, stream) : launch_form<KB, VB, G, 4, 1>(a, stream);
+}
+template <int G>
+hipError_t launch_group(const ChunkArgs& a, int kb, int vb, const ChunkForm& form, hipStream_t stream) {
+  switch (kb * 10 + vb) {
+    case 22: return launch_bits<2, 2, G>(a, form, stream);
+    case 23: return launch_bits<2, 3, G>(a, form, stream);
+    case 24: return launch_bits<2, 4, G>(a, form, stream);
+    case 32: return launch_bits<3, 2, G>(a, form, stream);
+    case 33: return launch_bits<3, 3, G>(a, form, stream);
+    case 34: return launch_bits<3, 4, G>(a, form, stream);
+    case 42: return launch_bits<4, 2, G>(a, form, stream);
+    case 43: return launch_bits<4, 3, G>(a, form, stream);
+    case 44: return launch_bits<4, 4, G>(a, form, stream);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+#if INNERQ_CHUNK_G == 32
+// The splits of a row joined: a wavefront a row, a lane per two channels.
+__global__ void __launch_bounds__(256) chunk_merge_kernel(ChunkArgs a, long long rows_all) {
+  const long long at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = (int)threadIdx.x & 63;
+  if (at >= rows_all) return;
+  const int rows = a.t_new * a.heads_per_kv;
+  const long long bh = at / rows;
+  const int row = (int)(at - bh * rows), b = (int)(bh / a.n_kv_heads), h = (int)(bh - (long long)b * a.n_kv_heads);
+  const int i = row / a.heads_per_kv;
+  if (a.t_dev && i >= a.t_dev[b]) return;
+  const float* ml = a.ws_ml + at * a.n_splits * 2;
+  const float* po = a.ws_o + at * a.n_splits * D + 2 * lane;
+  float top = -INFINITY;
+  for (int p = lane; p < a.n_splits; p += 64) top = fmaxf(top, ml[2 * p]);
+#pragma unroll
+  for (int x = 32; x > 0; x /= 2) top = fmaxf(top, __shfl_xor(top, x));
+  float den = 0.f, n0 = 0.f, n1 = 0.f;
+  for (int p0 = 0; p0 < a.n_splits; p0 += 64) {
+    float f = 0.f, l = 0.f;
+    if (p0 + lane < a.n_splits) {
+      const float2 s = *reinterpret_cast<const float2*>(ml + 2 * (p0 + lane));
+      f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - top);
+      l = s.y;
+    }
+    den += f * l;
+    const int n = a.n_splits - p0 < 64 ? a.n_splits - p0 : 64;
+    for (int p = 0; p < n; ++p) {
+      const float2 o = *reinterpret_cast<const float2*>(po + (long long)(p0 + p) * D);
+      const float w = __shfl(f, p);
+      n0 = __builtin_fmaf(w, o.x, n0);
+      n1 = __builtin_fmaf(w, o.y, n1);
+    }
+  }
+#pragma unroll
+  for (int x = 32; x > 0; x /= 2) den += __shfl_xor(den, x);
+  const float inv = 1.0f / den;
+  const long long dst = b * a.out_batch + (h * a.heads_per_kv + row - i * a.heads_per_kv) * a.out_head + i * a.out_token + 2 * lane;
+  if (a.out_is_fp32) *reinterpret_cast<float2*>(static_cast<float*>(a.out) + dst) = float2{n0 * inv, n1 * inv};
+  else *reinterpret_cast<half2_t*>(static_cast<_Float16*>(a.out) + dst) = half2_t{(_Float16)(n0 * inv), (_Float16)(n1 * inv)};
+}
+#endif
+
+}  // namespace
+
+#if INNERQ_CHUNK_G == 32
+hipError_t launch_chunk_g32(const ChunkArgs& a, int kb, int vb, const ChunkForm& form, hipStream_t stream) { return launch_group<32>(a, kb, vb, form, stream); }
+hipError_t launch_chunk_merge(const ChunkArgs& a, hipStream_t stream) {
+  const long long rows = (long long)a.batch * a.n_kv_heads * a.t_new * a.heads_per_kv;
+  chunk_merge_kernel<<<(unsigned)ceil_div(rows, 4), 256, 0, stream>>>(a, rows);
+  return hipGetLastError();
+}
+#else
+hipError_t launch_chunk_g64(const ChunkArgs& a, int kb, int vb, const ChunkForm& form, hipStream_t stream) { return launch_group<64>(a, kb, vb, form, stream); }
+#endif
+
+}  // namespace innerq

@@ -109,3 +109,43 @@ def test_append_states():
 def test_struct_layout_matches_the_header():
     assert C.sizeof(iq.innerq_strides_t) == 24 and iq.innerq_strides_t.token.offset == 16
     assert C.sizeof(iq.innerq_rotation_t) == 3 * 8 + 3 * 4 + 64 + 4 and iq.innerq_rotation_t.pair_axis.offset == 36
+
+
+def attentions(cfg=None, cache=None, k=P, ks=None, v=P, vs=None, q=P, qs=None, t=3, scale=None, out=P, outs=None, fp32=0, ws=P, ws_bytes=1 << 40,
+               n_dev=P, t_dev=P, most=500):
+    cfg, cache = cfg or config(), cache or cache_of()
+    s = [x or strides(token=1280) for x in (ks, vs, qs, outs)]
+    rows = [k, ref(s[0]), v, ref(s[1]), q, ref(s[2]), t, scale, out, ref(s[3]), fp32, ws, ws_bytes, None]
+    return (L.innerq_chunk_attention(ref(cfg), ref(cache), *rows), L.innerq_chunk_attention_ragged(ref(cfg), ref(cache), n_dev, t_dev, most, *rows))
+
+
+@pytest.mark.parametrize("over,want", [
+    (dict(k=None), iq.E_NULL), (dict(v=None), iq.E_NULL), (dict(q=None), iq.E_NULL), (dict(out=None), iq.E_NULL), (dict(ws=None), iq.E_NULL),
+    (dict(k=P + 8), iq.E_ALIGN), (dict(v=P + 2), iq.E_ALIGN), (dict(q=P + 4), iq.E_ALIGN), (dict(out=P + 8), iq.E_ALIGN), (dict(ws=P + 8), iq.E_ALIGN),
+    (dict(scale=P + 4), iq.E_ALIGN), (dict(qs=strides(head=132)), iq.E_ALIGN), (dict(ks=strides(token=-8)), iq.E_ARG), (dict(outs=strides(token=0)), iq.E_ARG),
+    (dict(outs=strides(head=132), fp32=0), iq.E_ALIGN), (dict(t=-1), iq.E_ARG), (dict(t=0), iq.OK), (dict(t=1025), iq.E_CAPACITY), (dict(ws_bytes=63), iq.E_WORKSPACE),
+    (dict(cfg=config(kind=iq.KIND_OUTER)), iq.E_UNSUPPORTED), (dict(cfg=config(kind=iq.KIND_FP16)), iq.E_UNSUPPORTED),
+    (dict(cfg=config(capacity_tokens=(1 << 24) + 32)), iq.E_UNSUPPORTED), (dict(cfg=config(n_q_heads=1 << 24, capacity_tokens=1 << 20), t=1 << 10), iq.E_UNSUPPORTED)])
+def test_chunk_attention(over, want):
+    assert attentions(**over) == (want, want)
+
+
+def test_chunk_attention_states():
+    assert L.innerq_chunk_attention(ref(config()), None, *([P, None] * 3), 3, None, P, None, 0, P, 1 << 40, None) == iq.E_NULL
+    assert attentions(cache=cache_of(1022))[0] == iq.E_CAPACITY
+    for over, want in ((dict(n_dev=None), iq.E_NULL), (dict(t_dev=None), iq.E_NULL), (dict(n_dev=P + 2), iq.E_ALIGN), (dict(most=0), iq.E_ARG), (dict(most=1025), iq.E_CAPACITY)):
+        assert attentions(**over)[1] == want
+    # too little workspace, by a byte, where the keys may be split
+    need = iq.innerq_chunk_workspace_bytes(config(), 3)
+    assert need > 64 and attentions(ws_bytes=need - 1) == (iq.E_WORKSPACE, iq.E_WORKSPACE)
+
+
+def test_chunk_workspace():
+    for bad in (config(bits=5), config(kind=iq.KIND_FP16)):
+        assert iq.innerq_chunk_workspace_bytes(bad, 4) == 0
+    assert iq.innerq_chunk_workspace_bytes(config(), 0) == 0 and iq.innerq_chunk_workspace_bytes(config(), -1) == 0
+    assert iq.innerq_chunk_workspace_bytes(config(), 1 << 25) == 0
+    # never more than two rounds of work-groups of 128 rows, whatever the sizes
+    for batch, hk, r, cap, t in ((1, 1, 1, 1 << 20, 1), (1, 8, 4, 1 << 17, 2048), (64, 8, 8, 32768, 5), (4, 32, 1, 65536, 33)):
+        c = iq.make_config(batch, hk * r, hk, 128, 2, 32, 4, 128, capacity_tokens=cap)
+        assert 64 <= iq.innerq_chunk_workspace_bytes(c, t) <= 1024 * 128 * 130 * 4 + 64
