@@ -709,7 +709,7 @@ bool chunk_rows_fit(const innerq_config_t& c, long long t_new) { return t_new <=
 
 ChunkTensor chunk_tensor(const innerq_config_t& c, const innerq_cache_t& k, int which, const void* fresh, const innerq_strides_t& s) {
   const TensorView v = view_of(c, k, which, 0);
-  return {v.codes, v.scales, v.zeros, v.sink, v.ring, rows_of(fresh, s), v.slots};
+  return {v.codes, v.scales, v.zeros ? v.zeros : v.scales, v.sink, v.ring, rows_of(fresh, s), v.slots};
 }
 
 // tokens: the most that a query attends to, cached and new ones.

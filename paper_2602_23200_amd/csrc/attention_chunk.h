@@ -9,7 +9,7 @@ namespace innerq {
 struct ChunkTensor {
   const uint8_t* codes;
   const __half* scales;
-  const __half* zeros;                 // null: symmetric
+  const __half* zeros;                 // of a symmetric tensor, which has none: its scales (read, never used)
   const __half* sink;
   const __half* ring;
   RowView fresh;                       // new rows

@@ -52,11 +52,6 @@ struct Piece {
   static constexpr int BYTES = 32 * (BITS == 3 ? 2 : BITS) / 8;       // of the (low) plane
   uint32_t w[BITS];
   uint32_t scale, zero;
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int i = 0; i < BITS; ++i) w[i] = 0u;
-    scale = zero = 0u;
-  }
   // low: the fields (3-bit: their low two bits), high: the plane of high bits
   __device__ __forceinline__ void load(const uint8_t* low, const uint8_t* high, const __half* s, const __half* z) {
     if constexpr (BITS == 4) {
@@ -68,7 +63,7 @@ struct Piece {
       if constexpr (BITS == 3) w[2] = *reinterpret_cast<const uint32_t*>(high);
     }
     scale = *reinterpret_cast<const unsigned short*>(s);
-    zero = z ? *reinterpret_cast<const unsigned short*>(z) : 0u;
+    zero = *reinterpret_cast<const unsigned short*>(z);
   }
 };
 
@@ -136,11 +131,14 @@ __device__ __forceinline__ void put_words(char* dst, const uint32_t (&w)[16]) {
   for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4*>(dst + 16 * i) = u32x4{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
 }
 
+// Matrix instructions and LDS reads stay in the order in which they are written; arithmetic, global loads and LDS writes may move.
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0x616); }
+
 // ---- a sequence
 
-// Cached and new tokens; sink tokens; packed rows of keys and of values.  Keys of a row: the packed_v rows of the store, then the rest in
-// order of their tokens (number w of them is token w of the sink, else token w + packed_v).
-struct ChunkSeq { int n, t, sink, packed_k, packed_v; };
+// Cached and new tokens; sink tokens; packed rows of keys and of values; cached tokens beside the packed_v rows of the store (number w of
+// them is token w of the sink, else token w + packed_v).
+struct ChunkSeq { int n, t, sink, packed_k, packed_v, beside; };
 __device__ __forceinline__ ChunkSeq chunk_seq(const ChunkArgs& a, int b, int group) {
   const int cap = (int)a.capacity;
   ChunkSeq s;
@@ -155,124 +153,192 @@ __device__ __forceinline__ ChunkSeq chunk_seq(const ChunkArgs& a, int b, int gro
   s.sink = s.n < a.w_sink ? s.n : a.w_sink;
   s.packed_k = (int)quantised_rows(a.w_sink, a.w_recent, group, kPerToken, s.n);
   s.packed_v = (int)quantised_rows(a.w_sink, a.w_recent, group, kPerChannel, s.n);
+  s.beside = s.n - s.packed_v;
   return s;
 }
+
+// Where a thread finds its piece of a tile of packed rows: offsets from the tile's first row (a row takes 16 BITS bytes of codes
+// and 128 / G scales in either tensor), for a whole tile and for one of 32 rows.
+template <int BITS, int G>
+struct PieceAt {
+  uint32_t low, high, scale;
+  // quarter of a key row
+  __device__ __forceinline__ void key(int token, int quarter) {
+    low = (uint32_t)(token * 16 * BITS + quarter * Piece<BITS>::BYTES);
+    high = (uint32_t)(token * 16 * BITS + D * 2 / 8 + quarter * 4);
+    scale = (uint32_t)(token * (D / G) + quarter * 32 / G);
+  }
+  // 32 tokens of a value channel
+  __device__ __forceinline__ void value(int channel, int block) {
+    const int group = G == 64 ? 0 : block, part = G == 64 ? block : 0;
+    const uint32_t run = (uint32_t)((group * D + channel) * (G * BITS / 8));
+    low = run + (uint32_t)(part * Piece<BITS>::BYTES);
+    high = run + (uint32_t)(G * 2 / 8 + part * 4);
+    scale = (uint32_t)(group * D + channel);
+  }
+};
 
 template <int KB, int VB, int G, int RW, int TW>
 struct ChunkKernel {
   static constexpr int KT = RW == 1 ? 32 : 64;           // tokens of a tile
   static constexpr int NB = KT / 32;                     // blocks of 32 of them
   static constexpr int NT = 64 * RW;                     // threads that bring a tile
-  static constexpr int P = KT * 4 / NT;                  // pieces of each tensor a thread brings
+  static constexpr bool APART = RW == 8;                 // half of the wavefronts bring keys, half values
+  static constexpr int P = APART ? 1 : KT * 4 / NT;      // pieces of each tensor a thread brings
   static constexpr int VPITCH = 2 * KT + 16;             // bytes of a channel of V^T
   static constexpr int VALUES = KT * kKeyPitch;          // where they begin
   static constexpr int BUF = VALUES + D * VPITCH;
-  static constexpr int NBUF = RW == 1 ? 1 : 2;           // (a wavefront by itself takes its LDS operations in order)
+  static constexpr int NBUF = RW == 1 ? 1 : RW == 4 ? 2 : 4;          // buffers (a wavefront by itself takes its LDS operations in order)
   static constexpr int JOIN = TW > 1 ? TW * (64 * 64 + 128) * 4 : 0;
   static constexpr int LDS = BUF * NBUF * TW > JOIN ? BUF * NBUF * TW : JOIN;
 
-  struct Packed { Piece<KB> k[P]; Piece<VB> v[P]; };
+  static constexpr bool ONE = APART && KB == VB;         // a thread's piece is a key's or a value's, decoded alike
+  struct Packed { Piece<KB> k[P]; Piece<VB> v[ONE ? 1 : P]; };
   struct Plain { u32x4 k[P][4]; u32x4 v[P][4]; };
 
-  // Tile of store rows row0 .. : pieces in registers.  (row0 is a multiple of the tile, so one page holds it.)
-  static __device__ __forceinline__ void load_packed(const ChunkArgs& a, const ChunkSeq& s, long long bh, int row0, int tid, Packed& x) {
+  // Store rows row0 .. (a multiple of the tile, so one page holds them): pieces in registers.  Behind the last packed row: the
+  // same rows again, whose scores are masked.
+  static __device__ __forceinline__ void load_packed(const ChunkArgs& a, const ChunkSeq& s, long long bh, int row0, int tid, bool values, Packed& x) {
     const long long lin = store_row(a.pages, a.n_kv_heads, a.capacity, bh, row0);
+    const bool whole = KT == 32 || s.packed_v - row0 >= KT;
+    if constexpr (ONE) {
+      const int p = tid % (NT / 2);
+      PieceAt<KB, G> k, v;
+      k.key(whole ? p >> 2 : (p >> 2) & 31, p & 3);
+      v.value(p % D, whole ? p / D : 0);
+      const ChunkTensor& t = values ? a.v : a.k;
+      const uint8_t* codes = t.codes + lin * (16 * KB);
+      const uint32_t scale = values ? v.scale : k.scale;
+      x.k[0].load(codes + (values ? v.low : k.low), codes + (values ? v.high : k.high), t.scales + lin * (D / G) + scale, t.zeros + lin * (D / G) + scale);
+      return;
+    }
 #pragma unroll
     for (int m = 0; m < P; ++m) {
-      const int p = tid + m * NT;
-      const int tok = p >> 2, quarter = p & 3;
-      if (row0 + tok < s.packed_v) {
-        const uint8_t* row = a.k.codes + (lin + tok) * (D * KB / 8);
-        const long long at = (lin + tok) * (D / G) + quarter * 32 / G;
-        x.k[m].load(row + quarter * Piece<KB>::BYTES, row + D * 2 / 8 + quarter * 4, a.k.scales + at, a.k.zeros ? a.k.zeros + at : nullptr);
-      } else {
-        x.k[m].clear();
+      const int p = (APART ? tid % (NT / 2) : tid) + m * NT;
+      if (!APART || !values) {
+        PieceAt<KB, G> at;
+        at.key(whole ? p >> 2 : (p >> 2) & 31, p & 3);
+        const uint8_t* codes = a.k.codes + lin * (16 * KB);
+        x.k[m].load(codes + at.low, codes + at.high, a.k.scales + lin * (D / G) + at.scale, a.k.zeros + lin * (D / G) + at.scale);
       }
-      const int c = p % D, sub = p / D;                  // channel, block of 32 tokens
-      const int row = row0 + 32 * sub;
-      if (row < s.packed_v) {
-        const long long at = (lin + 32 * sub) / G * D + c;
-        const uint8_t* run = a.v.codes + at * (G * VB / 8);
-        const int part = G == 64 ? (row & 63) / 32 : 0;
-        x.v[m].load(run + part * Piece<VB>::BYTES, run + G * 2 / 8 + part * 4, a.v.scales + at, a.v.zeros ? a.v.zeros + at : nullptr);
-      } else {
-        x.v[m].clear();
+      if (!APART || values) {
+        // (tiles of 32 tokens may begin in the middle of a group of 64)
+        const int block = KT == 32 ? (G == 64 ? (row0 & 63) / 32 : 0) : whole ? p / D : 0;
+        const long long first = KT == 32 && G == 64 ? lin - (row0 & 63) : lin;
+        PieceAt<VB, G> at;
+        at.value(p % D, block);
+        const uint8_t* codes = a.v.codes + first * (16 * VB);
+        x.v[m].load(codes + at.low, codes + at.high, a.v.scales + first * (D / G) + at.scale, a.v.zeros + first * (D / G) + at.scale);
       }
     }
   }
-  static __device__ __forceinline__ void put_packed(char* buf, int tid, const Packed& x) {
+  static __device__ __forceinline__ void put_packed(char* buf, int tid, bool values, const Packed& x) {
 #pragma unroll
     for (int m = 0; m < P; ++m) {
-      const int p = tid + m * NT;
+      const int p = (APART ? tid % (NT / 2) : tid) + m * NT;
       uint32_t w[16];
-      decode<KB>(x.k[m], w);
-      put_words(buf + (p >> 2) * kKeyPitch + (p & 3) * 64, w);
-      decode<VB>(x.v[m], w);
-      put_words(buf + VALUES + (p % D) * VPITCH + (p / D) * 64, w);
+      char* k = buf + (p >> 2) * kKeyPitch + (p & 3) * 64;
+      char* v = buf + VALUES + (p % D) * VPITCH + (p / D) * 64;
+      if constexpr (!APART) {
+        decode<KB>(x.k[m], w);
+        put_words(k, w);
+        decode<VB>(x.v[m], w);
+        put_words(v, w);
+      } else if constexpr (KB == VB) {
+        decode<KB>(x.k[0], w);
+        put_words(values ? v : k, w);
+      } else if (values) {
+        decode<VB>(x.v[m], w);
+        put_words(v, w);
+      } else {
+        decode<KB>(x.k[m], w);
+        put_words(k, w);
+      }
     }
   }
 
-  // fp16 row of the token of number w (which must exist); null for a key that is packed.
-  static __device__ __forceinline__ const __half* plain_row(const ChunkArgs& a, const ChunkSeq& s, const ChunkTensor& x, int packed, int b, int h, int w) {
-    const long long bh = (long long)b * a.n_kv_heads + h;
+  // Number w of the cached tokens beside the packed rows: its fp16 row; null for a key that is packed.
+  static __device__ __forceinline__ const __half* cached_row(const ChunkArgs& a, const ChunkSeq& s, const ChunkTensor& x, int packed, long long bh, int w) {
     if (w < s.sink) return x.sink + (bh * a.w_sink + w) * D;
     const int token = w + s.packed_v;
-    if (token >= s.n) return x.fresh.p + b * x.fresh.batch + h * x.fresh.head + (token - s.n) * x.fresh.token;
     if (token - a.w_sink < packed) return nullptr;
     return x.ring + (bh * x.slots + (uint32_t)token % (uint32_t)x.slots) * D;
   }
-  // Numbers w0 .. of the rest; end: behind the last one.
-  static __device__ __forceinline__ void load_plain(const ChunkArgs& a, const ChunkSeq& s, int b, int h, int w0, int end, int tid, Plain& x) {
+  // Tile of numbers w0 .. (behind the last one: the last one again, whose scores are masked).
+  static __device__ __forceinline__ void load_cached(const ChunkArgs& a, const ChunkSeq& s, long long bh, int w0, int tid, bool values, Plain& x) {
 #pragma unroll
     for (int m = 0; m < P; ++m) {
-      const int p = tid + m * NT;
-      {
-        const int w = w0 + (p >> 2), quarter = p & 3;
+      const int p = (APART ? tid % (NT / 2) : tid) + m * NT;
+      if (!APART || !values) {
+        const int w = w0 + (p >> 2) < s.beside ? w0 + (p >> 2) : s.beside - 1, quarter = p & 3;
+        const __half* row = cached_row(a, s, a.k, s.packed_k, bh, w);
+        if (row) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x.k[m][i] = u32x4{0u, 0u, 0u, 0u};
-        if (w < end) {
-          const __half* row = plain_row(a, s, a.k, s.packed_k, b, h, w);
-          if (row) {
-            const __half* src = row + quarter * 32;
+          for (int i = 0; i < 4; ++i) x.k[m][i] = *reinterpret_cast<const u32x4*>(row + quarter * 32 + 8 * i);
+        } else {
+          // (a key that has left its window before the values of its group have left theirs)
+          const long long lin = store_row(a.pages, a.n_kv_heads, a.capacity, bh, w + s.packed_v - a.w_sink);
+          const uint8_t* codes = a.k.codes + lin * (D * KB / 8);
+          const long long at = lin * (D / G) + quarter * 32 / G;
+          Piece<KB> piece;
+          piece.load(codes + quarter * Piece<KB>::BYTES, codes + D * 2 / 8 + quarter * 4, a.k.scales + at, a.k.zeros + at);
+          uint32_t o[16];
+          decode<KB>(piece, o);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x.k[m][i] = *reinterpret_cast<const u32x4*>(src + 8 * i);
-#pragma unroll
-            for (int i = 0; i < 4; i += 2) {
-              const u32x4 f = x.k[m][i], g = x.k[m][i + 1];
-              x.k[m][i] = u32x4{low_halves(f.x, g.x), high_halves(f.x, g.x), low_halves(f.y, g.y), high_halves(f.y, g.y)};
-              x.k[m][i + 1] = u32x4{low_halves(f.z, g.z), high_halves(f.z, g.z), low_halves(f.w, g.w), high_halves(f.w, g.w)};
-            }
-          } else {
-            // (a key that has left its window before the values of its group have left theirs)
-            const long long lin = store_row(a.pages, a.n_kv_heads, a.capacity, (long long)b * a.n_kv_heads + h, w + s.packed_v - a.w_sink);
-            const uint8_t* codes = a.k.codes + lin * (D * KB / 8);
-            const long long at = lin * (D / G) + quarter * 32 / G;
-            Piece<KB> piece;
-            piece.load(codes + quarter * Piece<KB>::BYTES, codes + D * 2 / 8 + quarter * 4, a.k.scales + at, a.k.zeros ? a.k.zeros + at : nullptr);
-            uint32_t o[16];
-            decode<KB>(piece, o);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x.k[m][i] = u32x4{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
+          for (int i = 0; i < 2; ++i) {                    // (back into the order of the channels, as the other rows are)
+            const uint32_t* q = o + 8 * i;
+            x.k[m][2 * i] = u32x4{low_halves(q[0], q[1]), low_halves(q[2], q[3]), low_halves(q[4], q[5]), low_halves(q[6], q[7])};
+            x.k[m][2 * i + 1] = u32x4{high_halves(q[0], q[1]), high_halves(q[2], q[3]), high_halves(q[4], q[5]), high_halves(q[6], q[7])};
           }
         }
       }
+      if (APART && !values) continue;
       const int set = p % (KT / 4), chunk = p / (KT / 4);
       const int first = w0 + 16 * (set >> 2) + 2 * (set & 3);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int w = first + (i & 1) * 8 + (i >> 1);
-        x.v[m][i] = u32x4{0u, 0u, 0u, 0u};
-        if (w < end) x.v[m][i] = *reinterpret_cast<const u32x4*>(plain_row(a, s, a.v, s.packed_v, b, h, w) + 8 * chunk);
+        x.v[m][i] = *reinterpret_cast<const u32x4*>(cached_row(a, s, a.v, s.packed_v, bh, w < s.beside ? w : s.beside - 1) + 8 * chunk);
       }
     }
   }
-  static __device__ __forceinline__ void put_plain(char* buf, int tid, const Plain& x) {
+  // Tile of new tokens i0 .. (behind the last one, `last`: that one again, whose scores are masked).
+  static __device__ __forceinline__ void load_fresh(const ChunkArgs& a, int b, int h, int i0, int last, int tid, bool values, Plain& x) {
+    const RowView &k = a.k.fresh, &v = a.v.fresh;
 #pragma unroll
     for (int m = 0; m < P; ++m) {
-      const int p = tid + m * NT;
-      char* k = buf + (p >> 2) * kKeyPitch + (p & 3) * 64;
+      const int p = (APART ? tid % (NT / 2) : tid) + m * NT;
+      if (!APART || !values) {
+        const int i = i0 + (p >> 2) < last ? i0 + (p >> 2) : last;
+        const __half* src = k.p + b * k.batch + h * k.head + i * k.token + (p & 3) * 32;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4*>(k + 16 * i) = x.k[m][i];
+        for (int e = 0; e < 4; ++e) x.k[m][e] = *reinterpret_cast<const u32x4*>(src + 8 * e);
+      }
+      if (APART && !values) continue;
+      const int set = p % (KT / 4), chunk = p / (KT / 4);
+      const int first = i0 + 16 * (set >> 2) + 2 * (set & 3);
+      const __half* src = v.p + b * v.batch + h * v.head + 8 * chunk;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = first + (e & 1) * 8 + (e >> 1);
+        x.v[m][e] = *reinterpret_cast<const u32x4*>(src + (i < last ? i : last) * v.token);
+      }
+    }
+  }
+  static __device__ __forceinline__ void put_plain(char* buf, int tid, bool values, const Plain& x) {
+#pragma unroll
+    for (int m = 0; m < P; ++m) {
+      const int p = (APART ? tid % (NT / 2) : tid) + m * NT;
+      if (!APART || !values) {
+        char* k = buf + (p >> 2) * kKeyPitch + (p & 3) * 64;
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+          const u32x4 f = x.k[m][i], g = x.k[m][i + 1];
+          *reinterpret_cast<u32x4*>(k + 16 * i) = u32x4{low_halves(f.x, g.x), high_halves(f.x, g.x), low_halves(f.y, g.y), high_halves(f.y, g.y)};
+          *reinterpret_cast<u32x4*>(k + 16 * i + 16) = u32x4{low_halves(f.z, g.z), high_halves(f.z, g.z), low_halves(f.w, g.w), high_halves(f.w, g.w)};
+        }
+      }
+      if (APART && !values) continue;
       const int set = p % (KT / 4), chunk = p / (KT / 4);
       char* v = buf + VALUES + 8 * chunk * VPITCH + 8 * set;
 #pragma unroll
@@ -291,19 +357,31 @@ struct ChunkKernel {
     float m, l;
   };
 
-  // masked: some row does not attend to every token of the tile; limit: the last one that the lane's row attends to, counted from the tile's first.
-  static __device__ __forceinline__ void attend(const char* buf, Rows& r, int lane, bool masked, int limit, float scale) {
-    const int col = lane & 31, half = lane >> 5;
-    const char* keys = buf + col * kKeyPitch + 16 * half;
-    const char* values = buf + VALUES + col * VPITCH + 16 * half;
-    float16_t s[NB];
+  static __device__ __forceinline__ void scores(const char* buf, const Rows& r, int lane, float16_t (&s)[NB]) {
+    const char* keys = buf + (lane & 31) * kKeyPitch + 16 * (lane >> 5);
+    // operands eight ahead of their instructions; what decodes the next tile may stand between these
+    half8_t k[8];
+#pragma unroll
+    for (int st = 0; st < 8; ++st) k[st] = *reinterpret_cast<const half8_t*>(keys + 32 * st);
+    keep_order();
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       s[n] = float16_t{};
 #pragma unroll
-      for (int st = 0; st < 8; ++st)
-        s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8_t*>(keys + 32 * n * kKeyPitch + 32 * st), r.q[st], s[n], 0, 0, 0);
+      for (int st = 0; st < 8; ++st) {
+        s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[st], r.q[st], s[n], 0, 0, 0);
+        if (n + 1 < NB) k[st] = *reinterpret_cast<const half8_t*>(keys + 32 * (n + 1) * kKeyPitch + 32 * st);
+        keep_order();
+      }
     }
+  }
+  // masked: some row does not attend to every token of the tile; limit: the last one that the lane's row attends to, counted from the tile's first.
+  static __device__ __forceinline__ void finish(const char* buf, Rows& r, float16_t (&s)[NB], int lane, bool masked, int limit, float scale) {
+    const int half = lane >> 5;
+    const char* values = buf + VALUES + (lane & 31) * VPITCH + 16 * half;
+    half8_t v[8];                                        // (the first values are on their way under the softmax)
+#pragma unroll
+    for (int x = 0; x < 8; ++x) v[x] = *reinterpret_cast<const half8_t*>(values + 32 * (x & 3) * VPITCH + 32 * (x >> 2));
     if (masked) {
 #pragma unroll
       for (int n = 0; n < NB; ++n)
@@ -317,7 +395,7 @@ struct ChunkKernel {
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
     top = fmaxf(top, other_half(top)) * scale;
-    const bool raise = top > r.m + kRaise || (r.m == -INFINITY && top > -INFINITY);
+    const bool raise = top > r.m + kRaise;               // (from the empty state: if there is a token at all)
     if (__builtin_amdgcn_ballot_w64(raise)) {
       const float level = raise ? top : r.m;
       const float f = raise ? __builtin_amdgcn_exp2f(r.m - level) : 1.f;       // (0 from the empty state)
@@ -333,16 +411,23 @@ struct ChunkKernel {
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i], scale, -level));
-        r.l += e;
-        p[2 * n + i / 8][2 * (i % 4) + (i / 4) % 2] = (_Float16)e;
-      }
+      for (int i = 0; i < 16; ++i)
+        p[2 * n + i / 8][2 * (i % 4) + (i / 4) % 2] = (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i], scale, -level));
+    // (the sum is that of the weights as they are rounded)
 #pragma unroll
     for (int st = 0; st < 2 * NB; ++st)
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
-        r.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8_t*>(values + 32 * x * VPITCH + 32 * st), p[st], r.o[x], 0, 0, 0);
+      for (int e = 0; e < 8; e += 2)
+        r.l = __builtin_amdgcn_fdot2(half2_t{p[st][e], p[st][e + 1]}, half2_t{(_Float16)1.0f, (_Float16)1.0f}, r.l, false);
+#pragma unroll
+    for (int st = 0; st < 2 * NB; ++st)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int at = 4 * st + x;
+        r.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[at & 7], p[st], r.o[x], 0, 0, 0);
+        if (at + 8 < 8 * NB) v[at & 7] = *reinterpret_cast<const half8_t*>(values + 32 * x * VPITCH + 32 * (st + 2));
+        keep_order();
+      }
   }
 
   static __device__ __forceinline__ void load_queries(const ChunkArgs& a, int b, int h, int row, bool live, int half, Rows& r) {
@@ -401,20 +486,73 @@ struct ChunkKernel {
   }
 };
 
-// Work-groups: (sequence-head, split, block of rows), the rows of one sequence-head next to each other on one XCD (its L2 then brings every
-// tile from memory once), the last rows, which have the most keys, first.
+// Tiles u0 .. u1 of one kind: load(u, registers), put(buffer, registers), masks(u) -> {masked, limit} as for finish.  This wavefront's rows
+// attend to those before `mine`.  The next tile is put into LDS, and the one after it loaded, between the two products (behind the last tile:
+// the same again).
+struct TileMask { bool masked; int limit; };
+template <typename C, typename Regs, typename Load, typename Put, typename Mask>
+__device__ __forceinline__ void pass_tiles(int u0, int u1, int mine, char* lds, typename C::Rows& r, int lane, float scale, Load load, Put put, Mask mask) {
+  if (u0 >= u1) return;
+  Regs x;
+  float16_t sc[C::NB];
+  if constexpr (C::NBUF == 1) {
+    load(u0, x);
+    for (int u = u0; u < u1; ++u) {
+      put(lds, x);
+      if (u + 1 < u1) load(u + 1, x);
+      asm volatile("" ::: "memory");                     // (a wavefront's LDS operations are performed in order)
+      __builtin_amdgcn_wave_barrier();
+      if (u < mine) {
+        C::scores(lds, r, lane, sc);
+        const TileMask m = mask(u);
+        C::finish(lds, r, sc, lane, m.masked, m.limit, scale);
+      }
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_wave_barrier();
+    }
+  } else {
+    constexpr int STEP = C::NBUF / 2;                      // tiles that the work-group takes between two barriers
+    auto at = [&](int u) { return lds + ((u - u0) % C::NBUF) * C::BUF; };
+    auto bound = [&](int u) { return u < u1 ? u : u1 - 1; };
+    load(u0, x);
+#pragma unroll
+    for (int i = 0; i < STEP; ++i) {
+      put(at(u0 + i), x);
+      load(bound(u0 + i + 1), x);
+    }
+    int u = u0;
+    for (; u < mine && u < u1; ++u) {
+      if (STEP == 1 || (u - u0) % STEP == 0) __syncthreads();
+      C::scores(at(u), r, lane, sc);
+      put(at(u + STEP), x);
+      load(bound(u + STEP + 1), x);
+      const TileMask m = mask(u);
+      C::finish(at(u), r, sc, lane, m.masked, m.limit, scale);
+    }
+    for (; u < u1; ++u) {
+      if (STEP == 1 || (u - u0) % STEP == 0) __syncthreads();
+      put(at(u + STEP), x);
+      load(bound(u + STEP + 1), x);
+    }
+    __syncthreads();
+  }
+}
+
+// Work-groups: the last rows, which have the most keys, first; where the sequence-heads can be shared out evenly, those of one stay on one XCD (its L2
+// then brings every tile from memory once).
 template <int KB, int VB, int G, int RW, int TW>
-__global__ void __launch_bounds__(64 * RW * TW, 2) attention_chunk_kernel(ChunkArgs a, unsigned items, unsigned per_xcd) {
+__global__ void __launch_bounds__(64 * RW * TW) __attribute__((amdgpu_waves_per_eu(2, 2))) attention_chunk_kernel(ChunkArgs a) {
   using C = ChunkKernel<KB, VB, G, RW, TW>;
   __shared__ __align__(16) char lds[C::LDS];
-  const unsigned slot = blockIdx.x / 8u, item = (blockIdx.x % 8u) * per_xcd + slot;
-  if (item >= items) return;
-  const unsigned rb = item % (unsigned)a.row_blocks, rest = item / (unsigned)a.row_blocks;
-  const unsigned split = rest % (unsigned)a.n_splits, bh = rest / (unsigned)a.n_splits;
+  const unsigned heads = (unsigned)(a.batch * a.n_kv_heads);
+  const bool pinned = heads % 8u == 0u;
+  const unsigned slot = pinned ? blockIdx.x / 8u : blockIdx.x, mine_heads = pinned ? heads / 8u : heads;
+  const unsigned rank = slot / (mine_heads * (unsigned)a.n_splits), rest = slot % (mine_heads * (unsigned)a.n_splits);
+  const unsigned split = rest % (unsigned)a.n_splits, bh = rest / (unsigned)a.n_splits + (pinned ? blockIdx.x % 8u * mine_heads : 0u);
   const int b = (int)(bh / (unsigned)a.n_kv_heads), h = (int)(bh % (unsigned)a.n_kv_heads);
   const ChunkSeq s = chunk_seq(a, b, G);
   const int rows = s.t * a.heads_per_kv;
-  const int row_base = (a.row_blocks - 1 - (int)rb) * 32 * RW;
+  const int row_base = (a.row_blocks - 1 - (int)rank) * 32 * RW;
   if (row_base >= rows) return;                          // (uniform)
   const int wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63, half = lane >> 5;
   const int group = wave / RW, tid = (int)threadIdx.x % C::NT;
@@ -428,59 +566,33 @@ __global__ void __launch_bounds__(64 * RW * TW, 2) attention_chunk_kernel(ChunkA
   r.l = 0.f;
   const float scale = 0.08838834764831845f * 1.4426950408889634f;
 
-  // numbers of the rest that a row attends to: up to n - packed + its token
+  // new tokens that the rows of the work-group, of the wavefront and of the lane attend to
   const int last_row = row_base + 32 * RW < rows ? row_base + 32 * RW : rows;
-  const int end = s.n - s.packed_v + (last_row - 1) / a.heads_per_kv + 1;
-  const int limit = s.n - s.packed_v + (live ? row : rows - 1) / a.heads_per_kv;
+  const int last = (last_row - 1) / a.heads_per_kv;
   const int wave_last = first + 32 < rows ? first + 32 : rows;
+  const int newest = (live ? row : rows - 1) / a.heads_per_kv, oldest = first / a.heads_per_kv;
   const bool has_rows = first < rows;
-  const int least = s.n - s.packed_v + first / a.heads_per_kv, most = s.n - s.packed_v + (wave_last - 1) / a.heads_per_kv;
 
-  const int packed_tiles = (s.packed_v + C::KT - 1) / C::KT, tiles = packed_tiles + (end + C::KT - 1) / C::KT;
-  // this wavefront's share: of the split, of the work-group
+  // tiles: packed rows, cached tokens beside them, new tokens; this wavefront's share of them
+  const int tiles1 = (s.packed_v + C::KT - 1) / C::KT, tiles2 = tiles1 + (s.beside + C::KT - 1) / C::KT, tiles = tiles2 + last / C::KT + 1;
   const int parts = a.n_splits * TW, part = (int)split * TW + group;
   const int per = tiles / parts, more = tiles % parts;
   const int t0 = part * per + (part < more ? part : more), t1 = t0 + per + (part < more ? 1 : 0);
-  const int p1 = t1 < packed_tiles ? t1 : packed_tiles;
+  auto from = [&](int t) { return t0 > t ? t0 - t : 0; };
+  auto to = [&](int t, int end) { return (t1 < end ? t1 : end) - t; };
+  const bool values = __builtin_amdgcn_readfirstlane(wave) >= RW / 2;
   char* mine = lds + group * C::BUF * C::NBUF;
-  int buf = 0;
-  auto meet = [&] {
-    if constexpr (RW > 1) {
-      __syncthreads();
-    } else {
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-    }
-  };
-  if (t0 < p1) {
-    typename C::Packed x;
-    C::load_packed(a, s, bh, t0 * C::KT, tid, x);
-    for (int t = t0; t < p1; ++t) {
-      char* at = mine + buf * C::BUF;
-      C::put_packed(at, tid, x);
-      if (t + 1 < p1) C::load_packed(a, s, bh, (t + 1) * C::KT, tid, x);
-      meet();
-      const int left = s.packed_v - t * C::KT;
-      if (has_rows) C::attend(at, r, lane, left < C::KT, left - 1, scale);
-      if constexpr (RW > 1) buf ^= 1;
-      else meet();
-    }
-  }
-  const int w1 = (t1 - packed_tiles) * C::KT;
-  int w = (t0 > packed_tiles ? t0 - packed_tiles : 0) * C::KT;
-  if (w < w1) {
-    typename C::Plain x;
-    C::load_plain(a, s, b, h, w, end, tid, x);
-    for (; w < w1; w += C::KT) {
-      char* at = mine + buf * C::BUF;
-      C::put_plain(at, tid, x);
-      if (w + C::KT < w1) C::load_plain(a, s, b, h, w + C::KT, end, tid, x);
-      meet();
-      if (has_rows && w <= most) C::attend(at, r, lane, w + C::KT - 1 > least, limit - w, scale);
-      if constexpr (RW > 1) buf ^= 1;
-      else meet();
-    }
-  }
+  auto put_packed = [&](char* at, const typename C::Packed& x) { C::put_packed(at, tid, values, x); };
+  auto put_plain = [&](char* at, const typename C::Plain& x) { C::put_plain(at, tid, values, x); };
+  pass_tiles<C, typename C::Packed>(from(0), to(0, tiles1), has_rows ? tiles1 : 0, mine, r, lane, scale,
+      [&](int u, typename C::Packed& x) { C::load_packed(a, s, bh, u * C::KT, tid, values, x); }, put_packed,
+      [&](int u) { return TileMask{s.packed_v - u * C::KT < C::KT, s.packed_v - u * C::KT - 1}; });
+  pass_tiles<C, typename C::Plain>(from(tiles1), to(tiles1, tiles2), has_rows ? tiles2 : 0, mine, r, lane, scale,
+      [&](int u, typename C::Plain& x) { C::load_cached(a, s, bh, u * C::KT, tid, values, x); }, put_plain,
+      [&](int u) { return TileMask{s.beside - u * C::KT < C::KT, s.beside - u * C::KT - 1}; });
+  pass_tiles<C, typename C::Plain>(from(tiles2), to(tiles2, tiles), has_rows ? (wave_last - 1) / a.heads_per_kv / C::KT + 1 : 0, mine, r, lane, scale,
+      [&](int u, typename C::Plain& x) { C::load_fresh(a, b, h, u * C::KT, last, tid, values, x); }, put_plain,
+      [&](int u) { return TileMask{u * C::KT + C::KT - 1 > oldest, newest - u * C::KT}; });
   r.l += other_half(r.l);
 
   if constexpr (TW == 1) {
@@ -524,13 +636,14 @@ template <int KB, int VB, int G, int RW, int TW>
 hipError_t launch_form(const ChunkArgs& a, hipStream_t stream) {
   const long long items = (long long)a.batch * a.n_kv_heads * a.n_splits * a.row_blocks;
   if (items >= (1LL << 30)) return hipErrorInvalidValue;
-  const unsigned per = (unsigned)ceil_div(items, 8);
-  attention_chunk_kernel<KB, VB, G, RW, TW><<<per * 8, 64 * RW * TW, 0, stream>>>(a, (unsigned)items, per);
+  attention_chunk_kernel<KB, VB, G, RW, TW><<<(unsigned)items, 64 * RW * TW, 0, stream>>>(a);
   return hipGetLastError();
 }
 template <int KB, int VB, int G>
 hipError_t launch_bits(const ChunkArgs& a, const ChunkForm& form, hipStream_t stream) {
-  return form.row_waves == 1 ? launch_form<KB, VB, G, 1, 4>(a, stream) : launch_form<KB, VB, G, 4, 1>(a, stream);
+  return form.row_waves == 1   ? launch_form<KB, VB, G, 1, 4>(a, stream)
+         : form.row_waves == 4 ? launch_form<KB, VB, G, 4, 1>(a, stream)
+                               : launch_form<KB, VB, G, 8, 1>(a, stream);
 }
 template <int G>
 hipError_t launch_group(const ChunkArgs& a, int kb, int vb, const ChunkForm& form, hipStream_t stream) {

@@ -16,7 +16,7 @@ struct ChunkForm {
   int tile;                             // tokens of a tile
 };
 // Few rows: a wavefront has all of them, and four of a work-group share the keys; else four wavefronts of 32 rows share a tile.
-inline ChunkForm chunk_form(long long rows) { return rows <= kChunkWaveRows ? ChunkForm{1, 4, 32} : ChunkForm{4, 1, 64}; }
+inline ChunkForm chunk_form(long long rows) { return rows <= kChunkWaveRows ? ChunkForm{1, 4, 32} : rows <= 128 ? ChunkForm{4, 1, 64} : ChunkForm{8, 1, 64}; }
 
 struct ChunkSizes {
   ChunkForm form;
