@@ -67,6 +67,26 @@ struct Piece {
   }
 };
 
+// Masks of fields at bits 0, 2, .. of both halves of a word, in registers: an instruction that ANDs and ORs takes no literals.
+template <int BITS>
+struct Masks {
+  uint32_t at[BITS == 2 ? 5 : BITS == 3 ? 4 : 2], high[BITS == 3 ? 4 : 1];
+  __device__ __forceinline__ void start() {
+#pragma unroll
+    for (int i = 0; i < (BITS == 2 ? 5 : BITS == 3 ? 4 : 2); ++i) {
+      at[i] = (BITS == 4 ? 0x000f000fu << (4 * i) : 0x00030003u << (2 * i));
+      asm("" : "+v"(at[i]));
+    }
+    if constexpr (BITS == 3) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        high[i] = 0x00040004u << (2 * i);
+        asm("" : "+v"(high[i]));
+      }
+    }
+  }
+};
+
 template <int BITS>
 struct Decoder {
   half2_t s, z;
@@ -84,46 +104,46 @@ struct Decoder {
       off[i] = asym ? c0 : c1;
     }
   }
-  // the field at bit AT of each half (AT even, up to 8)
+  // the field at bit AT of each half (AT even, up to 8); three bits: its high bit, in the place above the low ones, in `high`
   template <int AT>
-  __device__ __forceinline__ uint32_t value(uint32_t x) const {
-    constexpr uint32_t mask = ((1u << BITS) - 1u) << AT, base = (25u - AT) << 10;
-    const half2_t raw = as_half2((x & (mask * 0x10001u)) | (base * 0x10001u));
-    return as_u32(__builtin_elementwise_fma(raw + off[AT / 2], s, z));
+  __device__ __forceinline__ uint32_t value(const Masks<BITS>& m, uint32_t x, uint32_t high = 0u) const {
+    constexpr uint32_t base = ((25u - AT) << 10) * 0x10001u;
+    uint32_t raw = (x & m.at[BITS == 4 ? AT / 4 : AT / 2]) | base;
+    if constexpr (BITS == 3) raw = (high & m.high[AT / 2]) | raw;
+    return as_u32(__builtin_elementwise_fma(as_half2(raw) + off[AT / 2], s, z));
   }
 };
 
-// The piece's 32 values as fp16, in the order of the products: 16 words.
+// Fields 16 B .. of a piece as fp16, in the order of the products; PART 0, 1: the first and the last four words, those of one half
+// of a wavefront.
+template <int BITS, int B, int PART>
+__device__ __forceinline__ u32x4 decode_part(const Masks<BITS>& m, const Decoder<BITS>& d, const uint32_t (&w)[BITS]) {
+  if constexpr (BITS == 4) {
+    const uint32_t x = PART ? high_halves(w[2 * B], w[2 * B + 1]) : low_halves(w[2 * B], w[2 * B + 1]);
+    return u32x4{d.template value<0>(m, x), d.template value<4>(m, x), d.template value<0>(m, x >> 8), d.template value<4>(m, x >> 8)};
+  } else if constexpr (BITS == 2) {
+    const uint32_t x = w[B], y = x >> 10;
+    if constexpr (PART == 0) return u32x4{d.template value<0>(m, x), d.template value<2>(m, x), d.template value<4>(m, x), d.template value<6>(m, x)};
+    else return u32x4{d.template value<8>(m, x), d.template value<0>(m, y), d.template value<2>(m, y), d.template value<4>(m, y)};
+  } else {
+    // low bits of fields k and 8 + k at bits 2 k of the halves, their high bits at bit k of h
+    const uint32_t n = w[2] >> (16 * B), h = (n & 0xffu) | (n & 0xff00u) << 8;
+    const uint32_t x = PART ? w[B] >> 8 : w[B];
+    if constexpr (PART == 0)
+      return u32x4{d.template value<0>(m, x, h << 2), d.template value<2>(m, x, h << 3), d.template value<4>(m, x, h << 4), d.template value<6>(m, x, h << 5)};
+    else
+      return u32x4{d.template value<0>(m, x, h >> 2), d.template value<2>(m, x, h >> 1), d.template value<4>(m, x, h), d.template value<6>(m, x, h << 1)};
+  }
+}
+
+// The piece's 32 values: 16 words.
 template <int BITS>
-__device__ __forceinline__ void decode(const Piece<BITS>& p, uint32_t (&out)[16]) {
+__device__ __forceinline__ void decode(const Masks<BITS>& m, const Piece<BITS>& p, uint32_t (&out)[16]) {
   Decoder<BITS> d;
   d.start(p.scale, p.zero);
+  const u32x4 w[4] = {decode_part<BITS, 0, 0>(m, d, p.w), decode_part<BITS, 0, 1>(m, d, p.w), decode_part<BITS, 1, 0>(m, d, p.w), decode_part<BITS, 1, 1>(m, d, p.w)};
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    uint32_t* o = out + 8 * b;
-    if constexpr (BITS == 4) {
-      const uint32_t lo = low_halves(p.w[2 * b], p.w[2 * b + 1]), hi = high_halves(p.w[2 * b], p.w[2 * b + 1]);
-      o[0] = d.template value<0>(lo); o[1] = d.template value<4>(lo);
-      o[2] = d.template value<0>(lo >> 8); o[3] = d.template value<4>(lo >> 8);
-      o[4] = d.template value<0>(hi); o[5] = d.template value<4>(hi);
-      o[6] = d.template value<0>(hi >> 8); o[7] = d.template value<4>(hi >> 8);
-    } else if constexpr (BITS == 2) {
-      const uint32_t x = p.w[b], y = x >> 10;
-      o[0] = d.template value<0>(x); o[1] = d.template value<2>(x); o[2] = d.template value<4>(x);
-      o[3] = d.template value<6>(x); o[4] = d.template value<8>(x);
-      o[5] = d.template value<0>(y); o[6] = d.template value<2>(y); o[7] = d.template value<4>(y);
-    } else {
-      // three-bit fields put together in place: low bits of fields k and 8 + k at bits 2 k of the halves, their high bits at bit k of h
-      const uint32_t x = p.w[b], n = p.w[2] >> (16 * b);
-      const uint32_t h = (n & 0xffu) | (n & 0xff00u) << 8;
-      auto field = [&](uint32_t low, uint32_t high, int at) { return (low & (0x00030003u << at)) | (high & (0x00040004u << at)); };
-      const uint32_t y = x >> 8;
-      o[0] = d.template value<0>(field(x, h << 2, 0)); o[1] = d.template value<2>(field(x, h << 3, 2));
-      o[2] = d.template value<4>(field(x, h << 4, 4)); o[3] = d.template value<6>(field(x, h << 5, 6));
-      o[4] = d.template value<0>(field(y, h >> 2, 0)); o[5] = d.template value<2>(field(y, h >> 1, 2));
-      o[6] = d.template value<4>(field(y, h, 4)); o[7] = d.template value<6>(field(y, h << 1, 6));
-    }
-  }
+  for (int i = 0; i < 16; ++i) out[i] = w[i / 4][i % 4];
 }
 
 __device__ __forceinline__ void put_words(char* dst, const uint32_t (&w)[16]) {
@@ -195,6 +215,7 @@ struct ChunkKernel {
   static constexpr bool ONE = APART && KB == VB;         // a thread's piece is a key's or a value's, decoded alike
   struct Packed { Piece<KB> k[P]; Piece<VB> v[ONE ? 1 : P]; };
   struct Plain { u32x4 k[P][4]; u32x4 v[P][4]; };
+  enum Which { kBoth, kKeys, kValues };                  // of a thread's pieces
 
   // Store rows row0 .. (a multiple of the tile, so one page holds them): pieces in registers.  Behind the last packed row: the
   // same rows again, whose scores are masked.
@@ -232,7 +253,8 @@ struct ChunkKernel {
       }
     }
   }
-  static __device__ __forceinline__ void put_packed(char* buf, int tid, bool values, const Packed& x) {
+  struct FieldMasks { Masks<KB> k; Masks<VB> v; };
+  static __device__ __forceinline__ void put_packed(const FieldMasks& f, char* buf, int tid, bool values, const Packed& x) {
 #pragma unroll
     for (int m = 0; m < P; ++m) {
       const int p = (APART ? tid % (NT / 2) : tid) + m * NT;
@@ -240,18 +262,18 @@ struct ChunkKernel {
       char* k = buf + (p >> 2) * kKeyPitch + (p & 3) * 64;
       char* v = buf + VALUES + (p % D) * VPITCH + (p / D) * 64;
       if constexpr (!APART) {
-        decode<KB>(x.k[m], w);
+        decode<KB>(f.k, x.k[m], w);
         put_words(k, w);
-        decode<VB>(x.v[m], w);
+        decode<VB>(f.v, x.v[m], w);
         put_words(v, w);
       } else if constexpr (KB == VB) {
-        decode<KB>(x.k[0], w);
+        decode<KB>(f.k, x.k[0], w);
         put_words(values ? v : k, w);
       } else if (values) {
-        decode<VB>(x.v[m], w);
+        decode<VB>(f.v, x.v[m], w);
         put_words(v, w);
       } else {
-        decode<KB>(x.k[m], w);
+        decode<KB>(f.k, x.k[m], w);
         put_words(k, w);
       }
     }
@@ -265,11 +287,12 @@ struct ChunkKernel {
     return x.ring + (bh * x.slots + (uint32_t)token % (uint32_t)x.slots) * D;
   }
   // Tile of numbers w0 .. (behind the last one: the last one again, whose scores are masked).
+  template <Which WHICH = kBoth>
   static __device__ __forceinline__ void load_cached(const ChunkArgs& a, const ChunkSeq& s, long long bh, int w0, int tid, bool values, Plain& x) {
 #pragma unroll
     for (int m = 0; m < P; ++m) {
       const int p = (APART ? tid % (NT / 2) : tid) + m * NT;
-      if (!APART || !values) {
+      if (WHICH != kValues && (!APART || !values)) {
         const int w = w0 + (p >> 2) < s.beside ? w0 + (p >> 2) : s.beside - 1, quarter = p & 3;
         const __half* row = cached_row(a, s, a.k, s.packed_k, bh, w);
         if (row) {
@@ -283,7 +306,9 @@ struct ChunkKernel {
           Piece<KB> piece;
           piece.load(codes + quarter * Piece<KB>::BYTES, codes + D * 2 / 8 + quarter * 4, a.k.scales + at, a.k.zeros + at);
           uint32_t o[16];
-          decode<KB>(piece, o);
+          Masks<KB> masks;
+          masks.start();
+          decode<KB>(masks, piece, o);
 #pragma unroll
           for (int i = 0; i < 2; ++i) {                    // (back into the order of the channels, as the other rows are)
             const uint32_t* q = o + 8 * i;
@@ -292,7 +317,7 @@ struct ChunkKernel {
           }
         }
       }
-      if (APART && !values) continue;
+      if (WHICH == kKeys || (APART && !values)) continue;
       const int set = p % (KT / 4), chunk = p / (KT / 4);
       const int first = w0 + 16 * (set >> 2) + 2 * (set & 3);
 #pragma unroll
@@ -303,18 +328,19 @@ struct ChunkKernel {
     }
   }
   // Tile of new tokens i0 .. (behind the last one, `last`: that one again, whose scores are masked).
+  template <Which WHICH = kBoth>
   static __device__ __forceinline__ void load_fresh(const ChunkArgs& a, int b, int h, int i0, int last, int tid, bool values, Plain& x) {
     const RowView &k = a.k.fresh, &v = a.v.fresh;
 #pragma unroll
     for (int m = 0; m < P; ++m) {
       const int p = (APART ? tid % (NT / 2) : tid) + m * NT;
-      if (!APART || !values) {
+      if (WHICH != kValues && (!APART || !values)) {
         const int i = i0 + (p >> 2) < last ? i0 + (p >> 2) : last;
         const __half* src = k.p + b * k.batch + h * k.head + i * k.token + (p & 3) * 32;
 #pragma unroll
         for (int e = 0; e < 4; ++e) x.k[m][e] = *reinterpret_cast<const u32x4*>(src + 8 * e);
       }
-      if (APART && !values) continue;
+      if (WHICH == kKeys || (APART && !values)) continue;
       const int set = p % (KT / 4), chunk = p / (KT / 4);
       const int first = i0 + 16 * (set >> 2) + 2 * (set & 3);
       const __half* src = v.p + b * v.batch + h * v.head + 8 * chunk;
@@ -325,11 +351,12 @@ struct ChunkKernel {
       }
     }
   }
+  template <Which WHICH = kBoth>
   static __device__ __forceinline__ void put_plain(char* buf, int tid, bool values, const Plain& x) {
 #pragma unroll
     for (int m = 0; m < P; ++m) {
       const int p = (APART ? tid % (NT / 2) : tid) + m * NT;
-      if (!APART || !values) {
+      if (WHICH != kValues && (!APART || !values)) {
         char* k = buf + (p >> 2) * kKeyPitch + (p & 3) * 64;
 #pragma unroll
         for (int i = 0; i < 4; i += 2) {
@@ -338,7 +365,7 @@ struct ChunkKernel {
           *reinterpret_cast<u32x4*>(k + 16 * i + 16) = u32x4{low_halves(f.z, g.z), high_halves(f.z, g.z), low_halves(f.w, g.w), high_halves(f.w, g.w)};
         }
       }
-      if (APART && !values) continue;
+      if (WHICH == kKeys || (APART && !values)) continue;
       const int set = p % (KT / 4), chunk = p / (KT / 4);
       char* v = buf + VALUES + 8 * chunk * VPITCH + 8 * set;
 #pragma unroll
@@ -358,11 +385,11 @@ struct ChunkKernel {
   };
 
   static __device__ __forceinline__ void scores(const char* buf, const Rows& r, int lane, float16_t (&s)[NB]) {
-    const char* keys = buf + (lane & 31) * kKeyPitch + 16 * (lane >> 5);
+    const char* keys = buf + (lane & 31) * kKeyPitch + 128 * (lane >> 5);
     // operands eight ahead of their instructions; what decodes the next tile may stand between these
     half8_t k[8];
 #pragma unroll
-    for (int st = 0; st < 8; ++st) k[st] = *reinterpret_cast<const half8_t*>(keys + 32 * st);
+    for (int st = 0; st < 8; ++st) k[st] = *reinterpret_cast<const half8_t*>(keys + 16 * st);
     keep_order();
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
@@ -370,18 +397,31 @@ struct ChunkKernel {
 #pragma unroll
       for (int st = 0; st < 8; ++st) {
         s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[st], r.q[st], s[n], 0, 0, 0);
-        if (n + 1 < NB) k[st] = *reinterpret_cast<const half8_t*>(keys + 32 * (n + 1) * kKeyPitch + 32 * st);
+        if (n + 1 < NB) k[st] = *reinterpret_cast<const half8_t*>(keys + 32 * (n + 1) * kKeyPitch + 16 * st);
         keep_order();
       }
     }
   }
   // masked: some row does not attend to every token of the tile; limit: the last one that the lane's row attends to, counted from the tile's first.
   static __device__ __forceinline__ void finish(const char* buf, Rows& r, float16_t (&s)[NB], int lane, bool masked, int limit, float scale) {
-    const int half = lane >> 5;
-    const char* values = buf + VALUES + (lane & 31) * VPITCH + 16 * half;
+    const char* values = buf + VALUES + (lane & 31) * VPITCH + 16 * (lane >> 5);
     half8_t v[8];                                        // (the first values are on their way under the softmax)
 #pragma unroll
     for (int x = 0; x < 8; ++x) v[x] = *reinterpret_cast<const half8_t*>(values + 32 * (x & 3) * VPITCH + 32 * (x >> 2));
+    half8_t p[2 * NB];
+    weights(r, s, lane >> 5, masked, limit, scale, p);
+#pragma unroll
+    for (int st = 0; st < 2 * NB; ++st)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int at = 4 * st + x;
+        r.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[at & 7], p[st], r.o[x], 0, 0, 0);
+        if (at + 8 < 8 * NB) v[at & 7] = *reinterpret_cast<const half8_t*>(values + 32 * x * VPITCH + 32 * (st + 2));
+        keep_order();
+      }
+  }
+  // The softmax weights of a tile's scores, as operands; level and sum move on.
+  static __device__ __forceinline__ void weights(Rows& r, float16_t (&s)[NB], int half, bool masked, int limit, float scale, half8_t (&p)[2 * NB]) {
     if (masked) {
 #pragma unroll
       for (int n = 0; n < NB; ++n)
@@ -407,7 +447,6 @@ struct ChunkKernel {
       r.m = level;
     }
     const float level = r.m == -INFINITY ? 0.f : r.m;    // (a row that has met no token yet)
-    half8_t p[2 * NB];
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -419,15 +458,108 @@ struct ChunkKernel {
 #pragma unroll
       for (int e = 0; e < 8; e += 2)
         r.l = __builtin_amdgcn_fdot2(half2_t{p[st][e], p[st][e + 1]}, half2_t{(_Float16)1.0f, (_Float16)1.0f}, r.l, false);
+  }
+
+  // ---- a wavefront by itself takes packed tiles of 32 tokens straight from memory to its operands.  Keys: a lane has half a row of one
+  // token, 64 channels.  Values: a lane has four channels, of which it needs the sixteen tokens of its half (the other half of the
+  // wavefront loads the same words).
+  struct Direct {
+    uint32_t k[2][KB], kscale, kzero;
+    uint32_t v[4][VB], vscale[4], vzero[4];
+  };
+  // (addresses: a uniform one and 32 bits of a lane's own)
+  static __device__ __forceinline__ void load_direct_keys(const ChunkArgs& a, long long lin, int lane, Direct& x) {
+    const uint32_t tok = (uint32_t)lane & 31u, half = (uint32_t)lane >> 5;
+    const uint8_t* codes = a.k.codes + lin * (16 * KB);
+    const uint32_t low = tok * (16 * KB) + half * (2 * Piece<KB>::BYTES);
+    constexpr int N = KB == 3 ? 2 : KB;                  // words of a piece's (low) plane
+    uint32_t w[2 * N];
 #pragma unroll
-    for (int st = 0; st < 2 * NB; ++st)
+    for (int i = 0; i < 2 * N; i += 4) {
+      const u32x4 q = *reinterpret_cast<const u32x4*>(codes + (low + 4 * i));
+      w[i] = q.x; w[i + 1] = q.y; w[i + 2] = q.z; w[i + 3] = q.w;
+    }
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int at = 4 * st + x;
-        r.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[at & 7], p[st], r.o[x], 0, 0, 0);
-        if (at + 8 < 8 * NB) v[at & 7] = *reinterpret_cast<const half8_t*>(values + 32 * x * VPITCH + 32 * (st + 2));
-        keep_order();
-      }
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int i = 0; i < N; ++i) x.k[p][i] = w[p * N + i];
+    if constexpr (KB == 3) {
+      const u32x2 q = *reinterpret_cast<const u32x2*>(codes + (tok * (16 * KB) + D * 2 / 8 + half * 8));
+      x.k[0][2] = q.x; x.k[1][2] = q.y;
+    }
+    const uint8_t* scales = reinterpret_cast<const uint8_t*>(a.k.scales + lin * (D / G));
+    const uint8_t* zeros = reinterpret_cast<const uint8_t*>(a.k.zeros + lin * (D / G));
+    const uint32_t at = tok * (2 * D / G) + half * (128 / G);
+    if constexpr (G == 32) {                             // (both groups' in one word)
+      x.kscale = *reinterpret_cast<const uint32_t*>(scales + at);
+      x.kzero = *reinterpret_cast<const uint32_t*>(zeros + at);
+    } else {
+      x.kscale = *reinterpret_cast<const unsigned short*>(scales + at);
+      x.kzero = *reinterpret_cast<const unsigned short*>(zeros + at);
+    }
+  }
+  static __device__ __forceinline__ void load_direct_values(const ChunkArgs& a, long long lin, int row0, int lane, Direct& x) {
+    const int part = G == 64 ? (row0 & 63) / 32 : 0;     // (half a group of 64)
+    const long long first = G == 64 ? lin - (row0 & 63) : lin;
+    constexpr uint32_t RUN = G * VB / 8;                 // bytes of a channel
+    const uint32_t c = (uint32_t)lane & 31u;
+    const uint8_t* codes = a.v.codes + first * (16 * VB) + part * Piece<VB>::BYTES;
+    const uint8_t* high = a.v.codes + first * (16 * VB) + G * 2 / 8 + part * 4;
+    const uint8_t* scales = reinterpret_cast<const uint8_t*>(a.v.scales + first * (D / G));
+    const uint8_t* zeros = reinterpret_cast<const uint8_t*>(a.v.zeros + first * (D / G));
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const uint32_t run = c * RUN + 32 * n * RUN, at = 2 * c + 64 * n;
+      Piece<VB> p;
+      p.load(codes + run, high + run, reinterpret_cast<const __half*>(scales + at), reinterpret_cast<const __half*>(zeros + at));
+#pragma unroll
+      for (int i = 0; i < VB; ++i) x.v[n][i] = p.w[i];
+      x.vscale[n] = p.scale;
+      x.vzero[n] = p.zero;
+    }
+  }
+  template <int P>
+  static __device__ __forceinline__ void direct_scores(const FieldMasks& f, const Direct& x, const Rows& r, Decoder<KB>& d, float16_t& s) {
+    if (P == 0) d.start(x.kscale & 0xffffu, x.kzero & 0xffffu);
+    else if (G == 32) d.start(x.kscale >> 16, x.kzero >> 16);
+    s = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, decode_part<KB, 0, 0>(f.k, d, x.k[P])), r.q[4 * P], s, 0, 0, 0);
+    s = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, decode_part<KB, 0, 1>(f.k, d, x.k[P])), r.q[4 * P + 1], s, 0, 0, 0);
+    s = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, decode_part<KB, 1, 0>(f.k, d, x.k[P])), r.q[4 * P + 2], s, 0, 0, 0);
+    s = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, decode_part<KB, 1, 1>(f.k, d, x.k[P])), r.q[4 * P + 3], s, 0, 0, 0);
+  }
+  // Words of the fields that the lane's half needs, brought to the places of half 0, so that one code serves both.
+  static __device__ __forceinline__ void own_half(const uint32_t (&w)[VB], int half, uint32_t (&out)[VB]) {
+    if constexpr (VB == 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) out[i] = half ? w[i] >> 16 : w[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) out[i] = half ? w[i] >> 8 : w[i];
+      if constexpr (VB == 3) out[2] = half ? w[2] >> 4 : w[2];
+    }
+  }
+  static __device__ __forceinline__ void direct_tile(const ChunkArgs& a, const FieldMasks& f, Direct& x, Rows& r, int lane, float scale, long long next, int next_row0) {
+    float16_t s[NB];
+    s[0] = float16_t{};
+    Decoder<KB> dk;
+    direct_scores<0>(f, x, r, dk, s[0]);
+    __builtin_amdgcn_sched_barrier(0);
+    direct_scores<1>(f, x, r, dk, s[0]);
+    load_direct_keys(a, next, lane, x);
+    __builtin_amdgcn_sched_barrier(0);
+    half8_t p[2 * NB];
+    weights(r, s, lane >> 5, false, 0, scale, p);
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      Decoder<VB> d;
+      d.start(x.vscale[n], x.vzero[n]);
+      uint32_t w[VB];
+      own_half(x.v[n], lane >> 5, w);
+      r.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, decode_part<VB, 0, 0>(f.v, d, w)), p[0], r.o[n], 0, 0, 0);
+      r.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, decode_part<VB, 1, 0>(f.v, d, w)), p[1], r.o[n], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);                 // (decoded early, the operands do not fit the registers)
+    }
+    load_direct_values(a, next, next_row0, lane, x);
   }
 
   static __device__ __forceinline__ void load_queries(const ChunkArgs& a, int b, int h, int row, bool live, int half, Rows& r) {
@@ -437,10 +569,11 @@ struct ChunkKernel {
     for (int st = 0; st < 8; ++st) {
       u32x2 x = {0u, 0u}, y = {0u, 0u};
       if (live) {
-        x = *reinterpret_cast<const u32x2*>(src + 16 * st + 4 * half);
-        y = *reinterpret_cast<const u32x2*>(src + 16 * st + 8 + 4 * half);
+        const int c = 64 * half + 16 * (st / 2) + 4 * (st % 2);
+        x = *reinterpret_cast<const u32x2*>(src + c);
+        y = *reinterpret_cast<const u32x2*>(src + c + 8);
         if (a.q_scale) {
-          const float* f = a.q_scale + h * D + 16 * st + 4 * half;
+          const float* f = a.q_scale + h * D + c;
           __half* hx = reinterpret_cast<__half*>(&x);
           __half* hy = reinterpret_cast<__half*>(&y);
 #pragma unroll
@@ -496,10 +629,8 @@ __device__ __forceinline__ void pass_tiles(int u0, int u1, int mine, char* lds, 
   Regs x;
   float16_t sc[C::NB];
   if constexpr (C::NBUF == 1) {
-    load(u0, x);
     for (int u = u0; u < u1; ++u) {
-      put(lds, x);
-      if (u + 1 < u1) load(u + 1, x);
+      load(u, x);                                        // (brings them into LDS, too)
       asm volatile("" ::: "memory");                     // (a wavefront's LDS operations are performed in order)
       __builtin_amdgcn_wave_barrier();
       if (u < mine) {
@@ -554,7 +685,7 @@ __global__ void __launch_bounds__(64 * RW * TW) __attribute__((amdgpu_waves_per_
   const int rows = s.t * a.heads_per_kv;
   const int row_base = (a.row_blocks - 1 - (int)rank) * 32 * RW;
   if (row_base >= rows) return;                          // (uniform)
-  const int wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63, half = lane >> 5;
   const int group = wave / RW, tid = (int)threadIdx.x % C::NT;
   const int first = row_base + (wave % RW) * 32, row = first + (lane & 31);
   const bool live = row < rows;
@@ -580,18 +711,59 @@ __global__ void __launch_bounds__(64 * RW * TW) __attribute__((amdgpu_waves_per_
   const int t0 = part * per + (part < more ? part : more), t1 = t0 + per + (part < more ? 1 : 0);
   auto from = [&](int t) { return t0 > t ? t0 - t : 0; };
   auto to = [&](int t, int end) { return (t1 < end ? t1 : end) - t; };
-  const bool values = __builtin_amdgcn_readfirstlane(wave) >= RW / 2;
+  const bool values = wave >= RW / 2;
   char* mine = lds + group * C::BUF * C::NBUF;
-  auto put_packed = [&](char* at, const typename C::Packed& x) { C::put_packed(at, tid, values, x); };
+  typename C::FieldMasks masks;
+  masks.k.start();
+  masks.v.start();
+  auto put_packed = [&](char* at, const typename C::Packed& x) { C::put_packed(masks, at, tid, values, x); };
   auto put_plain = [&](char* at, const typename C::Plain& x) { C::put_plain(at, tid, values, x); };
-  pass_tiles<C, typename C::Packed>(from(0), to(0, tiles1), has_rows ? tiles1 : 0, mine, r, lane, scale,
-      [&](int u, typename C::Packed& x) { C::load_packed(a, s, bh, u * C::KT, tid, values, x); }, put_packed,
-      [&](int u) { return TileMask{s.packed_v - u * C::KT < C::KT, s.packed_v - u * C::KT - 1}; });
+  if constexpr (RW == 1) {
+    const int u0 = from(0), u1 = to(0, tiles1);
+    auto row = [&](int u) { return (u < u1 ? u : u1 - 1) * C::KT; };
+    auto place = [&](int row0) { return store_row(a.pages, a.n_kv_heads, a.capacity, bh, row0); };
+    if (u0 < u1) {
+      // two tiles under way: a tile's registers are loaded again as soon as they have been used
+      typename C::Direct x, y;
+      C::load_direct_keys(a, place(row(u0)), lane, x);
+      C::load_direct_values(a, place(row(u0)), row(u0), lane, x);
+      C::load_direct_keys(a, place(row(u0 + 1)), lane, y);
+      C::load_direct_values(a, place(row(u0 + 1)), row(u0 + 1), lane, y);
+      for (int u = u0;;) {
+        C::direct_tile(a, masks, x, r, lane, scale, place(row(u + 2)), row(u + 2));
+        if (++u == u1) break;
+        C::direct_tile(a, masks, y, r, lane, scale, place(row(u + 2)), row(u + 2));
+        if (++u == u1) break;
+      }
+    }
+  } else {
+    pass_tiles<C, typename C::Packed>(from(0), to(0, tiles1), has_rows ? tiles1 : 0, mine, r, lane, scale,
+        [&](int u, typename C::Packed& x) { C::load_packed(a, s, bh, u * C::KT, tid, values, x); }, put_packed,
+        [&](int u) { return TileMask{s.packed_v - u * C::KT < C::KT, s.packed_v - u * C::KT - 1}; });
+  }
   pass_tiles<C, typename C::Plain>(from(tiles1), to(tiles1, tiles2), has_rows ? tiles2 : 0, mine, r, lane, scale,
-      [&](int u, typename C::Plain& x) { C::load_cached(a, s, bh, u * C::KT, tid, values, x); }, put_plain,
+      [&](int u, typename C::Plain& x) {
+        if constexpr (RW > 1) {
+          C::load_cached(a, s, bh, u * C::KT, tid, values, x);
+        } else {                                           // (one tensor after the other: all registers are not there for both)
+          C::template load_cached<C::kKeys>(a, s, bh, u * C::KT, tid, values, x);
+          C::template put_plain<C::kKeys>(mine, tid, values, x);
+          C::template load_cached<C::kValues>(a, s, bh, u * C::KT, tid, values, x);
+          C::template put_plain<C::kValues>(mine, tid, values, x);
+        }
+      }, put_plain,
       [&](int u) { return TileMask{s.beside - u * C::KT < C::KT, s.beside - u * C::KT - 1}; });
   pass_tiles<C, typename C::Plain>(from(tiles2), to(tiles2, tiles), has_rows ? (wave_last - 1) / a.heads_per_kv / C::KT + 1 : 0, mine, r, lane, scale,
-      [&](int u, typename C::Plain& x) { C::load_fresh(a, b, h, u * C::KT, last, tid, values, x); }, put_plain,
+      [&](int u, typename C::Plain& x) {
+        if constexpr (RW > 1) {
+          C::load_fresh(a, b, h, u * C::KT, last, tid, values, x);
+        } else {
+          C::template load_fresh<C::kKeys>(a, b, h, u * C::KT, last, tid, values, x);
+          C::template put_plain<C::kKeys>(mine, tid, values, x);
+          C::template load_fresh<C::kValues>(a, b, h, u * C::KT, last, tid, values, x);
+          C::template put_plain<C::kValues>(mine, tid, values, x);
+        }
+      }, put_plain,
       [&](int u) { return TileMask{u * C::KT + C::KT - 1 > oldest, newest - u * C::KT}; });
   r.l += other_half(r.l);
 
