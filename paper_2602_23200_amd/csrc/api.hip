@@ -727,7 +727,7 @@ int chunk_attention(const innerq_config_t* cfg, const innerq_cache_t* cache, con
   if (misaligned(workspace) || (q_scale && misaligned(q_scale))) return INNERQ_E_ALIGN;
   if (!chunk_rows_fit(c, t_new)) return INNERQ_E_UNSUPPORTED;
   const ChunkSizes sizes = chunk_sizes(c, t_new);
-  if (workspace_bytes < sizes.bytes) return INNERQ_E_WORKSPACE;
+  if (workspace_bytes < chunk_workspace_bytes(c, t_new)) return INNERQ_E_WORKSPACE;
   ChunkArgs a;
   a.k = chunk_tensor(c, *cache, 0, k_new, *k_strides);
   a.v = chunk_tensor(c, *cache, 1, v_new, *v_strides);
@@ -745,13 +745,35 @@ int chunk_attention(const innerq_config_t* cfg, const innerq_cache_t* cache, con
   a.t_dev = t_new_dev;
   a.row_blocks = (int)sizes.row_blocks;
   a.n_splits = chunk_splits(sizes, tokens);
-  a.ws_ml = static_cast<float*>(workspace);
-  a.ws_o = a.ws_ml + (sizes.heads * sizes.rows * a.n_splits * 2 + 3) / 4 * 4;
+  a.table = nullptr;
+  a.list_groups = 0;
+  a.rows_from = 0; a.rows_to = 0x7fffffff;
+  a.ws = reinterpret_cast<float*>(static_cast<char*>(workspace) + kChunkTableBytes);
+  a.ws_few = a.ws;
+  a.slots = sizes.heads * sizes.row_blocks * a.n_splits;
   a.pages = pages_of(c, *cache);
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  hipError_t e = c.group == 32 ? launch_chunk_g32(a, bits_of(c, 0), bits_of(c, 1), sizes.form, stream)
-                               : launch_chunk_g64(a, bits_of(c, 0), bits_of(c, 1), sizes.form, stream);
-  if (e == hipSuccess && a.n_splits > 1) e = launch_chunk_merge(a, stream);
+  auto launch = [&](const ChunkForm& form) {
+    return c.group == 32 ? launch_chunk_g32(a, bits_of(c, 0), bits_of(c, 1), form, stream) : launch_chunk_g64(a, bits_of(c, 0), bits_of(c, 1), form, stream);
+  };
+  if (n_tokens_dev && c.batch <= kChunkListMost) {
+    const ChunkList list = chunk_list(c, t_new);
+    a.table = static_cast<int*>(workspace);
+    a.slots = kChunkListItems;
+    a.rows_to = kChunkWaveRows;
+    a.list_groups = (int)list.few;
+    hipError_t e = launch(kFewRows);
+    if (e == hipSuccess && list.some) {
+      a.ws = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ws) + (size_t)kChunkListItems * chunk_slot_bytes(kFewRows));
+      a.rows_from = kChunkWaveRows; a.rows_to = 0x7fffffff;
+      a.list_groups = (int)list.some;
+      e = launch(kSomeRows);
+    }
+    if (e == hipSuccess) e = launch_chunk_merge(a, kSomeRows, stream);
+    return e == hipSuccess ? INNERQ_OK : INNERQ_E_HIP;
+  }
+  hipError_t e = launch(sizes.form);
+  if (e == hipSuccess && a.n_splits > 1) e = launch_chunk_merge(a, sizes.form, stream);
   return e == hipSuccess ? INNERQ_OK : INNERQ_E_HIP;
 }
 
@@ -817,7 +839,7 @@ int innerq_append_rotated_ragged(const innerq_config_t* cfg, const innerq_cache_
 
 size_t innerq_chunk_workspace_bytes(const innerq_config_t* cfg, int64_t t_new) {
   if (check_config(cfg) != INNERQ_OK || cfg->kind != INNERQ_KIND_INNER || t_new < 1 || !chunk_rows_fit(*cfg, t_new)) return 0;
-  return chunk_sizes(*cfg, t_new).bytes;
+  return chunk_workspace_bytes(*cfg, t_new);
 }
 
 int innerq_chunk_attention(const innerq_config_t* cfg, const innerq_cache_t* cache, const void* k_new, const innerq_strides_t* k_strides,

@@ -28,13 +28,17 @@ struct ChunkArgs {
   int n_tokens;                        // cached, where n_dev is null
   const int* n_dev;
   const int* t_dev;
-  int row_blocks, n_splits;
-  float* ws_ml;                        // [B Hk][rows][n_splits][2], level in the log2 domain and sum
-  float* ws_o;                         // [B Hk][rows][n_splits][d]
+  int row_blocks, n_splits;            // the same for all sequences (without a list)
+  int* table;                          // a list: first slot and splits of every sequence are left here for the merge; else null
+  int list_groups;                     // work-groups of the launch
+  int rows_from, rows_to;              // sequences of this launch: with that many rows (from excluded, to included)
+  float* ws;                           // slots: (level in the log2 domain, sum) of every row, then 128 sums of every row
+  long long slots;                     // that ws holds
+  float* ws_few;                       // merge of a list: the slots of the sequences of few rows (ws: of the others)
   PageMap pages;
 };
 hipError_t launch_chunk_g32(const ChunkArgs& a, int kb, int vb, const ChunkForm& form, hipStream_t stream);
 hipError_t launch_chunk_g64(const ChunkArgs& a, int kb, int vb, const ChunkForm& form, hipStream_t stream);
-hipError_t launch_chunk_merge(const ChunkArgs& a, hipStream_t stream);
+hipError_t launch_chunk_merge(const ChunkArgs& a, const ChunkForm& form, hipStream_t stream);   // form: of the launch (without a list)
 
 }  // namespace innerq

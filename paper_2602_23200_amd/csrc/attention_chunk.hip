@@ -587,11 +587,11 @@ struct ChunkKernel {
     }
   }
 
-  // Channels 32 x .. of a row: the output itself, or the partial result of a split.
-  static __device__ __forceinline__ void store_channels(const ChunkArgs& a, int b, int h, int row, int split, int x, int half, const float16_t& o, float l) {
+  // Channels 32 x .. of a row: the output itself, or (split) the partial result of a slot.
+  static __device__ __forceinline__ void store_channels(const ChunkArgs& a, int b, int h, int row, long long slot_row, bool split, int x, int half, const float16_t& o, float l) {
     const int c0 = 32 * x + 4 * half;
-    if (a.n_splits > 1) {
-      float* dst = a.ws_o + ((((long long)b * a.n_kv_heads + h) * ((long long)a.t_new * a.heads_per_kv) + row) * a.n_splits + split) * D + c0;
+    if (split) {
+      float* dst = a.ws + a.slots * (32 * RW * 2) + slot_row * D + c0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(dst + 8 * i) = float4{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
       return;
@@ -613,11 +613,92 @@ struct ChunkKernel {
       }
     }
   }
-  static __device__ __forceinline__ void store_state(const ChunkArgs& a, int b, int h, int row, int split, float m, float l) {
-    float* ml = a.ws_ml + ((((long long)b * a.n_kv_heads + h) * ((long long)a.t_new * a.heads_per_kv) + row) * a.n_splits + split) * 2;
-    *reinterpret_cast<float2*>(ml) = float2{m, l};
+  static __device__ __forceinline__ void store_state(const ChunkArgs& a, long long slot_row, float m, float l) {
+    *reinterpret_cast<float2*>(a.ws + slot_row * 2) = float2{m, l};
   }
 };
+
+// ---- a ragged batch: what a work-group does, from the counts of all sequences (four a lane).  The keys of a sequence are cut into ranges of
+// `length` tiles, the least with which the launch's items (sequence, head, block of rows, range) are no more than aimed at; where even
+// whole sequences are more, they are not cut.  Every wavefront finds the same.
+struct ChunkWork { int b, h, row_block, split, n_splits, slot; };
+
+__device__ __forceinline__ int wave_sum(int x) {
+#pragma unroll
+  for (int i = 1; i < 64; i *= 2) x += __shfl_xor(x, i);
+  return x;
+}
+template <int ROWS, int TILE>                            // TILE: tokens that the work-group takes a turn
+__device__ __forceinline__ bool find_work(const ChunkArgs& a, int group, int item, ChunkWork& w) {
+  constexpr int N = kChunkListMost / 64, LEAST = 4;      // (a range shorter than that is mostly set-up)
+  const int lane = (int)threadIdx.x & 63;
+  int units[N], tiles[N];                                // (head, block of rows) and tiles of the lane's sequences
+  int most = 1;
+  float work = 0.f;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int b = N * lane + j;
+    units[j] = tiles[j] = 0;
+    if (b < a.batch) {
+      const ChunkSeq s = chunk_seq(a, b, group);
+      const int rows = s.t * a.heads_per_kv;
+      if (rows > a.rows_from && rows <= a.rows_to) {
+        units[j] = a.n_kv_heads * ((rows + ROWS - 1) / ROWS);
+        tiles[j] = (s.n + s.t + TILE - 1) / TILE;
+      }
+    }
+    most = tiles[j] > most ? tiles[j] : most;
+    work += (float)units[j] * (float)tiles[j];
+  }
+#pragma unroll
+  for (int i = 1; i < 64; i *= 2) {
+    const int x = __shfl_xor(most, i);
+    most = x > most ? x : most;
+    work += __shfl_xor(work, i);
+  }
+  most = __builtin_amdgcn_readfirstlane(most);
+  int length = __builtin_amdgcn_readfirstlane((int)(work * (1.0f / kChunkListItems)));
+  length = length < LEAST ? LEAST : length;
+  int mine;
+  for (;; length += 1 + length / 8) {
+    mine = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) mine += units[j] * ((tiles[j] + length - 1) / length);
+    if (length >= most || __builtin_amdgcn_readfirstlane(wave_sum(mine)) <= kChunkListItems) break;
+  }
+  // the sequence whose items hold this one
+  int before = mine;
+#pragma unroll
+  for (int i = 1; i < 64; i *= 2) {
+    const int x = __shfl_up(before, i);
+    if (lane >= i) before += x;
+  }
+  const unsigned long long reach = __builtin_amdgcn_ballot_w64(before > item);
+  if (reach == 0) return false;                          // (uniform)
+  const int owner = __builtin_ctzll(reach);
+  int first = __builtin_amdgcn_readlane(before - mine, owner);
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int u = __builtin_amdgcn_readlane(units[j], owner), t = __builtin_amdgcn_readlane(tiles[j], owner);
+    const int splits = (t + length - 1) / length, all = u * splits;
+    if (item >= first && item < first + all) {
+      const int at = item - first, unit = at / splits, blocks = u / a.n_kv_heads;
+      w.b = N * owner + j;
+      w.split = at - unit * splits;
+      w.n_splits = splits;
+      w.h = unit / blocks;
+      w.row_block = unit - w.h * blocks;
+      w.slot = item;
+      if (at == 0 && threadIdx.x == 0) {
+        a.table[2 * w.b] = item;
+        a.table[2 * w.b + 1] = splits;
+      }
+      return true;
+    }
+    first += all;
+  }
+  return false;
+}
 
 // Tiles u0 .. u1 of one kind: load(u, registers), put(buffer, registers), masks(u) -> {masked, limit} as for finish.  This wavefront's rows
 // attend to those before `mine`.  The next tile is put into LDS, and the one after it loaded, between the two products (behind the last tile:
@@ -675,15 +756,28 @@ template <int KB, int VB, int G, int RW, int TW>
 __global__ void __launch_bounds__(64 * RW * TW) __attribute__((amdgpu_waves_per_eu(2, 2))) attention_chunk_kernel(ChunkArgs a) {
   using C = ChunkKernel<KB, VB, G, RW, TW>;
   __shared__ __align__(16) char lds[C::LDS];
-  const unsigned heads = (unsigned)(a.batch * a.n_kv_heads);
-  const bool pinned = heads % 8u == 0u;
-  const unsigned slot = pinned ? blockIdx.x / 8u : blockIdx.x, mine_heads = pinned ? heads / 8u : heads;
-  const unsigned rank = slot / (mine_heads * (unsigned)a.n_splits), rest = slot % (mine_heads * (unsigned)a.n_splits);
-  const unsigned split = rest % (unsigned)a.n_splits, bh = rest / (unsigned)a.n_splits + (pinned ? blockIdx.x % 8u * mine_heads : 0u);
-  const int b = (int)(bh / (unsigned)a.n_kv_heads), h = (int)(bh % (unsigned)a.n_kv_heads);
+  ChunkWork work;
+  bool listed = false;
+  if constexpr (RW != 8) listed = a.table != nullptr;
+  if (listed) {
+    if (!find_work<32 * RW, C::KT * TW>(a, G, (int)blockIdx.x, work)) return;      // (uniform)
+  } else {
+    const unsigned heads = (unsigned)(a.batch * a.n_kv_heads);
+    const bool pinned = heads % 8u == 0u;
+    const unsigned slot = pinned ? blockIdx.x / 8u : blockIdx.x, mine_heads = pinned ? heads / 8u : heads;
+    const unsigned rank = slot / (mine_heads * (unsigned)a.n_splits), rest = slot % (mine_heads * (unsigned)a.n_splits);
+    const unsigned bh = rest / (unsigned)a.n_splits + (pinned ? blockIdx.x % 8u * mine_heads : 0u);
+    work.split = (int)(rest % (unsigned)a.n_splits);
+    work.n_splits = a.n_splits;
+    work.b = (int)(bh / (unsigned)a.n_kv_heads);
+    work.h = (int)(bh % (unsigned)a.n_kv_heads);
+    work.row_block = a.row_blocks - 1 - (int)rank;
+    work.slot = ((int)bh * a.row_blocks + work.row_block) * a.n_splits + work.split;
+  }
+  const int b = work.b, h = work.h, split = work.split, n_splits = work.n_splits;
+  const long long bh = (long long)b * a.n_kv_heads + h;
   const ChunkSeq s = chunk_seq(a, b, G);
-  const int rows = s.t * a.heads_per_kv;
-  const int row_base = (a.row_blocks - 1 - (int)rank) * 32 * RW;
+  const int rows = s.t * a.heads_per_kv, row_base = work.row_block * 32 * RW;
   if (row_base >= rows) return;                          // (uniform)
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63, half = lane >> 5;
   const int group = wave / RW, tid = (int)threadIdx.x % C::NT;
@@ -706,7 +800,7 @@ __global__ void __launch_bounds__(64 * RW * TW) __attribute__((amdgpu_waves_per_
 
   // tiles: packed rows, cached tokens beside them, new tokens; this wavefront's share of them
   const int tiles1 = (s.packed_v + C::KT - 1) / C::KT, tiles2 = tiles1 + (s.beside + C::KT - 1) / C::KT, tiles = tiles2 + last / C::KT + 1;
-  const int parts = a.n_splits * TW, part = (int)split * TW + group;
+  const int parts = n_splits * TW, part = split * TW + group;
   const int per = tiles / parts, more = tiles % parts;
   const int t0 = part * per + (part < more ? part : more), t1 = t0 + per + (part < more ? 1 : 0);
   auto from = [&](int t) { return t0 > t ? t0 - t : 0; };
@@ -767,11 +861,12 @@ __global__ void __launch_bounds__(64 * RW * TW) __attribute__((amdgpu_waves_per_
       [&](int u) { return TileMask{u * C::KT + C::KT - 1 > oldest, newest - u * C::KT}; });
   r.l += other_half(r.l);
 
+  const long long slot_row = (long long)work.slot * (32 * RW) + row - row_base;
   if constexpr (TW == 1) {
     if (!live) return;
-    if (a.n_splits > 1 && half == 0) C::store_state(a, b, h, row, (int)split, r.m, r.l);
+    if (n_splits > 1 && half == 0) C::store_state(a, slot_row, r.m, r.l);
 #pragma unroll
-    for (int x = 0; x < 4; ++x) C::store_channels(a, b, h, row, (int)split, x, half, r.o[x], r.l);
+    for (int x = 0; x < 4; ++x) C::store_channels(a, b, h, row, slot_row, n_splits > 1, x, half, r.o[x], r.l);
   } else {
     // the wavefronts' results meet in LDS, each joins the channels of its own number
     static_assert(TW == 4 && RW == 1);
@@ -799,14 +894,14 @@ __global__ void __launch_bounds__(64 * RW * TW) __attribute__((amdgpu_waves_per_
       for (int i = 0; i < 16; ++i) sum[i] = __builtin_fmaf(f, o[(n * 64 + wave * 16 + i) * 64 + lane], sum[i]);
     }
     if (!live) return;
-    if (a.n_splits > 1 && half == 0 && wave == 0) C::store_state(a, b, h, row, (int)split, top, l);
-    C::store_channels(a, b, h, row, (int)split, wave, half, sum, l);
+    if (n_splits > 1 && half == 0 && wave == 0) C::store_state(a, slot_row, top, l);
+    C::store_channels(a, b, h, row, slot_row, n_splits > 1, wave, half, sum, l);
   }
 }
 
 template <int KB, int VB, int G, int RW, int TW>
 hipError_t launch_form(const ChunkArgs& a, hipStream_t stream) {
-  const long long items = (long long)a.batch * a.n_kv_heads * a.n_splits * a.row_blocks;
+  const long long items = a.table ? a.list_groups : (long long)a.batch * a.n_kv_heads * a.n_splits * a.row_blocks;
   if (items >= (1LL << 30)) return hipErrorInvalidValue;
   attention_chunk_kernel<KB, VB, G, RW, TW><<<(unsigned)items, 64 * RW * TW, 0, stream>>>(a);
   return hipGetLastError();
@@ -834,8 +929,8 @@ hipError_t launch_group(const ChunkArgs& a, int kb, int vb, const ChunkForm& for
 }
 
 #if INNERQ_CHUNK_G == 32
-// The splits of a row joined: a wavefront a row, a lane per two channels.
-__global__ void __launch_bounds__(256) chunk_merge_kernel(ChunkArgs a, long long rows_all) {
+// The splits of a row joined: a wavefront a row, a lane per two channels.  slot_rows: rows of a slot.
+__global__ void __launch_bounds__(256) chunk_merge_kernel(ChunkArgs a, long long rows_all, int slot_rows) {
   const long long at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int lane = (int)threadIdx.x & 63;
   if (at >= rows_all) return;
@@ -843,28 +938,51 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(ChunkArgs a, long long
   const long long bh = at / rows;
   const int row = (int)(at - bh * rows), b = (int)(bh / a.n_kv_heads), h = (int)(bh - (long long)b * a.n_kv_heads);
   const int i = row / a.heads_per_kv;
-  if (a.t_dev && i >= a.t_dev[b]) return;
-  const float* ml = a.ws_ml + at * a.n_splits * 2;
-  const float* po = a.ws_o + at * a.n_splits * D + 2 * lane;
+  int n_splits = a.n_splits;
+  const float* ws = a.ws;
+  long long slots = a.slots, slot;
+  if (a.table) {
+    const int own = chunk_seq(a, b, 32).t * a.heads_per_kv;       // (the group does not matter)
+    if (row >= own) return;
+    n_splits = a.table[2 * b + 1];
+    if (n_splits == 1) return;                           // (written already)
+    const bool few = own <= kChunkWaveRows;
+    slot_rows = few ? kFewRows.row_waves * kChunkWaveRows : kSomeRows.row_waves * kChunkWaveRows;
+    if (few) ws = a.ws_few;
+    slots = kChunkListItems;
+    slot = a.table[2 * b] + (long long)(h * ((own + slot_rows - 1) / slot_rows) + row / slot_rows) * n_splits;
+  } else {
+    if (a.t_dev && i >= a.t_dev[b]) return;
+    slot = (bh * a.row_blocks + row / slot_rows) * n_splits;
+  }
+  const long long slot_row = slot * slot_rows + row % slot_rows;
+  const float* ml = ws + slot_row * 2;
+  const float* po = ws + slots * slot_rows * 2 + slot_row * D + 2 * lane;
+  const int step_ml = slot_rows * 2, step_o = slot_rows * D;
   float top = -INFINITY;
-  for (int p = lane; p < a.n_splits; p += 64) top = fmaxf(top, ml[2 * p]);
+  for (int p = lane; p < n_splits; p += 64) top = fmaxf(top, ml[p * step_ml]);
 #pragma unroll
   for (int x = 32; x > 0; x /= 2) top = fmaxf(top, __shfl_xor(top, x));
   float den = 0.f, n0 = 0.f, n1 = 0.f;
-  for (int p0 = 0; p0 < a.n_splits; p0 += 64) {
+  for (int p0 = 0; p0 < n_splits; p0 += 64) {
     float f = 0.f, l = 0.f;
-    if (p0 + lane < a.n_splits) {
-      const float2 s = *reinterpret_cast<const float2*>(ml + 2 * (p0 + lane));
+    if (p0 + lane < n_splits) {
+      const float2 s = *reinterpret_cast<const float2*>(ml + (p0 + lane) * step_ml);
       f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - top);
       l = s.y;
     }
     den += f * l;
-    const int n = a.n_splits - p0 < 64 ? a.n_splits - p0 : 64;
-    for (int p = 0; p < n; ++p) {
-      const float2 o = *reinterpret_cast<const float2*>(po + (long long)(p0 + p) * D);
-      const float w = __shfl(f, p);
-      n0 = __builtin_fmaf(w, o.x, n0);
-      n1 = __builtin_fmaf(w, o.y, n1);
+    const int n = n_splits - p0 < 64 ? n_splits - p0 : 64;
+    for (int p = 0; p < n; p += 8) {                     // (eight partial results under way)
+      float2 o[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = *reinterpret_cast<const float2*>(po + (long long)(p0 + (p + e < n ? p + e : n - 1)) * step_o);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float w = p + e < n ? __shfl(f, p + e) : 0.f;
+        n0 = __builtin_fmaf(w, o[e].x, n0);
+        n1 = __builtin_fmaf(w, o[e].y, n1);
+      }
     }
   }
 #pragma unroll
@@ -880,9 +998,9 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(ChunkArgs a, long long
 
 #if INNERQ_CHUNK_G == 32
 hipError_t launch_chunk_g32(const ChunkArgs& a, int kb, int vb, const ChunkForm& form, hipStream_t stream) { return launch_group<32>(a, kb, vb, form, stream); }
-hipError_t launch_chunk_merge(const ChunkArgs& a, hipStream_t stream) {
+hipError_t launch_chunk_merge(const ChunkArgs& a, const ChunkForm& form, hipStream_t stream) {
   const long long rows = (long long)a.batch * a.n_kv_heads * a.t_new * a.heads_per_kv;
-  chunk_merge_kernel<<<(unsigned)ceil_div(rows, 4), 256, 0, stream>>>(a, rows);
+  chunk_merge_kernel<<<(unsigned)ceil_div(rows, 4), 256, 0, stream>>>(a, rows, form.rows());
   return hipGetLastError();
 }
 #else

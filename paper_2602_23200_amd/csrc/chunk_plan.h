@@ -8,35 +8,39 @@ namespace innerq {
 
 constexpr int kChunkWaveRows = 32;      // query rows of a wavefront (a row: one query head of one new token)
 constexpr int kChunkSplitMost = 256;    // most ranges the keys of a row are split into
-constexpr int kChunkGroups = 512;       // work-groups that the chip holds at once (two a compute unit): what splitting aims at
+constexpr int kChunkListMost = 256;     // most sequences of a batch whose work is shared out by their lengths
+constexpr int kChunkListItems = 1024;   // work-groups that such a launch aims at (two rounds)
+constexpr int kChunkTableBytes = 2 * kChunkListMost * (int)sizeof(int);   // first slot and splits of every sequence, at the workspace's start
 
 struct ChunkForm {
   int row_waves;                        // wavefronts of a work-group that share a tile of keys, each with its own 32 rows
   int token_waves;                      // wavefronts of a work-group with tiles of their own (and the same rows)
   int tile;                             // tokens of a tile
+  int round;                            // work-groups that the chip holds at once
+  int rows() const { return row_waves * kChunkWaveRows; }
 };
-// Few rows: a wavefront has all of them, and four of a work-group share the keys; else four wavefronts of 32 rows share a tile.
-inline ChunkForm chunk_form(long long rows) { return rows <= kChunkWaveRows ? ChunkForm{1, 4, 32} : rows <= 128 ? ChunkForm{4, 1, 64} : ChunkForm{8, 1, 64}; }
+// Few rows: a wavefront has all of them, and four of a work-group share the keys.  More: four or eight wavefronts share a tile, brought to
+// fp16 once for 128 or 256 rows.
+constexpr ChunkForm kFewRows = {1, 4, 32, 512}, kSomeRows = {4, 1, 64, 512}, kManyRows = {8, 1, 64, 256};
+inline ChunkForm chunk_form(long long rows) { return rows <= kChunkWaveRows ? kFewRows : rows <= 128 ? kSomeRows : kManyRows; }
 
 struct ChunkSizes {
   ChunkForm form;
   long long heads, rows, row_blocks;    // sequence-heads of the cache; rows of one; work-groups that they take
-  int split_most;                       // most splits of the workspace
-  size_t bytes;                         // of the workspace: (m, l) and 128 sums a row and split
+  int split_most;                       // most splits
 };
 inline ChunkSizes chunk_sizes(const innerq_config_t& c, long long t_new) {
   ChunkSizes s;
   s.heads = (long long)c.batch * c.n_kv_heads;
   s.rows = t_new * (c.n_q_heads / c.n_kv_heads);
   s.form = chunk_form(s.rows);
-  s.row_blocks = ceil_div(s.rows, (long long)s.form.row_waves * kChunkWaveRows);
+  s.row_blocks = ceil_div(s.rows, s.form.rows());
   // up to two rounds of work-groups
-  long long most = 2 * kChunkGroups / (s.heads * s.row_blocks);
+  long long most = 2 * s.form.round / (s.heads * s.row_blocks);
   const long long tiles = ceil_div((long long)c.capacity_tokens, s.form.tile) + 2;
   most = most > kChunkSplitMost ? kChunkSplitMost : most;
   most = most > tiles ? tiles : most;
   s.split_most = (int)(most < 1 ? 1 : most);
-  s.bytes = s.split_most == 1 ? 64 : (size_t)s.heads * s.rows * s.split_most * (kHeadDim + 2) * sizeof(float) + 64;
   return s;
 }
 
@@ -45,11 +49,35 @@ inline int chunk_splits(const ChunkSizes& s, long long tokens) {
   const long long tiles = ceil_div(tokens, (long long)s.form.tile * s.form.token_waves);
   long long best = 1, best_cost = -1;
   for (long long n = 1; n <= s.split_most && n <= tiles; ++n) {
-    const long long rounds = ceil_div(s.heads * s.row_blocks * n, kChunkGroups);
+    const long long rounds = ceil_div(s.heads * s.row_blocks * n, s.form.round);
     const long long cost = rounds * (ceil_div(tiles, n) + 3) + (n > 1 ? 2 : 0);
     if (best_cost < 0 || cost < best_cost) { best = n; best_cost = cost; }
   }
   return (int)best;
+}
+
+// A partial result of a work-group (a slot): level, sum and 128 sums of every row.
+inline size_t chunk_slot_bytes(const ChunkForm& f) { return (size_t)f.rows() * (kHeadDim + 2) * sizeof(float); }
+
+// A ragged batch of up to kChunkListMost sequences: work-groups find their work in a list made from the counts, one launch for the sequences of few
+// rows and one for those of more.  Most work-groups of either launch (none: 0).
+struct ChunkList { long long few, some; };
+inline ChunkList chunk_list(const innerq_config_t& c, long long t_new) {
+  const long long rows = t_new * (c.n_q_heads / c.n_kv_heads), heads = (long long)c.batch * c.n_kv_heads;
+  const long long blocks = heads * ceil_div(rows, kSomeRows.rows());
+  return {heads > kChunkListItems ? heads : kChunkListItems, rows <= kChunkWaveRows ? 0 : blocks > kChunkListItems ? blocks : kChunkListItems};
+}
+
+inline size_t chunk_workspace_bytes(const innerq_config_t& c, long long t_new) {
+  const ChunkSizes s = chunk_sizes(c, t_new);
+  size_t bytes = s.split_most == 1 ? 0 : (size_t)(s.heads * s.row_blocks * s.split_most) * chunk_slot_bytes(s.form);
+  if (c.batch <= kChunkListMost) {
+    // (work-groups beyond the items that were aimed at have no partial results: their sequences are not split)
+    const ChunkList l = chunk_list(c, t_new);
+    const size_t list = (size_t)kChunkListItems * (chunk_slot_bytes(kFewRows) + (l.some ? chunk_slot_bytes(kSomeRows) : 0));
+    bytes = list > bytes ? list : bytes;
+  }
+  return kChunkTableBytes + bytes;
 }
 
 }  // namespace innerq
