@@ -414,19 +414,20 @@ def make_rotation(cos, sin, interleaved: bool = False, pair_axis=None) -> Rotati
 def _rows(t, cfg: innerq_config_t, heads: int, tokens: int, dtype=None):
     """Pointer and strides of rows [B, H, T, d]."""
     import torch
-    assert t.is_cuda and t.dtype == (dtype or torch.float16) and tuple(t.shape) == (cfg.batch, heads, tokens, cfg.head_dim)
-    assert t.stride(3) == 1
-    # (a dimension of one has no stride to speak of)
-    return t.data_ptr(), C.byref(innerq_strides_t(*(t.stride(i) if t.shape[i] > 1 else 0 for i in range(3))))
+    shape, s = t.shape, t.stride()
+    assert t.is_cuda and t.dtype == (dtype or torch.float16) and shape == (cfg.batch, heads, tokens, cfg.head_dim) and s[3] == 1
+    if 1 in shape:                                         # (a dimension of one has no stride to speak of)
+        s = [x if n > 1 else 0 for x, n in zip(s, shape)]
+    return t.data_ptr(), C.byref(innerq_strides_t(s[0], s[1], s[2]))
 
 
 def _positions(positions, rotation: Optional[Rotation], cfg: innerq_config_t, tokens: int) -> Optional[int]:
     import torch
     if positions is None or rotation is None:
         return None
+    axes, shape = rotation.c.n_axes, positions.shape
     assert positions.is_cuda and positions.dtype == torch.int32 and positions.is_contiguous()
-    axes = rotation.c.n_axes
-    assert tuple(positions.shape) == (axes, cfg.batch, tokens) or (axes == 1 and tuple(positions.shape) == (cfg.batch, tokens))
+    assert shape == (axes, cfg.batch, tokens) or (axes == 1 and shape == (cfg.batch, tokens))
     return positions.data_ptr()
 
 
@@ -434,7 +435,7 @@ def _counts(t, cfg: innerq_config_t) -> Optional[int]:
     import torch
     if t is None:
         return None
-    assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == (cfg.batch,)
+    assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.shape == (cfg.batch,)
     return t.data_ptr()
 
 
@@ -445,10 +446,11 @@ def innerq_rotate(cfg: innerq_config_t, rotation: Rotation, x, out=None, positio
     import torch
     if out is None:
         out = torch.empty_like(x)
-    xp, xs = _rows(x, cfg, x.shape[1], x.shape[2])
-    yp, ys = _rows(out, cfg, x.shape[1], x.shape[2])
-    st = lib().innerq_rotate(C.byref(cfg), C.byref(rotation.c), _positions(positions, rotation, cfg, x.shape[2]), n_tokens,
-                             _counts(n_tokens_dev, cfg), _counts(t_new_dev, cfg), xp, xs, yp, ys, x.shape[1], x.shape[2], _stream(stream))
+    _, heads, T, _ = x.shape
+    xp, xs = _rows(x, cfg, heads, T)
+    yp, ys = _rows(out, cfg, heads, T)
+    st = lib().innerq_rotate(C.byref(cfg), C.byref(rotation.c), _positions(positions, rotation, cfg, T), n_tokens,
+                             _counts(n_tokens_dev, cfg), _counts(t_new_dev, cfg), xp, xs, yp, ys, heads, T, _stream(stream))
     if st != OK:
         raise InnerQError(st, "innerq_rotate")
     return out

@@ -182,16 +182,18 @@ __global__ void __launch_bounds__(256) append_step_kernel(AppendArgs a, int rows
   }
 }
 
-// Chunks and prompts, keys: a work-group takes 64 store rows of one sequence through a range of kv heads.  A thread holds the cosines and
-// sines of two units (of two tokens) in registers for all heads; rotated rows meet in LDS, where a lane finds a whole group
-// (a group's rotation partners are anywhere in the row).  Two buffers, one barrier a head; the next head's rows are on
-// their way while this one is quantised.  Groups of 64: two heads a turn, so that every lane has a group.
-constexpr int kTileRows = 64;
+// Chunks and prompts, keys: a work-group takes 32 store rows of one sequence through a range of kv heads, two at a turn (groups of 64:
+// four), so that every lane has a group.  A thread holds the cosines and sines of one unit of one token in registers for all heads; rotated
+// rows meet in LDS, where a lane finds a whole group (a group's rotation partners are anywhere in the row): two buffers and one barrier a
+// turn, or (groups of 64, whose rows would leave room for two work-groups a compute unit) one buffer and two.
+constexpr int kTileRows = 32;
 constexpr int kTilePitch = kHeadDim + 8;                 // halfs: rows 16 bytes apart in the banks
+template <int G>
+using KeyTile = __half[G == 32 ? 2 : 1][G / 16][kTileRows][kTilePitch];
 
 template <int G, int BITS, bool FAST>
-__device__ __forceinline__ void append_keys(const AppendArgs& a, const QuantTensorJob& j, __half (*tile)[G / 32][kTileRows][kTilePitch], int tiles, int head_blocks, int heads) {
-  constexpr int HS = G / 32;                             // heads a turn
+__device__ __forceinline__ void append_keys(const AppendArgs& a, const QuantTensorJob& j, KeyTile<G>& tile, int tiles, int head_blocks, int heads) {
+  constexpr int HS = G / 16;                             // heads a turn
   const uint32_t bt = blockIdx.x / (uint32_t)head_blocks, hb = blockIdx.x - bt * (uint32_t)head_blocks;
   const int b = (int)(bt / (uint32_t)tiles), tl = (int)(bt - (uint32_t)b * (uint32_t)tiles);
   if (b >= a.q.batch) return;
@@ -199,56 +201,42 @@ __device__ __forceinline__ void append_keys(const AppendArgs& a, const QuantTens
   const int r0 = rows_of(a, kPerToken, s.n) + tl * kTileRows, r1 = rows_of(a, kPerToken, s.to);
   if (r0 >= r1) return;                                  // (uniform)
   const int h0 = (int)hb * heads, h1 = h0 + heads < a.q.n_kv_heads ? h0 + heads : a.q.n_kv_heads;
-  const int tid = (int)threadIdx.x;
-  Turn turn[2];
-  int item_row[2], item_i[2];                            // row of the tile; index among the new tokens, negative: in the ring
-  UnitChunks ch[2];
-  const int u = tid % kUnits;
-#pragma unroll
-  for (int m = 0; m < 2; ++m) {
-    item_row[m] = tid / kUnits + m * (kTileRows / 2);
-    const int row = r0 + item_row[m] < r1 ? r0 + item_row[m] : r1 - 1;
-    item_i[m] = a.q.w_sink + row - s.n;
-    ch[m] = {16 * u, 16 * u + 8};
-    if (a.rot.cos) ch[m] = unit_chunks(a.rot, u);
-    if (a.rot.cos && item_i[m] >= 0) load_turn(turn[m], a.rot, (long long)b * a.t_new + item_i[m], s.n + item_i[m], u);
+  const int tid = (int)threadIdx.x, u = tid % kUnits, row = tid / kUnits;
+  // (behind the last row: that one again, and nothing comes of it)
+  const int i = a.q.w_sink + (r0 + row < r1 ? r0 + row : r1 - 1) - s.n;      // index among the new tokens; negative: in the ring
+  Turn turn;
+  UnitChunks ch = {16 * u, 16 * u + 8};
+  if (a.rot.cos) {
+    ch = unit_chunks(a.rot, u);
+    if (i >= 0) load_turn(turn, a.rot, (long long)b * a.t_new + i, s.n + i, u);
   }
-  uint4 p[HS][2], q[HS][2];
-  auto load = [&](int h) {
+  const __half* src = i >= 0 ? a.k.p + b * a.k.batch + i * a.k.token : j.ring + ((long long)b * a.q.n_kv_heads * j.slots + mod32(s.n + i, j.slots)) * kHeadDim;
+  const long long head = i >= 0 ? a.k.head : (long long)j.slots * kHeadDim;
+  int buf = 0;
+  for (int h = h0; h < h1; h += HS) {
+    uint4 p[HS], q[HS];
 #pragma unroll
     for (int x = 0; x < HS; ++x) {
-      const int hh = h + x < h1 ? h + x : h1 - 1;
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        const __half* src = item_i[m] >= 0 ? a.k.p + b * a.k.batch + hh * a.k.head + item_i[m] * a.k.token
-                                           : j.ring + (((long long)b * a.q.n_kv_heads + hh) * j.slots + mod32(s.n + item_i[m], j.slots)) * kHeadDim;
-        p[x][m] = *reinterpret_cast<const uint4*>(src + ch[m].a);
-        q[x][m] = *reinterpret_cast<const uint4*>(src + ch[m].b);
-      }
+      const __half* at = src + (h + x < h1 ? h + x : h1 - 1) * head;
+      p[x] = *reinterpret_cast<const uint4*>(at + ch.a);
+      q[x] = *reinterpret_cast<const uint4*>(at + ch.b);
     }
-  };
-  load(h0);
-  int buf = 0;
-  for (int h = h0; h < h1; h += HS, buf ^= 1) {
 #pragma unroll
-    for (int x = 0; x < HS; ++x)
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        const int hh = h + x < h1 ? h + x : h1 - 1;
-        if (item_i[m] >= 0) finish_key_unit(a, turn[m], hh, u, ch[m], p[x][m], q[x][m]);
-        __half* row = tile[buf][x][item_row[m]];
-        *reinterpret_cast<uint4*>(row + ch[m].a) = p[x][m];
-        *reinterpret_cast<uint4*>(row + ch[m].b) = q[x][m];
-      }
-    if (h + HS < h1) load(h + HS);
+    for (int x = 0; x < HS; ++x) {
+      if (i >= 0) finish_key_unit(a, turn, h + x < h1 ? h + x : h1 - 1, u, ch, p[x], q[x]);
+      *reinterpret_cast<uint4*>(tile[buf][x][row] + ch.a) = p[x];
+      *reinterpret_cast<uint4*>(tile[buf][x][row] + ch.b) = q[x];
+    }
     __syncthreads();
     constexpr int GPR = kHeadDim / G;
-    const int x = tid / (kTileRows * GPR), row = tid / GPR % kTileRows, g = tid % GPR;
-    if (h + x < h1 && r0 + row < r1) {
+    const int x = tid / (kTileRows * GPR), r = tid / GPR % kTileRows, g = tid % GPR;
+    if (h + x < h1 && r0 + r < r1) {
       const long long bh = (long long)b * a.q.n_kv_heads + h + x;
-      per_token_group<G, BITS, FAST>(a.q, j, tile[buf][x][row] + g * G, false, (uint32_t)bh, (uint32_t)g,
-                                     store_row(a.q.pages, a.q.n_kv_heads, a.q.capacity, bh, r0 + row), 0u);
+      per_token_group<G, BITS, FAST>(a.q, j, tile[buf][x][r] + g * G, false, (uint32_t)bh, (uint32_t)g,
+                                     store_row(a.q.pages, a.q.n_kv_heads, a.q.capacity, bh, r0 + r), 0u);
     }
+    if (G == 32) buf ^= 1;
+    else __syncthreads();
   }
 }
 
@@ -300,8 +288,8 @@ struct ChunkPlan {
   int per_seq;                         // window copies a sequence (0: in a launch of their own)
 };
 template <int G, bool FAST>
-__global__ void __launch_bounds__(256) append_chunk_kernel(AppendArgs a, ChunkPlan plan) {
-  __shared__ __align__(16) __half tile[2][G / 32][kTileRows][kTilePitch];
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(G == 32 ? 5 : 3))) append_chunk_kernel(AppendArgs a, ChunkPlan plan) {
+  __shared__ __align__(16) KeyTile<G> tile;
   const int y = (int)blockIdx.y;
   const QuantTensorJob j = pick_job(a.q, y & 1);
   if (y >= 2) {
@@ -359,7 +347,7 @@ hipError_t launch_append(const AppendArgs& a, hipStream_t stream) {
     // as many heads a work-group as leave four work-groups a compute unit
     long long heads = B * p.tiles * H / (4LL * compute_units());
     heads = heads < 1 ? 1 : heads > H ? H : heads;
-    if (G == 64 && heads % 2) ++heads;
+    heads = div_up(heads, G / 16) * (G / 16);             // (whole turns)
     p.heads = (int)heads;
     p.head_blocks = (int)div_up(H, heads);
     p.groups = (int)(groups ? groups : 1);
