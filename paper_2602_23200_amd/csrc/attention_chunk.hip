@@ -89,13 +89,14 @@ struct Masks {
 
 template <int BITS>
 struct Decoder {
-  half2_t s, z;
+  half2_t s, z;                                          // (the low half, which an operand's selection brings to both)
   half2_t off[5];                                        // -(1024 + o), -(256 + o), -(64 + o), -(16 + o), -(4 + o), o = 2^(b-1) if symmetric
   __device__ __forceinline__ void start(uint32_t scale, uint32_t zero) {
     const bool asym = (scale & 0x8000u) != 0u;
-    const uint32_t a = scale & 0x7fffu, b = asym ? zero : 0u;
-    s = as_half2(a | a << 16);
-    z = as_half2(b | b << 16);
+    uint32_t a = scale & 0x7fffu, b = asym ? zero : 0u;
+    asm("" : "+v"(a), "+v"(b));                          // (whole words: their halves taken apart, the loads they come from go through memory)
+    s = as_half2(a);
+    z = as_half2(b);
     constexpr float H = (float)(1 << (BITS - 1));
 #pragma unroll
     for (int i = 0; i < 5; ++i) {
@@ -110,7 +111,7 @@ struct Decoder {
     constexpr uint32_t base = ((25u - AT) << 10) * 0x10001u;
     uint32_t raw = (x & m.at[BITS == 4 ? AT / 4 : AT / 2]) | base;
     if constexpr (BITS == 3) raw = (high & m.high[AT / 2]) | raw;
-    return as_u32(__builtin_elementwise_fma(as_half2(raw) + off[AT / 2], s, z));
+    return as_u32(__builtin_elementwise_fma(as_half2(raw) + off[AT / 2], half2_t{s.x, s.x}, half2_t{z.x, z.x}));
   }
 };
 
@@ -529,14 +530,12 @@ struct ChunkKernel {
   }
   // Words of the fields that the lane's half needs, brought to the places of half 0, so that one code serves both.
   static __device__ __forceinline__ void own_half(const uint32_t (&w)[VB], int half, uint32_t (&out)[VB]) {
-    if constexpr (VB == 4) {
+    constexpr int N = VB == 3 ? 2 : VB;
+    uint32_t by = half ? (VB == 4 ? 16u : 8u) : 0u;
+    asm("" : "+v"(by));                                  // (known, it becomes a load at another byte of what is put into memory first)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) out[i] = half ? w[i] >> 16 : w[i];
-    } else {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) out[i] = half ? w[i] >> 8 : w[i];
-      if constexpr (VB == 3) out[2] = half ? w[2] >> 4 : w[2];
-    }
+    for (int i = 0; i < N; ++i) out[i] = w[i] >> by;
+    if constexpr (VB == 3) out[2] = w[2] >> (by / 2);
   }
   static __device__ __forceinline__ void direct_tile(const ChunkArgs& a, const FieldMasks& f, Direct& x, Rows& r, int lane, float scale, long long next, int next_row0) {
     float16_t s[NB];
@@ -929,68 +928,84 @@ hipError_t launch_group(const ChunkArgs& a, int kb, int vb, const ChunkForm& for
 }
 
 #if INNERQ_CHUNK_G == 32
-// The splits of a row joined: a wavefront a row, a lane per two channels.  slot_rows: rows of a slot.
-__global__ void __launch_bounds__(256) chunk_merge_kernel(ChunkArgs a, long long rows_all, int slot_rows) {
-  const long long at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+// The splits of a row joined: a wavefront takes four rows of a head, a lane two channels of each; levels and sums come sixteen splits of the
+// four rows a load.  slot_rows: rows of a slot.
+constexpr int kMergeRows = 4;
+__global__ void __launch_bounds__(256) chunk_merge_kernel(ChunkArgs a, int blocks, int slot_rows) {
   const int lane = (int)threadIdx.x & 63;
-  if (at >= rows_all) return;
   const int rows = a.t_new * a.heads_per_kv;
-  const long long bh = at / rows;
-  const int row = (int)(at - bh * rows), b = (int)(bh / a.n_kv_heads), h = (int)(bh - (long long)b * a.n_kv_heads);
-  const int i = row / a.heads_per_kv;
+  const long long bh = blockIdx.x / (unsigned)blocks;
+  const int row0 = ((int)(blockIdx.x % (unsigned)blocks) * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6)) * kMergeRows;
+  const int b = (int)(bh / a.n_kv_heads), h = (int)(bh - (long long)b * a.n_kv_heads);
+  const int own = a.t_dev ? chunk_seq(a, b, 32).t * a.heads_per_kv : rows;       // (the group does not matter)
+  if (row0 >= own) return;
   int n_splits = a.n_splits;
   const float* ws = a.ws;
   long long slots = a.slots, slot;
   if (a.table) {
-    const int own = chunk_seq(a, b, 32).t * a.heads_per_kv;       // (the group does not matter)
-    if (row >= own) return;
     n_splits = a.table[2 * b + 1];
     if (n_splits == 1) return;                           // (written already)
     const bool few = own <= kChunkWaveRows;
     slot_rows = few ? kFewRows.row_waves * kChunkWaveRows : kSomeRows.row_waves * kChunkWaveRows;
     if (few) ws = a.ws_few;
     slots = kChunkListItems;
-    slot = a.table[2 * b] + (long long)(h * ((own + slot_rows - 1) / slot_rows) + row / slot_rows) * n_splits;
+    slot = a.table[2 * b] + (long long)(h * ((own + slot_rows - 1) / slot_rows) + row0 / slot_rows) * n_splits;
   } else {
-    if (a.t_dev && i >= a.t_dev[b]) return;
-    slot = (bh * a.row_blocks + row / slot_rows) * n_splits;
+    slot = (bh * a.row_blocks + row0 / slot_rows) * n_splits;
   }
-  const long long slot_row = slot * slot_rows + row % slot_rows;
+  // (slots have a multiple of four rows, those behind the last one as well: what stands there goes nowhere)
+  const long long slot_row = slot * slot_rows + row0 % slot_rows;
   const float* ml = ws + slot_row * 2;
   const float* po = ws + slots * slot_rows * 2 + slot_row * D + 2 * lane;
-  const int step_ml = slot_rows * 2, step_o = slot_rows * D;
-  float top = -INFINITY;
-  for (int p = lane; p < n_splits; p += 64) top = fmaxf(top, ml[p * step_ml]);
+  const long long step_ml = slot_rows * 2, step_o = (long long)slot_rows * D;
+  const int r = lane >> 4, p16 = lane & 15;              // the lane's row and split of what is loaded sixteen at a time
+  auto state = [&](int p) {
+    float2 s = {-INFINITY, 0.f};
+    if (p < n_splits && row0 + r < own) s = *reinterpret_cast<const float2*>(ml + p * step_ml + r * 2);
+    return s;
+  };
+  const float2 first = state(p16);
+  float top = first.x;
+  for (int p = p16 + 16; p < n_splits; p += 16) top = fmaxf(top, state(p).x);
 #pragma unroll
-  for (int x = 32; x > 0; x /= 2) top = fmaxf(top, __shfl_xor(top, x));
-  float den = 0.f, n0 = 0.f, n1 = 0.f;
-  for (int p0 = 0; p0 < n_splits; p0 += 64) {
-    float f = 0.f, l = 0.f;
-    if (p0 + lane < n_splits) {
-      const float2 s = *reinterpret_cast<const float2*>(ml + (p0 + lane) * step_ml);
-      f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - top);
-      l = s.y;
-    }
-    den += f * l;
-    const int n = n_splits - p0 < 64 ? n_splits - p0 : 64;
-    for (int p = 0; p < n; p += 8) {                     // (eight partial results under way)
-      float2 o[8];
+  for (int x = 8; x > 0; x /= 2) top = fmaxf(top, __shfl_xor(top, x));
+  float den = 0.f;
+  float2 n[kMergeRows] = {};
+  for (int p0 = 0; p0 < n_splits; p0 += 16) {
+    const float2 s = p0 == 0 ? first : state(p0 + p16);
+    const float f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - top);
+    den = __builtin_fmaf(f, s.y, den);
+    const int count = n_splits - p0 < 16 ? n_splits - p0 : 16;
+    for (int p = 0; p < count; p += 4) {                 // (sixteen partial results under way)
+      float2 o[4][kMergeRows];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = *reinterpret_cast<const float2*>(po + (long long)(p0 + (p + e < n ? p + e : n - 1)) * step_o);
+      for (int e = 0; e < 4; ++e)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float w = p + e < n ? __shfl(f, p + e) : 0.f;
-        n0 = __builtin_fmaf(w, o[e].x, n0);
-        n1 = __builtin_fmaf(w, o[e].y, n1);
-      }
+        for (int i = 0; i < kMergeRows; ++i) o[e][i] = *reinterpret_cast<const float2*>(po + (p0 + (p + e < count ? p + e : count - 1)) * step_o + i * D);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int i = 0; i < kMergeRows; ++i) {
+          const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), 16 * i + ((p + e) & 15)));
+          if (p + e < count && row0 + i < own) {
+            n[i].x = __builtin_fmaf(w, o[e][i].x, n[i].x);
+            n[i].y = __builtin_fmaf(w, o[e][i].y, n[i].y);
+          }
+        }
     }
   }
 #pragma unroll
-  for (int x = 32; x > 0; x /= 2) den += __shfl_xor(den, x);
-  const float inv = 1.0f / den;
-  const long long dst = b * a.out_batch + (h * a.heads_per_kv + row - i * a.heads_per_kv) * a.out_head + i * a.out_token + 2 * lane;
-  if (a.out_is_fp32) *reinterpret_cast<float2*>(static_cast<float*>(a.out) + dst) = float2{n0 * inv, n1 * inv};
-  else *reinterpret_cast<half2_t*>(static_cast<_Float16*>(a.out) + dst) = half2_t{(_Float16)(n0 * inv), (_Float16)(n1 * inv)};
+  for (int x = 8; x > 0; x /= 2) den += __shfl_xor(den, x);
+#pragma unroll
+  for (int i = 0; i < kMergeRows; ++i) {
+    const int row = row0 + i;
+    if (row >= own) return;
+    const float inv = 1.0f / __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(den), 16 * i));
+    const int token = row / a.heads_per_kv;
+    const long long dst = b * a.out_batch + (h * a.heads_per_kv + row - token * a.heads_per_kv) * a.out_head + token * a.out_token + 2 * lane;
+    if (a.out_is_fp32) *reinterpret_cast<float2*>(static_cast<float*>(a.out) + dst) = float2{n[i].x * inv, n[i].y * inv};
+    else *reinterpret_cast<half2_t*>(static_cast<_Float16*>(a.out) + dst) = half2_t{(_Float16)(n[i].x * inv), (_Float16)(n[i].y * inv)};
+  }
 }
 #endif
 
@@ -999,8 +1014,9 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(ChunkArgs a, long long
 #if INNERQ_CHUNK_G == 32
 hipError_t launch_chunk_g32(const ChunkArgs& a, int kb, int vb, const ChunkForm& form, hipStream_t stream) { return launch_group<32>(a, kb, vb, form, stream); }
 hipError_t launch_chunk_merge(const ChunkArgs& a, const ChunkForm& form, hipStream_t stream) {
-  const long long rows = (long long)a.batch * a.n_kv_heads * a.t_new * a.heads_per_kv;
-  chunk_merge_kernel<<<(unsigned)ceil_div(rows, 4), 256, 0, stream>>>(a, rows, form.rows());
+  const long long blocks = ceil_div((long long)a.t_new * a.heads_per_kv, 4 * kMergeRows), all = (long long)a.batch * a.n_kv_heads * blocks;
+  if (all >= (1LL << 31)) return hipErrorInvalidValue;
+  chunk_merge_kernel<<<(unsigned)all, 256, 0, stream>>>(a, (int)blocks, form.rows());
   return hipGetLastError();
 }
 #else
