@@ -199,6 +199,14 @@ struct PieceAt {
   }
 };
 
+// First store row of a tile (uniform: row0, and so the page, are the same for a wavefront).
+__device__ __forceinline__ long long tile_row(const ChunkArgs& a, int b, int h, int row0) {
+  if (!a.pages.table) return ((long long)b * a.n_kv_heads + h) * a.capacity + row0;
+  int page = __builtin_amdgcn_readfirstlane(a.pages.table[(long long)b * a.pages.tiles_per_seq + (row0 >> 6)]);
+  page = page < 0 ? 0 : page >= a.pages.pool_pages ? a.pages.pool_pages - 1 : page;
+  return ((long long)page * a.n_kv_heads + h) * kPageTokens + (row0 & 63);
+}
+
 template <int KB, int VB, int G, int RW, int TW>
 struct ChunkKernel {
   static constexpr int KT = RW == 1 ? 32 : 64;           // tokens of a tile
@@ -220,8 +228,8 @@ struct ChunkKernel {
 
   // Store rows row0 .. (a multiple of the tile, so one page holds them): pieces in registers.  Behind the last packed row: the
   // same rows again, whose scores are masked.
-  static __device__ __forceinline__ void load_packed(const ChunkArgs& a, const ChunkSeq& s, long long bh, int row0, int tid, bool values, Packed& x) {
-    const long long lin = store_row(a.pages, a.n_kv_heads, a.capacity, bh, row0);
+  static __device__ __forceinline__ void load_packed(const ChunkArgs& a, const ChunkSeq& s, int b, int h, int row0, int tid, bool values, Packed& x) {
+    const long long lin = tile_row(a, b, h, row0);
     const bool whole = KT == 32 || s.packed_v - row0 >= KT;
     if constexpr (ONE) {
       const int p = tid % (NT / 2);
@@ -537,15 +545,14 @@ struct ChunkKernel {
     for (int i = 0; i < N; ++i) out[i] = w[i] >> by;
     if constexpr (VB == 3) out[2] = w[2] >> (by / 2);
   }
-  static __device__ __forceinline__ void direct_tile(const ChunkArgs& a, const FieldMasks& f, Direct& x, Rows& r, int lane, float scale, long long next, int next_row0) {
-    float16_t s[NB];
+  // One tile: the scores of the one behind it (from `ahead`) are on their way while its own become weights.
+  static __device__ __forceinline__ void direct_keys(const FieldMasks& f, const Direct& x, const Rows& r, float16_t (&s)[NB]) {
     s[0] = float16_t{};
-    Decoder<KB> dk;
-    direct_scores<0>(f, x, r, dk, s[0]);
-    __builtin_amdgcn_sched_barrier(0);
-    direct_scores<1>(f, x, r, dk, s[0]);
-    load_direct_keys(a, next, lane, x);
-    __builtin_amdgcn_sched_barrier(0);
+    Decoder<KB> d;
+    direct_scores<0>(f, x, r, d, s[0]);
+    direct_scores<1>(f, x, r, d, s[0]);
+  }
+  static __device__ __forceinline__ void direct_values(const FieldMasks& f, const Direct& x, Rows& r, float16_t (&s)[NB], int lane, float scale) {
     half8_t p[2 * NB];
     weights(r, s, lane >> 5, false, 0, scale, p);
 #pragma unroll
@@ -556,9 +563,7 @@ struct ChunkKernel {
       own_half(x.v[n], lane >> 5, w);
       r.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, decode_part<VB, 0, 0>(f.v, d, w)), p[0], r.o[n], 0, 0, 0);
       r.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, decode_part<VB, 1, 0>(f.v, d, w)), p[1], r.o[n], 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);                 // (decoded early, the operands do not fit the registers)
     }
-    load_direct_values(a, next, next_row0, lane, x);
   }
 
   static __device__ __forceinline__ void load_queries(const ChunkArgs& a, int b, int h, int row, bool live, int half, Rows& r) {
@@ -814,24 +819,34 @@ __global__ void __launch_bounds__(64 * RW * TW) __attribute__((amdgpu_waves_per_
   if constexpr (RW == 1) {
     const int u0 = from(0), u1 = to(0, tiles1);
     auto row = [&](int u) { return (u < u1 ? u : u1 - 1) * C::KT; };
-    auto place = [&](int row0) { return store_row(a.pages, a.n_kv_heads, a.capacity, bh, row0); };
+    auto place = [&](int row0) { return tile_row(a, b, h, row0); };
     if (u0 < u1) {
-      // two tiles under way: a tile's registers are loaded again as soon as they have been used
+      // Two tiles under way, their registers loaded again as soon as they have been used; the scores of the next tile are formed in front of
+      // the present one's weights, so that nothing waits for a product (behind the last tile: its own once more).
       typename C::Direct x, y;
+      float16_t sx[C::NB], sy[C::NB];
       C::load_direct_keys(a, place(row(u0)), lane, x);
       C::load_direct_values(a, place(row(u0)), row(u0), lane, x);
       C::load_direct_keys(a, place(row(u0 + 1)), lane, y);
       C::load_direct_values(a, place(row(u0 + 1)), row(u0 + 1), lane, y);
+      C::direct_keys(masks, x, r, sx);
+      C::load_direct_keys(a, place(row(u0 + 2)), lane, x);
       for (int u = u0;;) {
-        C::direct_tile(a, masks, x, r, lane, scale, place(row(u + 2)), row(u + 2));
+        C::direct_keys(masks, y, r, sy);
+        C::load_direct_keys(a, place(row(u + 3)), lane, y);
+        C::direct_values(masks, x, r, sx, lane, scale);
+        C::load_direct_values(a, place(row(u + 2)), row(u + 2), lane, x);
         if (++u == u1) break;
-        C::direct_tile(a, masks, y, r, lane, scale, place(row(u + 2)), row(u + 2));
+        C::direct_keys(masks, x, r, sx);
+        C::load_direct_keys(a, place(row(u + 3)), lane, x);
+        C::direct_values(masks, y, r, sy, lane, scale);
+        C::load_direct_values(a, place(row(u + 2)), row(u + 2), lane, y);
         if (++u == u1) break;
       }
     }
   } else {
     pass_tiles<C, typename C::Packed>(from(0), to(0, tiles1), has_rows ? tiles1 : 0, mine, r, lane, scale,
-        [&](int u, typename C::Packed& x) { C::load_packed(a, s, bh, u * C::KT, tid, values, x); }, put_packed,
+        [&](int u, typename C::Packed& x) { C::load_packed(a, s, b, h, u * C::KT, tid, values, x); }, put_packed,
         [&](int u) { return TileMask{s.packed_v - u * C::KT < C::KT, s.packed_v - u * C::KT - 1}; });
   }
   pass_tiles<C, typename C::Plain>(from(tiles1), to(tiles1, tiles2), has_rows ? tiles2 : 0, mine, r, lane, scale,
