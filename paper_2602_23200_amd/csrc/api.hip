@@ -726,7 +726,7 @@ int chunk_attention(const innerq_config_t* cfg, const innerq_cache_t* cache, con
   if (!workspace) return INNERQ_E_NULL;
   if (misaligned(workspace) || (q_scale && misaligned(q_scale))) return INNERQ_E_ALIGN;
   if (!chunk_rows_fit(c, t_new)) return INNERQ_E_UNSUPPORTED;
-  const ChunkSizes sizes = chunk_sizes(c, t_new);
+  const ChunkSizes sizes = chunk_sizes(c, t_new, tokens - t_new);
   if (workspace_bytes < chunk_workspace_bytes(c, t_new)) return INNERQ_E_WORKSPACE;
   ChunkArgs a;
   a.k = chunk_tensor(c, *cache, 0, k_new, *k_strides);

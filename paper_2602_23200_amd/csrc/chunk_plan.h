@@ -20,20 +20,25 @@ struct ChunkForm {
   int rows() const { return row_waves * kChunkWaveRows; }
 };
 // Few rows: a wavefront has all of them, and four of a work-group share the keys.  More: four or eight wavefronts share a tile, brought to
-// fp16 once for 128 or 256 rows.
+// fp16 once for 128 or 256 rows.  Eight are the faster where most keys are packed (us, four and eight, 32 / 8 heads, 4 bits: 2048 new tokens
+// over 32k 1396, 1226; over 8k 446, 405; 512 over 16k 208, 188; 256 over 16k 120, 112), four among new tokens, where a work-group's rows
+// end at different ones and two work-groups a compute unit fill each other's gaps (2048 over none 72, 97; over 2048 165, 177; 4096 of 32
+// heads over none 200, 215; over 4096 586, 562).
 constexpr ChunkForm kFewRows = {1, 4, 32, 512}, kSomeRows = {4, 1, 64, 512}, kManyRows = {8, 1, 64, 256};
-inline ChunkForm chunk_form(long long rows) { return rows <= kChunkWaveRows ? kFewRows : rows <= 128 ? kSomeRows : kManyRows; }
+inline ChunkForm chunk_form(long long rows, long long t_new, long long cached) {
+  return rows <= kChunkWaveRows ? kFewRows : rows <= 128 || cached < 2 * t_new ? kSomeRows : kManyRows;
+}
 
 struct ChunkSizes {
   ChunkForm form;
   long long heads, rows, row_blocks;    // sequence-heads of the cache; rows of one; work-groups that they take
   int split_most;                       // most splits
 };
-inline ChunkSizes chunk_sizes(const innerq_config_t& c, long long t_new) {
+inline ChunkSizes chunk_sizes(const innerq_config_t& c, long long t_new, long long cached) {
   ChunkSizes s;
   s.heads = (long long)c.batch * c.n_kv_heads;
   s.rows = t_new * (c.n_q_heads / c.n_kv_heads);
-  s.form = chunk_form(s.rows);
+  s.form = chunk_form(s.rows, t_new, cached);
   s.row_blocks = ceil_div(s.rows, s.form.rows());
   // up to two rounds of work-groups
   long long most = 2 * s.form.round / (s.heads * s.row_blocks);
@@ -69,8 +74,12 @@ inline ChunkList chunk_list(const innerq_config_t& c, long long t_new) {
 }
 
 inline size_t chunk_workspace_bytes(const innerq_config_t& c, long long t_new) {
-  const ChunkSizes s = chunk_sizes(c, t_new);
-  size_t bytes = s.split_most == 1 ? 0 : (size_t)(s.heads * s.row_blocks * s.split_most) * chunk_slot_bytes(s.form);
+  size_t bytes = 0;
+  for (const long long cached : {0LL, 2 * t_new}) {      // (either form of that many rows)
+    const ChunkSizes s = chunk_sizes(c, t_new, cached);
+    const size_t need = s.split_most == 1 ? 0 : (size_t)(s.heads * s.row_blocks * s.split_most) * chunk_slot_bytes(s.form);
+    bytes = need > bytes ? need : bytes;
+  }
   if (c.batch <= kChunkListMost) {
     // (work-groups beyond the items that were aimed at have no partial results: their sequences are not split)
     const ChunkList l = chunk_list(c, t_new);
