@@ -75,7 +75,8 @@ inline ChunkList chunk_list(const innerq_config_t& c, long long t_new) {
 
 inline size_t chunk_workspace_bytes(const innerq_config_t& c, long long t_new) {
   size_t bytes = 0;
-  for (const long long cached : {0LL, 2 * t_new}) {      // (either form of that many rows)
+  const long long either[2] = {0, 2 * t_new};            // (either form of that many rows)
+  for (const long long cached : either) {
     const ChunkSizes s = chunk_sizes(c, t_new, cached);
     const size_t need = s.split_most == 1 ? 0 : (size_t)(s.heads * s.row_blocks * s.split_most) * chunk_slot_bytes(s.form);
     bytes = need > bytes ? need : bytes;

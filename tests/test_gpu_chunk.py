@@ -281,3 +281,121 @@ def test_recorded_and_replayed_with_appends(env):
         assert torch.equal(sides[0]["out"], sides[1]["out"])
     for name, b in sides[0]["cache"].buffers.items():
         assert b is None or torch.equal(b, sides[1]["cache"].buffers[name]), name
+
+
+def test_what_no_token_wrote_is_not_read(env):
+    """Every byte of the cache is a NaN's before the tokens come: rows behind the last one, free ring slots and unused sinks stay out."""
+    torch, iq = env
+    rng = np.random.default_rng(21)
+    for bits, group, lengths in ((2, 32, [0, 2, 100, 517]), (4, 64, [3, 60, 250, 700]), (3, 32, [1, 84, 85, 116])):
+        w = small(batch=4, n_q_heads=4, n_kv_heads=2, bits=bits, group=group)
+        o = oracle_config(w, capacity=768)
+        o1 = replace(o, batch=1)
+        cache = iq.allocate_cache(gpu_config(o))
+        for x in cache.buffers.values():
+            if x is not None:
+                x.fill_(255)
+        T = max(lengths)
+        _, _, K, V = projection(torch, rng, 4, T, 1, 2)
+        counts = torch.zeros(4, dtype=torch.int32, device="cuda")
+        iq.innerq_append_rotated_ragged(cache, counts, torch.tensor(lengths, dtype=torch.int32, device="cuda"), K, V)
+        refs = []
+        for b, n in enumerate(lengths):
+            refs.append(orc.cache_new(o1))
+            if n:
+                orc.quantize_append(o1, refs[b], K[b:b + 1, :, :n].cpu().numpy(), V[b:b + 1, :, :n].cpu().numpy())
+        for t in (1, 40):
+            _, q, k, v = projection(torch, rng, 4, t, 4, 2)
+            ts = torch.full((4,), t, dtype=torch.int32, device="cuda")
+            out = iq.innerq_chunk_attention_ragged(cache, counts, ts, 768, k, v, q, iq.allocate_chunk_workspace(cache.cfg, t))
+            check(torch, o1, refs, lengths, [t] * 4, q, k, v, out, False)
+
+
+@pytest.mark.parametrize("batch", [256, 257])
+def test_many_sequences(env, batch):
+    """As many sequences as a list holds, and one more (whose launch is planned without it)."""
+    torch, iq = env
+    rng = np.random.default_rng(batch)
+    w = small(batch=batch, n_q_heads=2, n_kv_heads=1, bits=4)
+    o = oracle_config(w, capacity=256)
+    lengths = [int(x) for x in rng.integers(0, 200, batch)]
+    ts = [int(x) for x in rng.integers(0, 41, batch)]
+    cache, o1, refs, counts = filled(torch, iq, o, lengths, rng)
+    T = max(ts)
+    _, q, k, v = projection(torch, rng, batch, T, 2, 1)
+    out = torch.full((batch, T, 2, 128), 9.0, dtype=torch.float16, device="cuda").transpose(1, 2)
+    iq.innerq_chunk_attention_ragged(cache, counts, torch.tensor(ts, dtype=torch.int32, device="cuda"), 256, k, v, q,
+                                     iq.allocate_chunk_workspace(cache.cfg, T), out=out)
+    check(torch, o1, refs, lengths, ts, q, k, v, out, True)
+    for b, t in enumerate(ts):
+        assert (out[b, :, t:] == 9.0).all()
+
+
+def test_counts_outside_their_bounds_touch_nothing_else(env):
+    torch, iq = env
+    rng = np.random.default_rng(5)
+    w = small(batch=4, n_q_heads=4, n_kv_heads=1, bits=4)
+    o = oracle_config(w, capacity=256)
+    lengths, t = [100, 0, 30, 0], 12
+    cache, o1, refs, counts = filled(torch, iq, o, lengths, rng)
+    _, q, k, v = projection(torch, rng, 4, t, 4, 1)
+    bad = torch.tensor([100, -7, 30, 1 << 20], dtype=torch.int32, device="cuda")
+    ts = torch.tensor([12, 500, -3, 5], dtype=torch.int32, device="cuda")
+    out = torch.full((4, t, 4, 128), 3.0, device="cuda").transpose(1, 2)
+    iq.innerq_chunk_attention_ragged(cache, bad, ts, 256, k, v, q, iq.allocate_chunk_workspace(cache.cfg, t), out=out)
+    check(torch, o1, refs, lengths, [12, 0, 0, 0], q, k, v, out, False)
+    assert (out[2] == 3.0).all() and (out[3, :, 5:] == 3.0).all()
+
+
+def test_two_streams(env):
+    """Two calls at once, each with its own workspace: the bits of one after the other."""
+    torch, iq = env
+    rng = np.random.default_rng(6)
+    w = small(batch=2, n_q_heads=8, n_kv_heads=2, bits=2)
+    o = oracle_config(w, capacity=4096)
+    cache = iq.allocate_cache(gpu_config(o))
+    _, _, K, V = projection(torch, rng, 2, 3000, 1, 2)
+    iq.innerq_append_rotated(cache, K, V)
+    jobs = []
+    for t in (5, 90):
+        _, q, k, v = projection(torch, rng, 2, t, 8, 2)
+        ws = iq.allocate_chunk_workspace(cache.cfg, t)
+        jobs.append((k, v, q, ws, iq.innerq_chunk_attention(cache, k, v, q, ws).clone()))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    for _ in range(5):
+        outs = [iq.innerq_chunk_attention(cache, k, v, q, ws, stream=s) for (k, v, q, ws, _), s in zip(jobs, streams)]
+        torch.cuda.synchronize()
+        for out, job in zip(outs, jobs):
+            assert torch.equal(out, job[4])
+
+
+def test_offsets_beyond_32_bits(env):
+    """Nine sequences of a million tokens on eight heads, 4.8 GB of packed keys: the last sequence by itself gives the same."""
+    torch, iq = env
+    n = (1 << 20) - 40
+    cfg = iq.make_config(9, 16, 8, 128, 4, 32, 4, 128, capacity_tokens=1 << 20)
+    cache = iq.allocate_cache(cfg)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    for name in ("k_codes", "v_codes"):
+        for part in cache.buffers[name].view(9, -1):
+            part.random_(0, 256, generator=gen)
+    for name in ("k_scales", "v_scales"):                   # (symmetric: 0.1 to 0.3)
+        x = cache.buffers[name].view(torch.float16).view(9, -1)
+        for part in x:
+            part.uniform_(0.1, 0.3, generator=gen)
+    for name in ("k_recent", "v_recent", "k_sink", "v_sink"):
+        cache.buffers[name].view(torch.float16).normal_(generator=gen)
+    one = iq.sequence_view(cache, 8)
+    cache.c.n_tokens = cache.c.store_ahead_tokens = one.c.n_tokens = one.c.store_ahead_tokens = n
+    rng = np.random.default_rng(2)
+    for t in (3, 20):
+        _, q, k, v = projection(torch, rng, 9, t, 16, 8)
+        out = iq.innerq_chunk_attention(cache, k, v, q, iq.allocate_chunk_workspace(cfg, t))
+        alone = iq.innerq_chunk_attention(one, k[8:], v[8:], q[8:], iq.allocate_chunk_workspace(one.cfg, t))
+        assert torch.isfinite(out).all()
+        # the same fp16 operands, the fp32 sums in another order: weights taken at another level are rounded anew (2^-11 each,
+        # independent), so means of values around 1 over a million tokens move by far less than 2^-11 of a value
+        assert (out[8] - alone[0]).abs().max() <= 2.0 ** -11
+        assert (out[8] - out[0]).abs().max() > 0

@@ -148,3 +148,20 @@ def test_another_stream_and_replays(env):
     iq.innerq_rotate(cfg, rot, x, out=out, n_tokens_dev=n, stream=side)
     side.synchronize()
     assert np.array_equal(out.cpu().numpy(), want)
+
+
+def test_offsets_beyond_32_bits(env):
+    """2.3 billion elements: rows at both ends against the formula."""
+    torch, iq = env
+    T, H = 375000, 48
+    x = torch.empty(1, T, H, 128, dtype=torch.float16, device="cuda")
+    for part in x[0].split(25000):
+        part.normal_()
+    cos, sin = rotation_tables(T, 128)
+    rot = iq.make_rotation(torch.from_numpy(cos).cuda(), torch.from_numpy(sin).cuda())
+    picks = np.array([0, 1, 187499, T - 2, T - 1])
+    before = x[:, picks].transpose(1, 2).cpu().numpy()
+    v = x.transpose(1, 2)
+    iq.innerq_rotate(config(iq, 1), rot, v, out=v)
+    got = x[:, picks].transpose(1, 2).cpu().numpy()
+    assert np.array_equal(got, rotate(before, cos, sin, picks[None, None], 128))
