@@ -9,7 +9,10 @@ namespace innerq {
 constexpr int kChunkWaveRows = 32;      // query rows of a wavefront (a row: one query head of one new token)
 constexpr int kChunkSplitMost = 256;    // most ranges the keys of a row are split into
 constexpr int kChunkListMost = 256;     // most sequences of a batch whose work is shared out by their lengths
-constexpr int kChunkListItems = 1024;   // work-groups that such a launch aims at (two rounds)
+// Work-groups that such a launch aims at: one round.  (us with 512, 1024 and 1536, 32 / 8 heads, 4 bits, counts spread over a factor of 16 and
+// more: 32 sequences to 8k tokens, to 64 new 111, 135, 146; 16 to 16k, to 8 new 53, 63, 72; 4 to 16k, to 512 new 122, 141, 157; 16 to 16k, to 256
+// new 244, 236, 258: more ranges share the work better and leave more partial results.)
+constexpr int kChunkListItems = 512;
 constexpr int kChunkTableBytes = 2 * kChunkListMost * (int)sizeof(int);   // first slot and splits of every sequence, at the workspace's start
 
 struct ChunkForm {
