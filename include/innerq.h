@@ -360,8 +360,9 @@ int innerq_decode_step_ragged(const innerq_config_t *cfg, const innerq_cache_t *
  * both (no counterpart in the paper, whose path decodes one token a step).  The calls below take rows where they
  * lie, in the output of a projection: a tensor is named by its first element and the strides of batch, head and
  * token in ELEMENTS; the head_dim channels of a row are contiguous.  Strides are multiples of 8 (rows start on 16
- * bytes) and not negative; a stride of 0 (the same row for all) is fine for what is read.  They serve inner-grouped
- * caches (INNERQ_E_UNSUPPORTED for the other kinds) of at most 2^24 capacity_tokens. */
+ * bytes) and not negative; a stride of 0 (the same row for all) is fine for what is read, rows that are written must
+ * not overlap each other (INNERQ_E_ARG).  The calls that take a cache serve inner-grouped ones (INNERQ_E_UNSUPPORTED
+ * for the other kinds) of at most 2^24 capacity_tokens. */
 typedef struct {
   int64_t batch, head, token;
 } innerq_strides_t;
@@ -408,7 +409,7 @@ int innerq_append_rotated(const innerq_config_t *cfg, innerq_cache_t *cache, con
  *   t_new         host: the bound that sizes the launch
  * Every store is left one step ahead of its sequence (as innerq_decode_step_ragged wants and keeps it).  Counts
  * outside their bounds are clamped on the device (a sequence that would pass capacity_tokens takes the tokens that
- * fit); no buffer is overrun. */
+ * fit); no buffer is overrun.  Two launches for single tokens (the rows, then the counts), else three. */
 int innerq_append_rotated_ragged(const innerq_config_t *cfg, const innerq_cache_t *cache,
                                  const innerq_rotation_t *rotation, const int32_t *positions, int32_t *n_tokens_dev,
                                  const int32_t *t_new_dev, const void *k_new, const innerq_strides_t *k_strides,

@@ -1,6 +1,7 @@
 // C ABI of libinnerq (see include/innerq.h): argument checks, the window /
 // eviction arithmetic on the host, and kernel dispatch.  No device memory is
 // allocated here and nothing synchronises.
+#include <algorithm>
 #include <time.h>
 #include <unistd.h>
 
@@ -632,13 +633,18 @@ int check_rows(const void* p, const innerq_strides_t* s, int unit = 8) {
   }
   return INNERQ_OK;
 }
-// Rows that are written: no two of them the same.
+// Rows that are written: none overlaps another (each dimension lies beyond the extent of those of smaller strides).
 int check_rows_out(const void* p, const innerq_strides_t* s, long long batch, long long heads, long long tokens, int unit = 8) {
   const int st = check_rows(p, s, unit);
   if (st != INNERQ_OK) return st;
-  const struct { int64_t stride; long long n; } dims[3] = {{s->batch, batch}, {s->head, heads}, {s->token, tokens}};
-  for (const auto& d : dims)
-    if (d.n > 1 && d.stride < kHeadDim) return INNERQ_E_ARG;
+  struct Dim { int64_t stride; long long n; } dims[3] = {{s->batch, batch}, {s->head, heads}, {s->token, tokens}};
+  std::sort(dims, dims + 3, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
+  int64_t extent = kHeadDim;                             // elements from the first to the last of the dimensions so far
+  for (const Dim& d : dims) {
+    if (d.n <= 1) continue;
+    if (d.stride < extent || d.stride > (INT64_MAX - extent) / (d.n - 1)) return INNERQ_E_ARG;
+    extent += d.stride * (d.n - 1);
+  }
   return INNERQ_OK;
 }
 RowView rows_of(const void* p, const innerq_strides_t& s) { return {static_cast<const __half*>(p), s.batch, s.head, s.token}; }
@@ -718,6 +724,7 @@ int chunk_attention(const innerq_config_t* cfg, const innerq_cache_t* cache, con
                     const innerq_strides_t* q_strides, int64_t t_new, const float* q_scale, void* out, const innerq_strides_t* out_strides,
                     int out_is_fp32, void* workspace, size_t workspace_bytes, void* hip_stream) {
   const innerq_config_t& c = *cfg;
+  if (!chunk_rows_fit(c, t_new)) return INNERQ_E_UNSUPPORTED;
   int st = check_rows(k_new, k_strides);
   if (st == INNERQ_OK) st = check_rows(v_new, v_strides);
   if (st == INNERQ_OK) st = check_rows(q, q_strides);
@@ -725,7 +732,6 @@ int chunk_attention(const innerq_config_t* cfg, const innerq_cache_t* cache, con
   if (st != INNERQ_OK) return st;
   if (!workspace) return INNERQ_E_NULL;
   if (misaligned(workspace) || (q_scale && misaligned(q_scale))) return INNERQ_E_ALIGN;
-  if (!chunk_rows_fit(c, t_new)) return INNERQ_E_UNSUPPORTED;
   const ChunkSizes sizes = chunk_sizes(c, t_new, tokens - t_new);
   if (workspace_bytes < chunk_workspace_bytes(c, t_new)) return INNERQ_E_WORKSPACE;
   ChunkArgs a;

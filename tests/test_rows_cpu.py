@@ -33,7 +33,7 @@ def rotation(**over):
     return r
 
 
-def strides(batch=1280, head=128, token=640):
+def strides(batch=16384, head=128, token=1280):
     return iq.innerq_strides_t(batch, head, token)
 
 
@@ -76,6 +76,22 @@ def test_rotate(over, want):
     assert call_rotate(**over) == want
 
 
+@pytest.mark.parametrize("s", [strides(head=128, token=128), strides(token=384), strides(head=384, token=128, batch=384), strides(batch=2560), strides(batch=2944, head=256)])
+def test_rows_that_are_written_do_not_overlap(s):
+    # two sequences, three tokens, four (rotation) or eight (attention) heads
+    assert call_rotate(ys=s) == iq.E_ARG
+    assert attentions(outs=strides(s.batch, s.head, s.token)) == (iq.E_ARG, iq.E_ARG)
+
+
+def test_rows_next_to_each_other_in_any_order_are_written():
+    for order in ((0, 1, 2), (0, 2, 1), (1, 0, 2), (2, 1, 0)):
+        n, at, s = (2, 4, 3), 128, [0, 0, 0]
+        for d in reversed(order):
+            s[d] = at
+            at *= n[d]
+        assert call_rotate(ys=strides(*s), n_dev=P + 1) == iq.E_ALIGN      # (what is looked at next: the rows are accepted, nothing is launched)
+
+
 def appends(cfg, cache, k=P, ks=None, v=P, vs=None, t=3, inv=None, n_dev=P, t_dev=P, rot=None, positions=None):
     ks, vs = ks or strides(), vs or strides()
     before = cache.n_tokens if cache else None
@@ -114,7 +130,7 @@ def test_struct_layout_matches_the_header():
 def attentions(cfg=None, cache=None, k=P, ks=None, v=P, vs=None, q=P, qs=None, t=3, scale=None, out=P, outs=None, fp32=0, ws=P, ws_bytes=1 << 40,
                n_dev=P, t_dev=P, most=500):
     cfg, cache = cfg or config(), cache or cache_of()
-    s = [x or strides(token=1280) for x in (ks, vs, qs, outs)]
+    s = [x or strides() for x in (ks, vs, qs, outs)]
     rows = [k, ref(s[0]), v, ref(s[1]), q, ref(s[2]), t, scale, out, ref(s[3]), fp32, ws, ws_bytes, None]
     return (L.innerq_chunk_attention(ref(cfg), ref(cache), *rows), L.innerq_chunk_attention_ragged(ref(cfg), ref(cache), n_dev, t_dev, most, *rows))
 
