@@ -226,11 +226,12 @@ struct ChunkKernel {
   struct Plain { u32x4 k[P][4]; u32x4 v[P][4]; };
   enum Which { kBoth, kKeys, kValues };                  // of a thread's pieces
 
-  // Store rows row0 .. (a multiple of the tile, so one page holds them): pieces in registers.  Behind the last packed row: the
+  // Store rows row0 .. (a multiple of the tile of 64, so one page holds them): pieces in registers.  Behind the last packed row: the
   // same rows again, whose scores are masked.
   static __device__ __forceinline__ void load_packed(const ChunkArgs& a, const ChunkSeq& s, int b, int h, int row0, int tid, bool values, Packed& x) {
     const long long lin = tile_row(a, b, h, row0);
-    const bool whole = KT == 32 || s.packed_v - row0 >= KT;
+    static_assert(KT == 64);
+    const bool whole = s.packed_v - row0 >= KT;
     if constexpr (ONE) {
       const int p = tid % (NT / 2);
       PieceAt<KB, G> k, v;
@@ -252,13 +253,10 @@ struct ChunkKernel {
         x.k[m].load(codes + at.low, codes + at.high, a.k.scales + lin * (D / G) + at.scale, a.k.zeros + lin * (D / G) + at.scale);
       }
       if (!APART || values) {
-        // (tiles of 32 tokens may begin in the middle of a group of 64)
-        const int block = KT == 32 ? (G == 64 ? (row0 & 63) / 32 : 0) : whole ? p / D : 0;
-        const long long first = KT == 32 && G == 64 ? lin - (row0 & 63) : lin;
         PieceAt<VB, G> at;
-        at.value(p % D, block);
-        const uint8_t* codes = a.v.codes + first * (16 * VB);
-        x.v[m].load(codes + at.low, codes + at.high, a.v.scales + first * (D / G) + at.scale, a.v.zeros + first * (D / G) + at.scale);
+        at.value(p % D, whole ? p / D : 0);
+        const uint8_t* codes = a.v.codes + lin * (16 * VB);
+        x.v[m].load(codes + at.low, codes + at.high, a.v.scales + lin * (D / G) + at.scale, a.v.zeros + lin * (D / G) + at.scale);
       }
     }
   }
@@ -545,7 +543,6 @@ struct ChunkKernel {
     for (int i = 0; i < N; ++i) out[i] = w[i] >> by;
     if constexpr (VB == 3) out[2] = w[2] >> (by / 2);
   }
-  // One tile: the scores of the one behind it (from `ahead`) are on their way while its own become weights.
   static __device__ __forceinline__ void direct_keys(const FieldMasks& f, const Direct& x, const Rows& r, float16_t (&s)[NB]) {
     s[0] = float16_t{};
     Decoder<KB> d;
@@ -705,7 +702,7 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int group, int ite
 }
 
 // Tiles u0 .. u1 of one kind: load(u, registers), put(buffer, registers), masks(u) -> {masked, limit} as for finish.  This wavefront's rows
-// attend to those before `mine`.  The next tile is put into LDS, and the one after it loaded, between the two products (behind the last tile:
+// attend to those before `mine`.  One buffer (a wavefront by itself): load also puts.  Else the next tile is put into LDS, and the one after it loaded, between the two products (behind the last tile:
 // the same again).
 struct TileMask { bool masked; int limit; };
 template <typename C, typename Regs, typename Load, typename Put, typename Mask>
@@ -818,7 +815,6 @@ __global__ void __launch_bounds__(64 * RW * TW) __attribute__((amdgpu_waves_per_
   typename C::FieldMasks masks;
   masks.k.start();
   masks.v.start();
-  auto put_packed = [&](char* at, const typename C::Packed& x) { C::put_packed(masks, at, tid, values, x); };
   auto put_plain = [&](char* at, const typename C::Plain& x) { C::put_plain(at, tid, values, x); };
   if constexpr (RW == 1) {
     const int u0 = from(0), u1 = to(0, tiles1);
@@ -850,7 +846,8 @@ __global__ void __launch_bounds__(64 * RW * TW) __attribute__((amdgpu_waves_per_
     }
   } else {
     pass_tiles<C, typename C::Packed>(from(0), to(0, tiles1), has_rows ? tiles1 : 0, mine, r, lane, scale,
-        [&](int u, typename C::Packed& x) { C::load_packed(a, s, b, h, u * C::KT, tid, values, x); }, put_packed,
+        [&](int u, typename C::Packed& x) { C::load_packed(a, s, b, h, u * C::KT, tid, values, x); },
+        [&](char* at, const typename C::Packed& x) { C::put_packed(masks, at, tid, values, x); },
         [&](int u) { return TileMask{s.packed_v - u * C::KT < C::KT, s.packed_v - u * C::KT - 1}; });
   }
   pass_tiles<C, typename C::Plain>(from(tiles1), to(tiles1, tiles2), has_rows ? tiles2 : 0, mine, r, lane, scale,
