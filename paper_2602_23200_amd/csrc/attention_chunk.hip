@@ -38,6 +38,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int D = kHeadDim;
 constexpr int kKeyPitch = 2 * D + 16;                    // bytes of a key row in LDS (16 apart in the banks)
 constexpr float kRaise = 6.0f;                           // log2 of the largest weight before the level is raised
+constexpr float kFar = 0x1p19f;                          // levels beyond: neighbours in fp32 are 2^-4 apart and more
+constexpr float kFarShare = 0x1p-16f;                    // of its own size, by which a level is raised the sooner
 
 __device__ __forceinline__ half2_t as_half2(uint32_t w) { return __builtin_bit_cast(half2_t, w); }
 __device__ __forceinline__ uint32_t as_u32(half2_t h) { return __builtin_bit_cast(uint32_t, h); }
@@ -446,9 +448,10 @@ struct ChunkKernel {
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
     top = fmaxf(top, other_half(top)) * scale;
-    const bool raise = top > r.m + kRaise;               // (from the empty state: if there is a token at all)
+    // (from the empty state: if there is a token at all; the larger the level, the sooner, and beyond kFar always)
+    const bool raise = top > __builtin_fmaf(-kFarShare, __builtin_fabsf(r.m), r.m) + kRaise;
     if (__builtin_amdgcn_ballot_w64(raise)) {
-      const float level = raise ? top : r.m;
+      const float level = raise ? fmaxf(r.m, top) : r.m;
       const float f = raise ? __builtin_amdgcn_exp2f(r.m - level) : 1.f;       // (0 from the empty state)
       r.l *= f;
 #pragma unroll
@@ -458,6 +461,18 @@ struct ChunkKernel {
       r.m = level;
     }
     const float level = r.m == -INFINITY ? 0.f : r.m;    // (a row that has met no token yet)
+    if (__builtin_amdgcn_ballot_w64(__builtin_fabsf(level) > kFar)) {
+      // The fused form below takes the level, which is rounded, from the exact product: at 2^28 the largest score would be up to 16 above its own
+      // level and its weight beyond fp16.  Scores of such tiles are rounded as the level is.
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[n][i] *= scale;
+          asm volatile("" : "+v"(s[n][i]));              // (one rounding here and one below)
+        }
+      scale = 1.f;
+    }
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
