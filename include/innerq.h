@@ -427,8 +427,9 @@ int innerq_append_rotated_ragged(const innerq_config_t *cfg, const innerq_cache_
  *   workspace   device scratch of innerq_chunk_workspace_bytes(cfg, t_new) bytes, content undefined; calls that may
  *               run at the same time need one each
  * Products are taken of fp16 operands on the matrix cores, accumulated in fp32: dequantised keys and values and the
- * softmax weights are rounded to fp16 (relative 2^-12 rms each), statistics and sums are fp32.  Cached values up to
- * 65000 in magnitude; inputs finite (rows beyond a sequence's count are not read). */
+ * softmax weights are rounded to fp16 (by at most 2^-11 of each, 2^-12 or so rms; weights below 2^-23 of a row's largest
+ * one by up to 2^-34 of that one), statistics and sums are fp32.  Cached values up to 65000 in magnitude; inputs finite
+ * (rows beyond a sequence's count are not read). */
 size_t innerq_chunk_workspace_bytes(const innerq_config_t *cfg, int64_t t_new);
 int innerq_chunk_attention(const innerq_config_t *cfg, const innerq_cache_t *cache, const void *k_new,
                            const innerq_strides_t *k_strides, const void *v_new, const innerq_strides_t *v_strides,

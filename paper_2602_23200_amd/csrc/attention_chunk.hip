@@ -14,8 +14,9 @@
 // Stored fields become fp16 exactly: masked in place under the exponent that gives their bits weight one (1024 + u, 256 + u, ..), that
 // constant subtracted (exact), then one fused |S| u + Z rounded to fp16 (relative 2^-12 rms, as the weights; scores, statistics and sums are fp32).
 //
-// The softmax reference level is raised only when a score passes it by 2^6 (weights up to 2^6 are far from fp16's end): the outputs
-// are scaled rarely.
+// The softmax reference level is put 2^9 below the score that raises it, and raised again only when a score passes it by 2^15: the outputs are
+// scaled rarely, and weights keep fp16's full precision down to 2^-23 of the largest one and some of it down to 2^-34.  (With the level at the
+// largest score, tokens 17 nats below it were off by 14 % and those 18 below it lost, which a long flat tail of them is not.)
 //
 // Many rows are bound by the matrix and the vector pipes: 2048 new tokens over 32k cached ones (32 / 8 heads, 4 bits) take 1142 us, 993
 // TFLOP/s, the matrix pipes 50 % and the vector pipes 53 % busy (a large library product: 1320 TFLOP/s).  Few rows are bound by the
@@ -37,7 +38,9 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int D = kHeadDim;
 constexpr int kKeyPitch = 2 * D + 16;                    // bytes of a key row in LDS (16 apart in the banks)
-constexpr float kRaise = 6.0f;                           // log2 of the largest weight before the level is raised
+// log2 of the weight that the largest score has when it raises the level, and of the largest weight before the level is raised: as high in fp16 as
+// rare raises allow, because weights are rounded coarser below 2^-14 and vanish below 2^-25 (2^-34 of the largest weight then).
+constexpr float kTop = 9.0f, kRaise = 15.0f;
 constexpr float kFar = 0x1p19f;                          // levels beyond: neighbours in fp32 are 2^-4 apart and more
 constexpr float kFarShare = 0x1p-16f;                    // of its own size, by which a level is raised the sooner
 
@@ -451,7 +454,7 @@ struct ChunkKernel {
     // (from the empty state: if there is a token at all; the larger the level, the sooner, and beyond kFar always)
     const bool raise = top > __builtin_fmaf(-kFarShare, __builtin_fabsf(r.m), r.m) + kRaise;
     if (__builtin_amdgcn_ballot_w64(raise)) {
-      const float level = raise ? fmaxf(r.m, top) : r.m;
+      const float level = raise ? fmaxf(r.m, __builtin_fabsf(top) > kFar ? top : top - kTop) : r.m;
       const float f = raise ? __builtin_amdgcn_exp2f(r.m - level) : 1.f;       // (0 from the empty state)
       r.l *= f;
 #pragma unroll

@@ -1,4 +1,5 @@
-"""innerq_chunk_attention where scores are very large: their neighbours in fp32 are whole numbers apart."""
+"""innerq_chunk_attention where scores lie far apart or are very large: weights far below the largest one, and scores whose neighbours in fp32
+are whole powers of two apart."""
 import math
 from dataclasses import replace
 
@@ -6,7 +7,7 @@ import numpy as np
 import pytest
 
 from oracle import innerq_oracle as orc
-from tests.chunk_reference import operands
+from tests.chunk_reference import attend, check, operands
 from tests.helpers import gpu_config, oracle_config
 from tests.test_gpu_chunk import small
 
@@ -22,6 +23,58 @@ def env():
     assert torch.cuda.is_available(), "these tests need the MI355X"
     iq.lib()
     return torch, iq
+
+
+@pytest.mark.parametrize("form", range(3))
+@pytest.mark.parametrize("strong", [0, 4, 30, 700])
+@pytest.mark.parametrize("nats", [5.0, 12.0, 16.0, 17.0, 18.0, 21.0])
+def test_one_token_far_above_the_others(env, nats, strong, form):
+    """A sink, the first packed token, one of the first tile, one of the window: its value is 0, so that the output is what the others' weights
+    are.  They are `nats` below it; in fp16 at a level equal to the largest score they would lose their bits (from 9.7 nats on) and vanish (from
+    17.3 on)."""
+    torch, iq = env
+    t, r = FORMS[form]
+    n, heads = 720, 512
+    w = small(n_q_heads=heads * r, n_kv_heads=heads, bits=4)
+    o = oracle_config(w, capacity=1024)
+    o1 = replace(o, n_q_heads=r, n_kv_heads=1)
+    rng = np.random.default_rng(form)
+    # one value in a row: asymmetric groups of one zero-point, nothing is rounded; many equal heads, so that the keys are not split
+    k = np.full((1, 1, n + t, 128), 0.25, np.float16)
+    k[:, :, strong] = 1.25
+    v = (1.0 + rng.random((1, 1, n + t, 128))).astype(np.float16)
+    v[:, :, strong] = 0.0
+    q = np.full((1, r, t, 128), nats / math.sqrt(128.0), np.float16)
+    cache, ref = iq.allocate_cache(gpu_config(o)), orc.cache_new(o1)
+    orc.quantize_append(o1, ref, k[:, :, :n], v[:, :, :n])
+    kd, vd = (torch.from_numpy(x).cuda().expand(-1, heads, -1, -1) for x in (k, v))
+    qd = torch.from_numpy(q).cuda().repeat(1, heads, 1, 1)
+    iq.innerq_append_rotated(cache, kd[:, :, :n], vd[:, :, :n])
+    out = iq.innerq_chunk_attention(cache, kd[:, :, n:], vd[:, :, n:], qd, iq.allocate_chunk_workspace(cache.cfg, t))
+    assert torch.equal(out[:, :r], out[:, -r:])
+    want, bound = attend(q[0], operands(o1, ref, "k", k[0, :, n:]), operands(o1, ref, "v", v[0, :, n:]), False)
+    print(check(out[0, :r].cpu().numpy(), want, bound))
+
+
+@pytest.mark.parametrize("nats", [12.0, 17.0, 21.0])
+def test_one_new_token_far_above_the_others(env, nats):
+    """The same within a first prompt, where the strong token is the first new one."""
+    torch, iq = env
+    t, heads = 900, 64
+    w = small(n_q_heads=heads, n_kv_heads=heads, bits=4)
+    o = oracle_config(w, capacity=1024)
+    rng = np.random.default_rng(1)
+    k = np.full((1, t, 128), 0.25, np.float16)
+    k[:, 0] = 1.25
+    v = (1.0 + rng.random((1, t, 128))).astype(np.float16)
+    v[:, 0] = 0.0
+    q = np.full((1, t, 128), nats / math.sqrt(128.0), np.float16)
+    cache = iq.allocate_cache(gpu_config(o))
+    kd, vd, qd = (torch.from_numpy(x).cuda()[None].expand(-1, heads, -1, -1) for x in (k, v, q))
+    out = iq.innerq_chunk_attention(cache, kd, vd, qd, iq.allocate_chunk_workspace(cache.cfg, t))
+    want, bound = attend(q, k.astype(np.float64), v.astype(np.float64), False)
+    print(check(out[0, :1].cpu().numpy(), want, bound))
+    assert torch.equal(out[0, 0], out[0, -1])
 
 
 MAGNITUDES = [(60.0, 100.0), (3000.0, 1000.0), (3000.0, 60000.0), (60000.0, 60000.0)]
