@@ -481,12 +481,14 @@ struct ChunkKernel {
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         p[2 * n + i / 8][2 * (i % 4) + (i / 4) % 2] = (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i], scale, -level));
-    // (the sum is that of the weights as they are rounded)
+    // (the sum is that of the weights as they are rounded; of the tile first: two at a time they would vanish in a row's sum of 2^25 times as much)
+    float sum = 0.f;
 #pragma unroll
     for (int st = 0; st < 2 * NB; ++st)
 #pragma unroll
       for (int e = 0; e < 8; e += 2)
-        r.l = __builtin_amdgcn_fdot2(half2_t{p[st][e], p[st][e + 1]}, half2_t{(_Float16)1.0f, (_Float16)1.0f}, r.l, false);
+        sum = __builtin_amdgcn_fdot2(half2_t{p[st][e], p[st][e + 1]}, half2_t{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
+    r.l += sum;
   }
 
   // ---- a wavefront by itself takes packed tiles of 32 tokens straight from memory to its operands.  Keys: a lane has half a row of one

@@ -77,6 +77,48 @@ def test_one_new_token_far_above_the_others(env, nats):
     assert torch.equal(out[0, 0], out[0, -1])
 
 
+@pytest.mark.parametrize("form", range(3))
+@pytest.mark.parametrize("nats", [15.0, 17.4, 20.0])
+def test_a_long_flat_tail(env, nats, form):
+    """A million tokens `nats` below one strong token, in a range of their own: together they hold 24 % to 0.2 % of the weight.  All blocks of the
+    store but the first are one page."""
+    torch, iq = env
+    t, r = FORMS[form]
+    n, B, heads = 1 << 20, [128, 64, 64][form], 8
+    cfg = iq.make_config(B, heads * r, heads, 128, 4, 32, 4, 128, orc.ASYM, orc.ASYM, capacity_tokens=n + 64, page_pool_pages=2)
+    table = torch.ones(B, (n + 64) // 64, dtype=torch.int32, device="cuda")
+    table[:, 0] = 0
+    cache = iq.allocate_cache(cfg, page_table=table)
+    # codes and scales 0: every value is its group's zero-point
+    for name, x in cache.buffers.items():
+        if name != "page_table":
+            x.zero_()
+    for which, low in (("k", 0.25), ("v", 1.0)):
+        cache.buffers[f"{which}_scales"].view(torch.float16).fill_(-0.0)
+        for part in ("zeros", "sink", "recent"):
+            cache.buffers[f"{which}_{part}"].view(torch.float16).fill_(low)
+    rows = cache.buffers["k_zeros"].view(torch.float16).view(2, heads, 64, 4)
+    rows[0, :, 0] = 1.25
+    # (a value's group is 32 tokens of a channel: the strong token's group says 0 for all of them, which are 31 of a million)
+    cache.buffers["v_zeros"].view(torch.float16).view(2, heads, 2, 128)[0, :, 0] = 0.0
+    cache.c.n_tokens = cache.c.store_ahead_tokens = n
+    k = torch.full((B, heads, t, 128), 0.25, dtype=torch.float16, device="cuda")
+    v = torch.ones(B, heads, t, 128, dtype=torch.float16, device="cuda")
+    x = np.float16(nats / math.sqrt(128.0))
+    q = torch.full((B, heads * r, t, 128), float(x), dtype=torch.float16, device="cuda")
+    out = iq.innerq_chunk_attention(cache, k, v, q, iq.allocate_chunk_workspace(cfg, t))
+    low = math.exp(-float(x) * 128.0 / math.sqrt(128.0))
+    for i in range(t):
+        others = n + i
+        want = (others - 31) * low / (1.0 + others * low)
+        # 2^-11 each for the roundings of the strong weight and of the tail's (all alike), 2^-34 of the strong one for those below the normal
+        # range; sums in fp32, whose addends are all alike, so that their roundings may be: 2^-24 of the sum for each of a wavefront's additions
+        most = 1.0 / (1.0 + others * low)
+        bound = 2 * want * (1 - want) * 2.0 ** -11 + 2.0 ** -34 * most * others + 2.0 ** -24 * (n / 16 + 600) * want
+        err = (out[:, :, i] - want).abs().max().item()
+        assert err <= bound, (i, err, bound, want)
+
+
 MAGNITUDES = [(60.0, 100.0), (3000.0, 1000.0), (3000.0, 60000.0), (60000.0, 60000.0)]
 
 
