@@ -408,8 +408,10 @@ int innerq_append_rotated(const innerq_config_t *cfg, innerq_cache_t *cache, con
  *   t_new_dev     int32 [B]: new tokens of every sequence, 0 .. t_new; rows of k_new, v_new beyond them are not read.
  *   t_new         host: the bound that sizes the launch
  * Every store is left one step ahead of its sequence (as innerq_decode_step_ragged wants and keeps it).  Counts
- * outside their bounds are clamped on the device (a sequence that would pass capacity_tokens takes the tokens that
- * fit); no buffer is overrun.  Two launches for single tokens (the rows, then the counts), else three. */
+ * outside their bounds are caught on the device: t_new_dev is clamped into 0 .. t_new, a sequence that would pass
+ * capacity_tokens takes the tokens that fit, and one whose count of cached tokens is outside 0 .. capacity_tokens
+ * takes none (its buffers and its count stay as they were).  Two launches for single tokens (the rows, then the
+ * counts), else three. */
 int innerq_append_rotated_ragged(const innerq_config_t *cfg, const innerq_cache_t *cache,
                                  const innerq_rotation_t *rotation, const int32_t *positions, int32_t *n_tokens_dev,
                                  const int32_t *t_new_dev, const void *k_new, const innerq_strides_t *k_strides,

@@ -52,16 +52,16 @@ __global__ void __launch_bounds__(256) rotate_kernel(RotateArgs a) {
 // ---- appends
 
 // A sequence's state: n cached tokens, t new ones, the store filled for a cache of `to` tokens.  Counts from the device are
-// clamped into the cache.
+// clamped into the cache; a sequence whose cached count is none takes nothing.
 struct SeqState { int n, t, to; };
 __device__ __forceinline__ SeqState sequence_state(const AppendArgs& a, int b) {
   const int cap = (int)a.q.capacity;
   int n = (int)a.q.n_old, t = a.t_new;
   if (a.q.n_dev) {
-    n = a.q.n_dev[b];
-    n = n < 0 ? 0 : n > cap ? cap : n;
+    const int count = a.q.n_dev[b];
+    n = count < 0 ? 0 : count > cap ? cap : count;
     t = a.t_dev[b];
-    t = t < 0 ? 0 : t > a.t_new ? a.t_new : t;
+    t = t < 0 || n != count ? 0 : t > a.t_new ? a.t_new : t;
   }
   t = t < cap - n ? t : cap - n;
   return {n, t, n + t + a.ahead < cap ? n + t + a.ahead : cap};
@@ -140,8 +140,8 @@ __global__ void __launch_bounds__(256) append_copies_kernel(AppendArgs a, int pe
 __global__ void __launch_bounds__(256) advance_counts_kernel(AppendArgs a, int* counts) {
   const int b = (int)(blockIdx.x * 256 + threadIdx.x);
   if (b >= a.q.batch) return;
-  const int n = counts[b];
-  if (n >= 0 && n <= a.q.capacity) counts[b] = n + sequence_state(a, b).t;
+  const int t = sequence_state(a, b).t;
+  if (t > 0) counts[b] += t;
 }
 
 // A step: one new token a sequence, everything that leaves a ring was there before.  Groups spread over eight lanes (the chain of a
