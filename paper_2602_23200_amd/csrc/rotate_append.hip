@@ -25,7 +25,8 @@ __global__ void __launch_bounds__(256) rotate_kernel(RotateArgs a) {
   const int b = (int)div32(bt, a.t_new), t = (int)(bt - (long long)b * a.t_new);
   if (a.t_dev && t >= a.t_dev[b]) return;
   Turn turn;
-  load_turn(turn, a.rot, bt, a.rot.positions ? 0 : (a.n_dev ? a.n_dev[b] : a.n_tokens) + t, u);
+  // (a count from the device may be anything: the sum saturates, so that a place beyond 32 bits is the table's last)
+  load_turn(turn, a.rot, bt, a.rot.positions ? 0 : __builtin_elementwise_add_sat(a.n_dev ? a.n_dev[b] : a.n_tokens, t), u);
   const UnitChunks ch = unit_chunks(a.rot, u);
   const __half* x = a.x.p + b * a.x.batch + t * a.x.token;
   __half* y = a.y + b * a.y_batch + t * a.y_token;

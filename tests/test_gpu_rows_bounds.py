@@ -6,7 +6,7 @@ import pytest
 
 from oracle import innerq_oracle as orc
 from tests.helpers import assert_cache_equal, gpu_config, oracle_config
-from tests.rows import projection
+from tests.rows import projection, rotate, rotation_tables
 from tests.test_gpu_append_rows import small
 
 pytestmark = pytest.mark.gpu
@@ -50,3 +50,18 @@ def test_a_sequence_with_a_count_outside_the_cache_takes_nothing(env, bad, T):
     for name, x in cache.buffers.items():
         if x is not None:
             assert torch.equal(x.view(3, -1)[1], guard[name].view(3, -1)[1]), name
+
+
+def test_places_at_the_end_of_32_bits(env):
+    """Without positions a token stands at n_b + t: sums that 32 bits do not hold are beyond the table, as the largest ones are."""
+    torch, iq = env
+    rng = np.random.default_rng(4)
+    B, T, H = 4, 9, 2
+    x = projection(torch, rng, B, T, H, 1)[1]
+    cos, sin = rotation_tables(300, 128)
+    rot = iq.make_rotation(torch.from_numpy(cos).cuda(), torch.from_numpy(sin).cuda())
+    cfg = iq.make_config(B, 4, 2, 128, 2, 32, 4, 128, capacity_tokens=64)
+    n = np.array([(1 << 31) - 1, (1 << 31) - 4, -(1 << 31), -5], np.int32)
+    y = iq.innerq_rotate(cfg, rot, x, n_tokens_dev=torch.from_numpy(n).cuda()).cpu().numpy()
+    place = n.astype(np.int64)[None, :, None] + np.arange(T)[None, None]
+    assert np.array_equal(y, rotate(x.cpu().numpy(), cos, sin, place, 128))
