@@ -643,9 +643,8 @@ struct ChunkKernel {
   }
 };
 
-// ---- a ragged batch: what a work-group does, from the counts of all sequences (four a lane).  The keys of a sequence are cut into ranges of
-// `length` tiles, the least with which the launch's items (sequence, head, block of rows, range) are no more than aimed at; where even
-// whole sequences are more, they are not cut.  Every wavefront finds the same.
+// ---- a ragged batch: what a work-group does, from the counts of all sequences (four a lane; the arithmetic is the plan's).  Every wavefront
+// finds the same.
 struct ChunkWork { int b, h, row_block, split, n_splits, slot; };
 
 __device__ __forceinline__ int wave_sum(int x) {
@@ -655,9 +654,9 @@ __device__ __forceinline__ int wave_sum(int x) {
 }
 template <int ROWS, int TILE>                            // TILE: tokens that the work-group takes a turn
 __device__ __forceinline__ bool find_work(const ChunkArgs& a, int group, int item, ChunkWork& w) {
-  constexpr int N = kChunkListMost / 64, LEAST = 4;      // (a range shorter than that is mostly set-up)
+  constexpr int N = kChunkListMost / 64;
   const int lane = (int)threadIdx.x & 63;
-  int units[N], tiles[N];                                // (head, block of rows) and tiles of the lane's sequences
+  int units[N], tiles[N];                                // of the lane's sequences
   int most = 1;
   float work = 0.f;
 #pragma unroll
@@ -666,11 +665,9 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int group, int ite
     units[j] = tiles[j] = 0;
     if (b < a.batch) {
       const ChunkSeq s = chunk_seq(a, b, group);
-      const int rows = s.t * a.heads_per_kv;
-      if (rows > a.rows_from && rows <= a.rows_to) {
-        units[j] = a.n_kv_heads * ((rows + ROWS - 1) / ROWS);
-        tiles[j] = (s.n + s.t + TILE - 1) / TILE;
-      }
+      const ChunkShare share = chunk_share(s.n, s.t, a.heads_per_kv, a.n_kv_heads, a.rows_from, a.rows_to, ROWS, TILE);
+      units[j] = share.units;
+      tiles[j] = share.tiles;
     }
     most = tiles[j] > most ? tiles[j] : most;
     work += (float)units[j] * (float)tiles[j];
@@ -682,14 +679,13 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int group, int ite
     work += __shfl_xor(work, i);
   }
   most = __builtin_amdgcn_readfirstlane(most);
-  int length = __builtin_amdgcn_readfirstlane((int)(work * (1.0f / kChunkListItems)));
-  length = length < LEAST ? LEAST : length;
+  int length = __builtin_amdgcn_readfirstlane(chunk_first_length(work));
   int mine;
-  for (;; length += 1 + length / 8) {
+  for (;; length = chunk_next_length(length)) {
     mine = 0;
 #pragma unroll
-    for (int j = 0; j < N; ++j) mine += units[j] * ((tiles[j] + length - 1) / length);
-    if (length >= most || __builtin_amdgcn_readfirstlane(wave_sum(mine)) <= kChunkListItems) break;
+    for (int j = 0; j < N; ++j) mine += units[j] * chunk_ranges(tiles[j], length);
+    if (chunk_length_fits(length, most, __builtin_amdgcn_readfirstlane(wave_sum(mine)))) break;
   }
   // the sequence whose items hold this one
   int before = mine;
@@ -704,17 +700,16 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int group, int ite
   int first = __builtin_amdgcn_readlane(before - mine, owner);
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    const int u = __builtin_amdgcn_readlane(units[j], owner), t = __builtin_amdgcn_readlane(tiles[j], owner);
-    const int splits = (t + length - 1) / length, all = u * splits;
+    const int u = __builtin_amdgcn_readlane(units[j], owner), splits = chunk_ranges(__builtin_amdgcn_readlane(tiles[j], owner), length), all = u * splits;
     if (item >= first && item < first + all) {
-      const int at = item - first, unit = at / splits, blocks = u / a.n_kv_heads;
+      const ChunkPlace at = chunk_place(item - first, u, a.n_kv_heads, splits);
       w.b = N * owner + j;
-      w.split = at - unit * splits;
+      w.h = at.h;
+      w.row_block = at.row_block;
+      w.split = at.split;
       w.n_splits = splits;
-      w.h = unit / blocks;
-      w.row_block = unit - w.h * blocks;
       w.slot = item;
-      if (at == 0 && threadIdx.x == 0) {
+      if (item == first && threadIdx.x == 0) {
         a.table[2 * w.b] = item;
         a.table[2 * w.b + 1] = splits;
       }

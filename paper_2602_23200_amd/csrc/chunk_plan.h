@@ -76,6 +76,31 @@ inline ChunkList chunk_list(const innerq_config_t& c, long long t_new) {
   return {heads > kChunkListItems ? heads : kChunkListItems, rows <= kChunkWaveRows ? 0 : blocks > kChunkListItems ? blocks : kChunkListItems};
 }
 
+// What every work-group of such a launch works out for itself (constexpr: device code, too).  A sequence's share of a launch: units, each a kv head
+// and a block of `block` rows, and tiles of its keys; none if its rows are not above `from` and up to `to`.
+struct ChunkShare { int units, tiles; };
+constexpr ChunkShare chunk_share(int cached, int fresh, int heads_per_kv, int n_kv_heads, int from, int to, int block, int tile) {
+  const int rows = fresh * heads_per_kv;
+  if (rows <= from || rows > to) return {0, 0};
+  return {n_kv_heads * ((rows + block - 1) / block), (cached + fresh + tile - 1) / tile};
+}
+// The keys of a unit are cut into ranges of `length` tiles, the same for all sequences: the first of these lengths with which the ranges are no
+// more than kChunkListItems, or that of the longest sequence, which cuts none.  work: tiles of all units.
+constexpr int kChunkListLeast = 4;       // (a range shorter than that is mostly set-up)
+constexpr int chunk_first_length(float work) {
+  const int even = (int)(work * (1.0f / kChunkListItems));
+  return even < kChunkListLeast ? kChunkListLeast : even;
+}
+constexpr int chunk_next_length(int length) { return length + 1 + length / 8; }
+constexpr int chunk_ranges(int tiles, int length) { return (tiles + length - 1) / length; }
+constexpr bool chunk_length_fits(int length, int longest, int ranges) { return length >= longest || ranges <= kChunkListItems; }
+// Range number `at` of a sequence.
+struct ChunkPlace { int h, row_block, split; };
+constexpr ChunkPlace chunk_place(int at, int units, int n_kv_heads, int splits) {
+  const int unit = at / splits, blocks = units / n_kv_heads, h = unit / blocks;
+  return {h, unit - h * blocks, at - unit * splits};
+}
+
 inline size_t chunk_workspace_bytes(const innerq_config_t& c, long long t_new) {
   size_t bytes = 0;
   const long long either[2] = {0, 2 * t_new};            // (either form of that many rows)
