@@ -423,7 +423,8 @@ int innerq_append_rotated_ragged(const innerq_config_t *cfg, const innerq_cache_
  *   out_i = softmax(q_i [K_cached; k_new_0 .. k_new_i]^T / sqrt(d)) [V_cached; v_new_0 .. v_new_i],
  * the cached tokens as the cache holds them (windows fp16, store dequantised), the new ones as they are given
  * (rotated, and divided by the key-norm factors if the cached ones are).  The cache is not modified: a program
- * appends afterwards what it keeps of the chunk or the draft.  Any number of query heads per kv head; n may be 0.
+ * appends afterwards what it keeps of the chunk or the draft.  Any number of query heads per kv head; n may be 0;
+ * n + t_new (max_tokens below) is at most capacity_tokens (INNERQ_E_CAPACITY).
  *   q, out      fp16 rows; out fp32 rows if out_is_fp32 (strides then multiples of 4), not overlapping an input
  *   q_scale     device, fp32 [Hk][d] or NULL: as for innerq_decode_attention
  *   workspace   device scratch of innerq_chunk_workspace_bytes(cfg, t_new) bytes, content undefined; calls that may
@@ -441,7 +442,9 @@ int innerq_chunk_attention(const innerq_config_t *cfg, const innerq_cache_t *cac
 
 /* The same with the counts of every sequence in DEVICE memory (innerq_append_rotated_ragged): n_tokens_dev cached
  * (read only here), t_new_dev new tokens, 0 .. t_new.  max_tokens (host) bounds n_tokens_dev[b] + t_new_dev[b] and
- * only sizes the launch.  Rows of out beyond a sequence's count are left as they were. */
+ * only sizes the launch.  Rows of out beyond a sequence's count are left as they were.  Counts outside their bounds are
+ * clamped on the device.  Where all sequences have the same counts and the host knows them, innerq_chunk_attention is the
+ * faster call for long chunks (up to 1.5 times). */
 int innerq_chunk_attention_ragged(const innerq_config_t *cfg, const innerq_cache_t *cache,
                                   const int32_t *n_tokens_dev, const int32_t *t_new_dev, int64_t max_tokens,
                                   const void *k_new, const innerq_strides_t *k_strides, const void *v_new,

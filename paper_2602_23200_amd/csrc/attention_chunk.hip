@@ -18,9 +18,10 @@
 // scaled rarely, and weights keep fp16's full precision down to 2^-23 of the largest one and some of it down to 2^-34.  (With the level at the
 // largest score, tokens 17 nats below it were off by 14 % and those 18 below it lost, which a long flat tail of them is not.)
 //
-// Many rows are bound by the matrix and the vector pipes: 2048 new tokens over 32k cached ones (32 / 8 heads, 4 bits) take 1142 us, 993
-// TFLOP/s, the matrix pipes 50 % and the vector pipes 53 % busy (a large library product: 1320 TFLOP/s).  Few rows are bound by the
-// decoding: 5 new tokens over 8 x 32k at 2 bits 75 us, 2.75 TB/s, vector pipes 70 % busy; without the decoding 63 us of 87 remained.
+// Many rows are bound by the matrix and the vector pipes, which hardly overlap: 2048 new tokens over 32k cached ones (32 / 8 heads, 4 bits)
+// take 1160 to 1230 us by session, 980 to 920 TFLOP/s, the matrix pipes 49 % and the vector pipes 54 % busy (a large library product: 1270 to
+// 1320 TFLOP/s).  Few rows are bound by the decoding: 5 new tokens over 8 x 32k at 2 bits 77 to 82 us, 2.7 to 2.5 TB/s, vector pipes 69 %
+// busy; without the decoding 63 us of 87 remained.
 #include "attention_chunk.h"
 
 #ifndef INNERQ_CHUNK_G
@@ -151,7 +152,8 @@ template <int BITS>
 __device__ __forceinline__ void decode(const Masks<BITS>& m, const Piece<BITS>& p, uint32_t (&out)[16]) {
   Decoder<BITS> d;
   d.start(p.scale, p.zero);
-  const u32x4 w[4] = {decode_part<BITS, 0, 0>(m, d, p.w), decode_part<BITS, 0, 1>(m, d, p.w), decode_part<BITS, 1, 0>(m, d, p.w), decode_part<BITS, 1, 1>(m, d, p.w)};
+  const u32x4 w[4] = {decode_part<BITS, 0, 0>(m, d, p.w), decode_part<BITS, 0, 1>(m, d, p.w),
+                      decode_part<BITS, 1, 0>(m, d, p.w), decode_part<BITS, 1, 1>(m, d, p.w)};
 #pragma unroll
   for (int i = 0; i < 16; ++i) out[i] = w[i / 4][i % 4];
 }
@@ -188,7 +190,7 @@ __device__ __forceinline__ ChunkSeq chunk_seq(const ChunkArgs& a, int b, int gro
 }
 
 // Where a thread finds its piece of a tile of packed rows: offsets from the tile's first row (a row takes 16 BITS bytes of codes
-// and 128 / G scales in either tensor), for a whole tile and for one of 32 rows.
+// and 128 / G scales in either tensor).
 template <int BITS, int G>
 struct PieceAt {
   uint32_t low, high, scale;
@@ -613,7 +615,8 @@ struct ChunkKernel {
   }
 
   // Channels 32 x .. of a row: the output itself, or (split) the partial result of a slot.
-  static __device__ __forceinline__ void store_channels(const ChunkArgs& a, int b, int h, int row, long long slot_row, bool split, int x, int half, const float16_t& o, float l) {
+  static __device__ __forceinline__ void store_channels(const ChunkArgs& a, int b, int h, int row, long long slot_row, bool split, int x, int half,
+                                                        const float16_t& o, float l) {
     const int c0 = 32 * x + 4 * half;
     if (split) {
       float* dst = a.ws + a.slots * (32 * RW * 2) + slot_row * D + c0;
@@ -721,8 +724,8 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int group, int ite
 }
 
 // Tiles u0 .. u1 of one kind: load(u, registers), put(buffer, registers), masks(u) -> {masked, limit} as for finish.  This wavefront's rows
-// attend to those before `mine`.  One buffer (a wavefront by itself): load also puts.  Else the next tile is put into LDS, and the one after it loaded, between the two products (behind the last tile:
-// the same again).
+// attend to those before `mine`.  One buffer (a wavefront by itself): load also puts.  Else the next tile is put into LDS, and the one after
+// it loaded, between the two products (behind the last tile: the same again).
 struct TileMask { bool masked; int limit; };
 template <typename C, typename Regs, typename Load, typename Put, typename Mask>
 __device__ __forceinline__ void pass_tiles(int u0, int u1, int mine, char* lds, typename C::Rows& r, int lane, float scale, Load load, Put put, Mask mask) {
@@ -819,8 +822,9 @@ __global__ void __launch_bounds__(64 * RW * TW) __attribute__((amdgpu_waves_per_
   const bool has_rows = first < rows;
 
   // tiles: packed rows, cached tokens beside them, new tokens; this wavefront's share of them.  A wavefront by itself brings fp16 tiles through
-  // LDS, one after the other: three times a packed tile (drafts of 5 over 8 x 32k tokens 87 us -> 82; counted so where there are eight tiles
-  // a wavefront, not in short calls: drafts of 4 over 500 tokens 11.3 -> 12.5).
+  // LDS, one after the other: three times a packed tile.  Counted so where there are eight tiles a wavefront: of the time with all tiles alike
+  // 0.89 to 0.97 at 8 to 16 tiles a wavefront, 0.95 to 1.05 at 60 and more; not below: 0.96 to 1.04 at 1 to 4 (1, 4 and 32 sequences, 32 / 8
+  // heads, 1k to 32k tokens, 1 to 8 new, 2 and 4 bits).
   const int tiles1 = (s.packed_v + C::KT - 1) / C::KT, tiles2 = tiles1 + (s.beside + C::KT - 1) / C::KT, tiles = tiles2 + last / C::KT + 1;
   const int parts = n_splits * TW, part = split * TW + group, plain = RW == 1 && tiles >= 8 * parts ? 3 : 1;
   const int cost = tiles1 + (tiles - tiles1) * plain, per = cost / parts, more = cost % parts;

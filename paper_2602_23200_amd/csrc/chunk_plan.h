@@ -68,7 +68,9 @@ inline int chunk_splits(const ChunkSizes& s, long long tokens) {
 inline size_t chunk_slot_bytes(const ChunkForm& f) { return (size_t)f.rows() * (kHeadDim + 2) * sizeof(float); }
 
 // A ragged batch of up to kChunkListMost sequences: work-groups find their work in a list made from the counts, one launch for the sequences of few
-// rows and one for those of more.  Most work-groups of either launch (none: 0).
+// rows and one for those of more.  Most work-groups of either launch (none: 0).  Such a list has four wavefronts a tile wherever the keys are, and
+// its work-groups go to any XCD: one sequence through the list and without it, us, 2048 new tokens over 32k 1420, 1226 (8 kv heads), first prompt
+// of 4096 314, 205 (32).
 struct ChunkList { long long few, some; };
 inline ChunkList chunk_list(const innerq_config_t& c, long long t_new) {
   const long long rows = t_new * (c.n_q_heads / c.n_kv_heads), heads = (long long)c.batch * c.n_kv_heads;

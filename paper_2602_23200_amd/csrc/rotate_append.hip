@@ -6,7 +6,7 @@
 // Both are bound by memory where there is much to do and by latency where there is little.  A rotation reads and writes a row once
 // (512 bytes a token and head); an append reads the new rows once (512 bytes a token and kv head) and writes them packed (96 bytes
 // at 2 bits, groups of 32), so rotating beforehand would almost double the keys' traffic.  Calls, least time by bytes at the rate of a copy
-// in brackets: rotation of 40 heads x 32k tokens 152 us (139); append of 4 x 8 heads x 32k tokens at 2 bits, keys rotated, 170 us (144);
+// in brackets: rotation of 40 heads x 32k tokens 150 us (139); append of 4 x 8 heads x 32k tokens at 2 bits, keys rotated, 171 to 180 us (144);
 // rotation of 8 x 40 heads, one token, 3.2 us in the kernel; a step of 32 x 8 heads 5.1, and 1.7 for the counts.
 #include "quantize_rows.h"
 #include "rotate.h"
@@ -288,10 +288,10 @@ __device__ __forceinline__ void append_values(const AppendArgs& a, const QuantTe
 struct ChunkPlan {
   int tiles, head_blocks, heads;       // keys: tiles a sequence, blocks of heads, heads of a block
   int groups;                          // value groups a sequence
-  int per_seq;                         // window copies a sequence (0: in a launch of their own)
+  int per_seq;                         // most window copies of a sequence
 };
 // Wavefronts a SIMD that the registers are made to fit: groups of 32 get four (LDS allows no more, as the compiler warns), but the code made for
-// five is the faster by 1 to 2 % (4 x 8 heads x 32k tokens 183 us, 185 with four asked for).
+// five is the faster by 1 to 2 % (4 x 8 heads x 32k tokens, in turn in one session: 183 us, 185 with four asked for).
 template <int G, bool FAST>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(G == 32 ? 5 : 3))) append_chunk_kernel(AppendArgs a, ChunkPlan plan) {
   __shared__ __align__(16) KeyTile<G> tile;
@@ -337,7 +337,8 @@ hipError_t launch_append(const AppendArgs& a, hipStream_t stream) {
     const long long kthreads = B * H * rows * (kHeadDim / G) * 8, vthreads = B * H * groups * kHeadDim * 8;
     const long long quant = div_up(kthreads > vthreads ? kthreads : vthreads, 256);
     if (quant + copy_blocks >= (1LL << 31)) return hipErrorInvalidValue;
-    append_step_kernel<G><<<dim3((unsigned)(quant + copy_blocks), 2), 256, 0, stream>>>(a, (int)(rows ? rows : 1), (int)(groups ? groups : 1), (unsigned)quant, (int)per_seq);
+    const dim3 grid((unsigned)(quant + copy_blocks), 2);
+    append_step_kernel<G><<<grid, 256, 0, stream>>>(a, (int)(rows ? rows : 1), (int)(groups ? groups : 1), (unsigned)quant, (int)per_seq);
     return hipGetLastError();
   }
   // one launch where no new token enters a ring slot that the call still reads
