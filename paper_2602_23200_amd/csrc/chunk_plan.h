@@ -90,8 +90,9 @@ constexpr ChunkShare chunk_share(int cached, int fresh, int heads_per_kv, int n_
 // more than kChunkListItems, or that of the longest sequence, which cuts none.  work: tiles of all units.
 constexpr int kChunkListLeast = 4;       // (a range shorter than that is mostly set-up)
 constexpr int chunk_first_length(float work) {
-  const int even = (int)(work * (1.0f / kChunkListItems));
-  return even < kChunkListLeast ? kChunkListLeast : even;
+  // (a call's tokens are at most 2^25, so no sequence has more than 2^19 tiles; beyond, sums with a length would pass 31 bits)
+  const float even = work * (1.0f / kChunkListItems);
+  return even < kChunkListLeast ? kChunkListLeast : even > 0x1p20f ? 1 << 20 : (int)even;
 }
 constexpr int chunk_next_length(int length) { return length + 1 + length / 8; }
 constexpr int chunk_ranges(int tiles, int length) { return (tiles + length - 1) / length; }

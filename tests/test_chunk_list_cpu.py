@@ -98,6 +98,13 @@ int main() {
       if (list.some) walk(n, t, heads, r, most_new, kChunkWaveRows, 0x7fffffff, kSomeRows, list.some, nudge);
     }
   }
+  // as much work as 31 bits of rows have over as many tokens as a call may name: lengths and ranges stay within 31 bits
+  for (float work = 1.0f; work < 1e14f; work *= 1.7f) {
+    const int length = chunk_first_length(work);
+    if (length < kChunkListLeast || (length < work / kChunkListItems - 1 && length < 1 << 19)) fail("first length", 0, 0, 0, 0);
+    for (const int tiles : {1, 1000, 1 << 19})
+      if (chunk_ranges(tiles, length) < 1 || (long long)chunk_ranges(tiles, length) * length < tiles) fail("ranges of a long length", 0, 0, 0, length);
+  }
   printf("%lld lists, %lld lengthened, %lld of more items than aimed at, %lld cut in part, %lld bad\n", lists, lengthened, uncut, mixed, bad);
   return bad || lengthened < 500 || uncut < 500 || mixed < 500;
 }
