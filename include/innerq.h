@@ -453,6 +453,124 @@ int innerq_chunk_attention_ragged(const innerq_config_t *cfg, const innerq_cache
                                   const innerq_strides_t *out_strides, int out_is_fp32, void *workspace,
                                   size_t workspace_bytes, void *hip_stream);
 
+/* ---- A cache held in 8 bits, with a scale for each block of tokens and head: for layers that do not bear 2 to 4 bits, and
+ * for an encoder's states (no counterpart in the paper).  It has a configuration, a cache and calls of its own; the
+ * conventions at the top of this file, the rows named by strides (16-byte rows, channels contiguous) and the page table are
+ * those of the other calls.  Keys and values that want a rotation are rotated before (innerq_rotate, in place).
+ *
+ * A block is `block` consecutive tokens (a multiple of it on) of one kv head; keys and values have a scale each,
+ *   S = fl(max |x| / T),  code = rn(fl(x / S)) (half to even; all zero where S = 0),  x^ = S * code,
+ * with T = 127 and 8-bit integers in two's complement (INNERQ_INT8), or T = 448 and floating point of four exponent and three
+ * mantissa bits, bias 7, subnormals, no infinities (INNERQ_E4M3).  Arithmetic is IEEE fp32 on the fp16 inputs.  A block is packed
+ * by the call that brings its last token; the tokens of a block that is not complete wait as they came, in the "open" rows.  So
+ * n cached tokens are n - n mod block packed ones and n mod block open ones, however they were split over calls.
+ *
+ * Layout: codes u8 [B][Hk][capacity/32][4096], 32 tokens of a head in the order in which the matrix cores take them:
+ *     keys    [a 2][h 2][g 4][c 16][e 16]      token 16 a + c of the 32, channel 32 g + 16 h + e
+ *     values  [q 4][g 4][c 16][m 2][i 2][j 4]  channel 32 q + 2 c + m, token 16 i + 4 g + j
+ *   scales fp32 [B][Hk][capacity/block]; open rows fp16 [B][Hk][block][d], token modulo block.
+ * Paged store: pages of 64 consecutive tokens of a sequence for all kv heads, in the layout above read with B = page_pool_pages
+ * and capacity = 64; the open rows stay per sequence.  Pages that hold complete blocks of 64 tokens are never written again. */
+typedef enum { INNERQ_INT8 = 0, INNERQ_E4M3 = 1 } innerq_block_type_t;
+
+typedef struct {
+  int32_t batch, n_q_heads, n_kv_heads, head_dim; /* head_dim = 128; n_q_heads % n_kv_heads == 0 */
+  int32_t type;            /* innerq_block_type_t of keys and values */
+  int32_t block;           /* 32 or 64 */
+  int64_t capacity_tokens; /* most tokens a sequence may ever hold; a multiple of 64, at most 2^24 */
+  int64_t page_pool_pages; /* 0: contiguous per sequence; else as in innerq_config_t */
+} innerq_block_config_t;
+
+typedef struct {
+  void *k_codes, *k_scales, *k_open; /* device */
+  void *v_codes, *v_scales, *v_open;
+  int64_t n_tokens;                  /* host: tokens cached so far, the same for the batch; advanced by innerq_block_append */
+  const int32_t *page_table;         /* device, int32 [B][capacity_tokens / 64]: as in innerq_cache_t.  Entries of the blocks that a
+                                        sequence's packed tokens reach after the call must name a page that no other live
+                                        sequence writes; entries outside the pool are clamped into it, never followed out of it. */
+} innerq_block_cache_t;
+
+typedef enum {
+  INNERQ_BLOCK_K_CODES = 0, INNERQ_BLOCK_K_SCALES, INNERQ_BLOCK_K_OPEN,
+  INNERQ_BLOCK_V_CODES, INNERQ_BLOCK_V_SCALES, INNERQ_BLOCK_V_OPEN,
+  INNERQ_BLOCK_BUF_COUNT
+} innerq_block_buffer_t;
+
+/* Host-only: as innerq_validate_config, innerq_buffer_bytes and innerq_chunk_workspace_bytes (t_new: rows of a sequence). */
+int innerq_block_validate_config(const innerq_block_config_t *cfg);
+size_t innerq_block_buffer_bytes(const innerq_block_config_t *cfg, int which /* innerq_block_buffer_t */);
+size_t innerq_block_workspace_bytes(const innerq_block_config_t *cfg, int64_t t_new);
+
+/* t_new tokens join the cache of every sequence; cache->n_tokens += t_new.  INNERQ_E_CAPACITY if they do not fit.  One launch.
+ *   k_new, v_new  device, fp16 rows, read only */
+int innerq_block_append(const innerq_block_config_t *cfg, innerq_block_cache_t *cache, const void *k_new,
+                        const innerq_strides_t *k_strides, const void *v_new, const innerq_strides_t *v_strides,
+                        int64_t t_new, void *hip_stream);
+
+/* The same with the counts of every sequence in DEVICE memory (a step can be recorded in a HIP graph).
+ *   n_tokens_dev  int32 [B]: tokens cached before the call; advanced by what was appended.  cache->n_tokens (host) is neither
+ *                 read nor written.
+ *   t_new_dev     int32 [B]: new tokens, clamped into 0 .. t_new; NULL: t_new each.  Rows beyond them are not read.
+ * A sequence that would pass capacity_tokens takes the tokens that fit; one whose count is outside 0 .. capacity_tokens takes
+ * none (its buffers and its count stay as they were).  One launch for up to `block` rows, else two. */
+int innerq_block_append_ragged(const innerq_block_config_t *cfg, const innerq_block_cache_t *cache, int32_t *n_tokens_dev,
+                               const int32_t *t_new_dev, const void *k_new, const innerq_strides_t *k_strides,
+                               const void *v_new, const innerq_strides_t *v_strides, int64_t t_new, void *hip_stream);
+
+/* Tokens first .. first + count - 1 of every sequence as fp16 rows: fp16(fl(S * code)) of packed tokens, open ones as they came.
+ *   k_out, v_out  device, fp16 rows (row i: token first + i); either may be NULL (with its strides) if it is not wanted
+ * INNERQ_E_ARG unless 0 <= first, 0 <= count and first + count <= n_tokens. */
+int innerq_block_read(const innerq_block_config_t *cfg, const innerq_block_cache_t *cache, int64_t first, int64_t count,
+                      void *k_out, const innerq_strides_t *k_strides, void *v_out, const innerq_strides_t *v_strides,
+                      void *hip_stream);
+
+/* The same with counts and first tokens of every sequence in DEVICE memory: rows i < count with 0 <= first_dev[b] + i <
+ * n_tokens_dev[b] are written, the others left as they were.  first_dev int32 [B], or NULL: 0.  Counts beyond the capacity are
+ * clamped. */
+int innerq_block_read_ragged(const innerq_block_config_t *cfg, const innerq_block_cache_t *cache,
+                             const int32_t *n_tokens_dev, const int32_t *first_dev, int64_t count, void *k_out,
+                             const innerq_strides_t *k_strides, void *v_out, const innerq_strides_t *v_strides,
+                             void *hip_stream);
+
+/* innerq_chunk_attention over such a cache: query i of the t_new new tokens attends to the n cached tokens, as the cache holds them, and
+ * to the new tokens 0 .. i,
+ *   out_i = softmax(q_i [K_cached; k_new_0 .. k_new_i]^T / sqrt(d)) [V_cached; v_new_0 .. v_new_i].
+ * The cache is not modified: a program appends afterwards what it keeps (a single token, a chunk, the accepted part of a
+ * draft).  Any number of query heads per kv head; n may be 0; n + t_new (max_tokens below) is at most capacity_tokens.
+ *   q, out      fp16 rows; out fp32 rows if out_is_fp32 (strides then multiples of 4), not overlapping an input
+ *   workspace   device scratch of innerq_block_workspace_bytes(cfg, t_new) bytes, content undefined; calls that may run at the
+ *               same time need one each
+ * Codes enter the products exactly, statistics and sums are fp32; inputs finite. */
+int innerq_block_attention(const innerq_block_config_t *cfg, const innerq_block_cache_t *cache, const void *k_new,
+                           const innerq_strides_t *k_strides, const void *v_new, const innerq_strides_t *v_strides,
+                           const void *q, const innerq_strides_t *q_strides, int64_t t_new, void *out,
+                           const innerq_strides_t *out_strides, int out_is_fp32, void *workspace, size_t workspace_bytes,
+                           void *hip_stream);
+
+/* The same with the counts of every sequence in DEVICE memory, read only: n_tokens_dev cached, t_new_dev new tokens (0 .. t_new; NULL:
+ * t_new each).  max_tokens (host) bounds n_tokens_dev[b] + t_new_dev[b] and only sizes the launch.  Rows of out beyond a sequence's
+ * count are left as they were.  Counts outside their bounds are clamped on the device. */
+int innerq_block_attention_ragged(const innerq_block_config_t *cfg, const innerq_block_cache_t *cache,
+                                  const int32_t *n_tokens_dev, const int32_t *t_new_dev, int64_t max_tokens,
+                                  const void *k_new, const innerq_strides_t *k_strides, const void *v_new,
+                                  const innerq_strides_t *v_strides, const void *q, const innerq_strides_t *q_strides,
+                                  int64_t t_new, void *out, const innerq_strides_t *out_strides, int out_is_fp32,
+                                  void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Cross attention: the t_new queries of every sequence attend to all of its cached tokens (an encoder's states, appended once),
+ *   out_i = softmax(q_i K_cached^T / sqrt(d)) V_cached,
+ * and a sequence without any has rows of zeros.  Arguments as for innerq_block_attention; t_new may be any number of rows (beams of
+ * a sequence among them), max_tokens bounds n_tokens_dev[b]. */
+int innerq_block_cross_attention(const innerq_block_config_t *cfg, const innerq_block_cache_t *cache, const void *q,
+                                 const innerq_strides_t *q_strides, int64_t t_new, void *out,
+                                 const innerq_strides_t *out_strides, int out_is_fp32, void *workspace,
+                                 size_t workspace_bytes, void *hip_stream);
+int innerq_block_cross_attention_ragged(const innerq_block_config_t *cfg, const innerq_block_cache_t *cache,
+                                        const int32_t *n_tokens_dev, const int32_t *t_new_dev, int64_t max_tokens,
+                                        const void *q, const innerq_strides_t *q_strides, int64_t t_new, void *out,
+                                        const innerq_strides_t *out_strides, int out_is_fp32, void *workspace,
+                                        size_t workspace_bytes, void *hip_stream);
+
 /* Measurement hook (no counterpart in the paper; its Section "Latency" times the fused
  * dequantise-and-multiply kernels on their own, and this lets a benchmark do the same).
  * The next attention call made by the calling host thread (innerq_decode_attention,

@@ -22,6 +22,9 @@ KIND_INNER, KIND_OUTER, KIND_FP16 = 0, 1, 2
 BUFFER_NAMES = ("k_codes", "k_scales", "k_zeros", "v_codes", "v_scales", "v_zeros",
                 "k_sink", "v_sink", "k_recent", "v_recent")
 
+INT8, E4M3 = 0, 1
+BLOCK_BUFFER_NAMES = ("k_codes", "k_scales", "k_open", "v_codes", "v_scales", "v_open")
+
 OK, E_NULL, E_ARG, E_UNSUPPORTED, E_CAPACITY, E_ALIGN, E_WORKSPACE, E_HIP = 0, -1, -2, -3, -4, -5, -6, -7
 
 
@@ -46,6 +49,15 @@ class innerq_strides_t(C.Structure):
 class innerq_rotation_t(C.Structure):
     _fields_ = [("cos_table", C.c_void_p), ("sin_table", C.c_void_p), ("table_positions", C.c_int64),
                 ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("n_axes", C.c_int32), ("pair_axis", C.c_uint8 * 64)]
+
+
+class innerq_block_config_t(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("type", C.c_int32), ("block", C.c_int32), ("capacity_tokens", C.c_int64), ("page_pool_pages", C.c_int64)]
+
+
+class innerq_block_cache_t(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in BLOCK_BUFFER_NAMES] + [("n_tokens", C.c_int64), ("page_table", C.c_void_p)]
 
 
 class InnerQError(RuntimeError):
@@ -123,6 +135,24 @@ def lib() -> C.CDLL:
                                                     C.c_void_p, strp, C.c_int64, C.c_void_p, C.c_void_p, strp, C.c_int, C.c_void_p,
                                                     C.c_size_t, C.c_void_p]
         L.innerq_chunk_attention_ragged.restype = C.c_int
+        bcfgp, bcachep, ptr, i64, size = C.POINTER(innerq_block_config_t), C.POINTER(innerq_block_cache_t), C.c_void_p, C.c_int64, C.c_size_t
+        L.innerq_block_validate_config.argtypes = [bcfgp]
+        L.innerq_block_buffer_bytes.argtypes = [bcfgp, C.c_int]
+        L.innerq_block_buffer_bytes.restype = C.c_size_t
+        L.innerq_block_workspace_bytes.argtypes = [bcfgp, i64]
+        L.innerq_block_workspace_bytes.restype = C.c_size_t
+        rows, result = [ptr, strp], [ptr, strp, C.c_int, ptr, size, ptr]
+        L.innerq_block_append.argtypes = [bcfgp, bcachep, *rows, *rows, i64, ptr]
+        L.innerq_block_append_ragged.argtypes = [bcfgp, bcachep, ptr, ptr, *rows, *rows, i64, ptr]
+        L.innerq_block_read.argtypes = [bcfgp, bcachep, i64, i64, *rows, *rows, ptr]
+        L.innerq_block_read_ragged.argtypes = [bcfgp, bcachep, ptr, ptr, i64, *rows, *rows, ptr]
+        L.innerq_block_attention.argtypes = [bcfgp, bcachep, *rows, *rows, *rows, i64, *result]
+        L.innerq_block_attention_ragged.argtypes = [bcfgp, bcachep, ptr, ptr, i64, *rows, *rows, *rows, i64, *result]
+        L.innerq_block_cross_attention.argtypes = [bcfgp, bcachep, *rows, i64, *result]
+        L.innerq_block_cross_attention_ragged.argtypes = [bcfgp, bcachep, ptr, ptr, i64, *rows, i64, *result]
+        for name in ("validate_config", "append", "append_ragged", "read", "read_ragged", "attention", "attention_ragged",
+                     "cross_attention", "cross_attention_ragged"):
+            getattr(L, "innerq_block_" + name).restype = C.c_int
         L.innerq_profile_next_attention.argtypes = [C.c_void_p, C.c_void_p]
         L.innerq_profile_next_attention.restype = C.c_int
         L.innerq_select_inner_kernel.argtypes = [C.c_int]
@@ -541,6 +571,149 @@ def innerq_chunk_attention_ragged(cache: Cache, n_tokens_dev, t_new_dev, max_tok
                                              workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream))
     if st != OK:
         raise InnerQError(st, "innerq_chunk_attention_ragged")
+    return out
+
+
+# ---- a cache in 8 bits with a scale for each block of tokens and head
+
+def make_block_config(batch, n_q_heads, n_kv_heads, head_dim=128, type=INT8, block=32, capacity_tokens=0,
+                      page_pool_pages=0) -> innerq_block_config_t:
+    return innerq_block_config_t(batch, n_q_heads, n_kv_heads, head_dim, type, block, capacity_tokens, page_pool_pages)
+
+
+def innerq_block_validate_config(cfg: innerq_block_config_t) -> int:
+    return lib().innerq_block_validate_config(C.byref(cfg))
+
+
+def innerq_block_buffer_bytes(cfg: innerq_block_config_t, which: int) -> int:
+    return lib().innerq_block_buffer_bytes(C.byref(cfg), which)
+
+
+def innerq_block_workspace_bytes(cfg: innerq_block_config_t, t_new: int) -> int:
+    return lib().innerq_block_workspace_bytes(C.byref(cfg), t_new)
+
+
+@dataclass
+class BlockCache:
+    """Caller-owned buffers of a cache in 8 bits (torch uint8 tensors on the GPU) plus the C struct that points at them."""
+    cfg: innerq_block_config_t
+    buffers: dict
+    c: innerq_block_cache_t
+
+    @property
+    def n_tokens(self) -> int:
+        return self.c.n_tokens
+
+
+def allocate_block_cache(cfg: innerq_block_config_t, device="cuda", page_table=None) -> BlockCache:
+    """Every buffer of the configuration, zero-filled.  page_table: as for allocate_cache."""
+    import torch
+    st = innerq_block_validate_config(cfg)
+    if st != OK:
+        raise InnerQError(st, "allocate_block_cache")
+    bufs, c = {}, innerq_block_cache_t()
+    for i, name in enumerate(BLOCK_BUFFER_NAMES):
+        bufs[name] = torch.zeros(innerq_block_buffer_bytes(cfg, i), dtype=torch.uint8, device=device)
+        setattr(c, name, _ptr(bufs[name]))
+    if cfg.page_pool_pages > 0:
+        assert page_table is not None and page_table.dtype == torch.int32 and page_table.is_contiguous()
+        assert tuple(page_table.shape) == (cfg.batch, cfg.capacity_tokens // 64)
+        bufs["page_table"] = page_table
+        c.page_table = _ptr(page_table)
+    return BlockCache(cfg, bufs, c)
+
+
+def allocate_block_workspace(cfg: innerq_block_config_t, t_new: int, device="cuda"):
+    import torch
+    return torch.empty(innerq_block_workspace_bytes(cfg, t_new), dtype=torch.uint8, device=device)
+
+
+def _checked(st: int, where: str) -> None:
+    if st != OK:
+        raise InnerQError(st, where)
+
+
+def innerq_block_append(cache: BlockCache, k_new, v_new, stream=None) -> None:
+    """k_new, v_new: fp16 rows [B, Hk, T, d] wherever they lie; a block is packed when its last token arrives."""
+    cfg, T = cache.cfg, k_new.shape[2]
+    _checked(lib().innerq_block_append(C.byref(cfg), C.byref(cache.c), *_rows(k_new, cfg, cfg.n_kv_heads, T),
+                                       *_rows(v_new, cfg, cfg.n_kv_heads, T), T, _stream(stream)), "innerq_block_append")
+
+
+def innerq_block_append_ragged(cache: BlockCache, n_tokens_dev, t_new_dev, k_new, v_new, stream=None) -> None:
+    """innerq_block_append with the counts of every sequence in device memory (int32 CUDA tensors [B]): n_tokens_dev cached,
+    advanced by the call, t_new_dev new ones, at most T (None: T each)."""
+    cfg, T = cache.cfg, k_new.shape[2]
+    _checked(lib().innerq_block_append_ragged(C.byref(cfg), C.byref(cache.c), _counts(n_tokens_dev, cfg), _counts(t_new_dev, cfg),
+                                              *_rows(k_new, cfg, cfg.n_kv_heads, T), *_rows(v_new, cfg, cfg.n_kv_heads, T), T,
+                                              _stream(stream)), "innerq_block_append_ragged")
+
+
+def _wanted_rows(t, cfg, count):
+    return (None, None) if t is None else _rows(t, cfg, cfg.n_kv_heads, count)
+
+
+def innerq_block_read(cache: BlockCache, first: int, k_out=None, v_out=None, stream=None):
+    """Tokens first .. of every sequence into the fp16 rows k_out, v_out [B, Hk, T, d] (either may be None)."""
+    cfg, T = cache.cfg, (v_out if k_out is None else k_out).shape[2]
+    _checked(lib().innerq_block_read(C.byref(cfg), C.byref(cache.c), first, T, *_wanted_rows(k_out, cfg, T), *_wanted_rows(v_out, cfg, T),
+                                     _stream(stream)), "innerq_block_read")
+    return k_out, v_out
+
+
+def innerq_block_read_ragged(cache: BlockCache, n_tokens_dev, first_dev, k_out=None, v_out=None, stream=None):
+    """innerq_block_read with counts and first tokens (None: 0) of every sequence in device memory; rows of tokens that are not there are
+    left as they were."""
+    cfg, T = cache.cfg, (v_out if k_out is None else k_out).shape[2]
+    _checked(lib().innerq_block_read_ragged(C.byref(cfg), C.byref(cache.c), _counts(n_tokens_dev, cfg), _counts(first_dev, cfg), T,
+                                            *_wanted_rows(k_out, cfg, T), *_wanted_rows(v_out, cfg, T), _stream(stream)),
+             "innerq_block_read_ragged")
+    return k_out, v_out
+
+
+def _block_result(cache: BlockCache, q, out, workspace, stream):
+    """The arguments from the queries on, and the output."""
+    cfg, T = cache.cfg, q.shape[2]
+    out = _chunk_out(out, q)
+    return out, (*_rows(q, cfg, cfg.n_q_heads, T), T, *_rows(out, cfg, cfg.n_q_heads, T, out.dtype), int(out.element_size() == 4),
+                 workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream))
+
+
+def innerq_block_attention(cache: BlockCache, k_new, v_new, q, workspace, out=None, stream=None):
+    """q [B, Hq, T, d] attends to the cache and causally to the new rows k_new, v_new [B, Hk, T, d] (not appended by this call)
+    -> out [B, Hq, T, d] (fp32 unless an fp16 `out` is passed)."""
+    cfg, T = cache.cfg, q.shape[2]
+    out, rest = _block_result(cache, q, out, workspace, stream)
+    _checked(lib().innerq_block_attention(C.byref(cfg), C.byref(cache.c), *_rows(k_new, cfg, cfg.n_kv_heads, T),
+                                          *_rows(v_new, cfg, cfg.n_kv_heads, T), *rest), "innerq_block_attention")
+    return out
+
+
+def innerq_block_attention_ragged(cache: BlockCache, n_tokens_dev, t_new_dev, max_tokens: int, k_new, v_new, q, workspace, out=None,
+                                  stream=None):
+    """innerq_block_attention with the counts of every sequence in device memory (int32 CUDA tensors [B]): n_tokens_dev cached, t_new_dev
+    new ones, at most T (None: T each); max_tokens bounds their sum."""
+    cfg, T = cache.cfg, q.shape[2]
+    out, rest = _block_result(cache, q, out, workspace, stream)
+    _checked(lib().innerq_block_attention_ragged(C.byref(cfg), C.byref(cache.c), _counts(n_tokens_dev, cfg), _counts(t_new_dev, cfg),
+                                                 max_tokens, *_rows(k_new, cfg, cfg.n_kv_heads, T),
+                                                 *_rows(v_new, cfg, cfg.n_kv_heads, T), *rest), "innerq_block_attention_ragged")
+    return out
+
+
+def innerq_block_cross_attention(cache: BlockCache, q, workspace, out=None, stream=None):
+    """q [B, Hq, T, d] attends to all cached tokens -> out [B, Hq, T, d] (fp32 unless an fp16 `out` is passed)."""
+    out, rest = _block_result(cache, q, out, workspace, stream)
+    _checked(lib().innerq_block_cross_attention(C.byref(cache.cfg), C.byref(cache.c), *rest), "innerq_block_cross_attention")
+    return out
+
+
+def innerq_block_cross_attention_ragged(cache: BlockCache, n_tokens_dev, t_new_dev, max_tokens: int, q, workspace, out=None, stream=None):
+    """innerq_block_cross_attention with the counts of every sequence in device memory; a sequence without a token has rows of zeros."""
+    cfg = cache.cfg
+    out, rest = _block_result(cache, q, out, workspace, stream)
+    _checked(lib().innerq_block_cross_attention_ragged(C.byref(cfg), C.byref(cache.c), _counts(n_tokens_dev, cfg), _counts(t_new_dev, cfg),
+                                                       max_tokens, *rest), "innerq_block_cross_attention_ragged")
     return out
 
 

@@ -36,6 +36,10 @@ SOURCES = {
     "attention_join_paged_g64.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "attention_chunk.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],
     "attention_chunk_g64.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "api_block.hip": [],
+    # (defined to the bit by single fp32 operations)
+    "block_store.hip": ["-ffp-contract=off"],
+    "attention_block.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],
     "attention_inner_f4.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 

@@ -1,0 +1,455 @@
+// Attention over the cache in 8 bits with block scales: one or a few new tokens of a sequence, and cross attention.
+//
+// A row is a query head of a new token; the rows of a kv head share its keys and values.  A wavefront takes tiles of 32 tokens:
+//   S^T = K Q^T   (16 x 16 x 32 instructions: rows are tokens, columns query rows)
+//   O^T = V^T P^T (rows are channels)
+// The store holds the codes in the order of these operands, so that a wavefront's loads are whole kilobytes, go from memory to registers and
+// are used where they stand: a lane's scores are those of four tokens of either half of the tile and of one query row, which
+// is what the second product wants of it as an operand.  Nothing passes through LDS but the wavefronts' results.
+//
+// Codes become fp16 exactly (8-bit integers: put under the exponent that gives the last bit weight one, the bias subtracted; E4M3: the
+// conversion instruction).  The scale of a block of keys is applied to finished scores, that of a block of values to finished
+// sums of a tile, both in fp32, and weights enter the second product as two fp16 pieces (22 bits), so the result is that of fp32 arithmetic
+// on the values the cache stands for.  The additional instructions are free: the kernel waits for memory.
+//
+// The softmax reference level is put 2^9 below the score that raises it and raised again only when a score passes it by 2^15, so outputs
+// are scaled rarely; the statistics of a row are shared by its four lanes only then.
+#include "block.h"
+
+namespace innerq {
+namespace {
+
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef float float4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int D = kHeadDim;
+// log2 of the weight that the largest score has when it raises the level, and of the largest weight before the level is raised.
+constexpr float kTop = 9.0f, kRaise = 15.0f;
+constexpr float kFar = 0x1p19f;                          // levels beyond: neighbours in fp32 are 2^-4 apart and more
+constexpr float kFarShare = 0x1p-16f;                    // of its own size, by which a level is raised the sooner
+
+__device__ __forceinline__ float row_most(float x) {     // over the four lanes of a query row
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float row_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+// Eight codes as fp16.
+template <bool E4M3>
+__device__ __forceinline__ half8_t expand(uint32_t a, uint32_t b) {
+  half2_t h[4];
+  if constexpr (E4M3) {
+    h[0] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false));
+    h[1] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true));
+    h[2] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, false));
+    h[3] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, true));
+  } else {
+    const half2_t bias = {(_Float16)-1152.f, (_Float16)-1152.f};
+    a ^= 0x80808080u;
+    b ^= 0x80808080u;
+    h[0] = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, a, 0x04010400u)) + bias;
+    h[1] = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, a, 0x04030402u)) + bias;
+    h[2] = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, b, 0x04010400u)) + bias;
+    h[3] = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, b, 0x04030402u)) + bias;
+  }
+  return half8_t{h[0].x, h[0].y, h[1].x, h[1].y, h[2].x, h[2].y, h[3].x, h[3].y};
+}
+
+struct BlockSeq { int n, t, packed; };
+__device__ __forceinline__ BlockSeq block_seq(const BlockAttnArgs& a, int b) {
+  const int cap = (int)a.s.capacity;
+  BlockSeq s = {a.s.n_tokens, a.s.t_new, 0};
+  if (a.s.n_dev) {
+    s.n = a.s.n_dev[b];
+    s.n = s.n < 0 ? 0 : s.n > cap ? cap : s.n;
+    if (a.s.t_dev) s.t = a.s.t_dev[b];
+    s.t = s.t < 0 ? 0 : s.t > a.s.t_new ? a.s.t_new : s.t;
+  }
+  s.packed = (int)block_packed(s.n, a.s.block);
+  return s;
+}
+
+// A wavefront's 16 NR query rows (lane: row lane % 16 of each sixteen; channels 32 (lane / 16) + 8 s + ..): operands, outputs (two
+// accumulators of 4: channels 32 q + 8 (lane / 16) + 2 i + m at o[2 q + m][i]), level, the lane's part of the sum.
+template <int NR>
+struct Rows {
+  half8_t q[NR][4];
+  float4_t o[NR][8];
+  float m[NR], l[NR];
+};
+
+// Weights of the scores of a tile (level and sum move on), in two pieces.  s[r][a][i]: token 16 a + 4 (lane / 16) + i.  by: factor of the scores.
+template <int NR>
+__device__ __forceinline__ void weights(Rows<NR>& r, float4_t (&s)[NR][2], float by, half8_t (&hi)[NR], half8_t (&lo)[NR]) {
+  bool raise = false;
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[n][a][i] *= by;
+        asm("" : "+v"(s[n][a][i]));                      // (rounded before the level is taken from it: far levels need that)
+      }
+    const float top = fmaxf(fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3])), fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3])));
+    raise |= top > __builtin_fmaf(-kFarShare, __builtin_fabsf(r.m[n]), r.m[n]) + kRaise || (r.m[n] == -INFINITY && top > -INFINITY);
+  }
+  if (__builtin_amdgcn_ballot_w64(raise)) {
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      float top = fmaxf(fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3])), fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3])));
+      top = row_most(top);
+      const bool up = top > __builtin_fmaf(-kFarShare, __builtin_fabsf(r.m[n]), r.m[n]) + kRaise || (r.m[n] == -INFINITY && top > -INFINITY);
+      const float level = up ? fmaxf(r.m[n], __builtin_fabsf(top) > kFar ? top : top - kTop) : r.m[n];
+      const float f = up ? __builtin_amdgcn_exp2f(r.m[n] - level) : 1.f;         // (0 from the empty state)
+      r.l[n] *= f;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) r.o[n][x] *= f;
+      r.m[n] = level;
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    const float level = r.m[n] == -INFINITY ? 0.f : r.m[n];                      // (a row that has met no token yet)
+    float sum = 0.f;
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p = __builtin_amdgcn_exp2f(s[n][a][i] - level);
+        hi[n][4 * a + i] = (_Float16)p;
+        lo[n][4 * a + i] = (_Float16)(p - (float)hi[n][4 * a + i]);
+        sum += p;
+      }
+    r.l[n] += sum;
+  }
+}
+
+// One tile's codes as they are loaded, and where they are.
+struct Tile {
+  u32x4 k[4], v[4];
+  float ks, vs;
+};
+
+template <bool E4M3, int NR>
+struct Kernel {
+  static __device__ __forceinline__ void scores(const Rows<NR>& r, const Tile& t, float4_t (&s)[NR][2]) {
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+#pragma unroll
+      for (int n = 0; n < NR; ++n) s[n][a] = float4_t{};
+#pragma unroll
+      for (int st = 0; st < 4; ++st) {
+        const u32x4 w = t.k[2 * a + st / 2];
+        const half8_t k = st & 1 ? expand<E4M3>(w.z, w.w) : expand<E4M3>(w.x, w.y);
+#pragma unroll
+        for (int n = 0; n < NR; ++n) s[n][a] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, r.q[n][st], s[n][a], 0, 0, 0);
+      }
+    }
+  }
+  static __device__ __forceinline__ void values(Rows<NR>& r, const Tile& t, const half8_t (&hi)[NR], const half8_t (&lo)[NR]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const half8_t v = m ? expand<E4M3>(t.v[q].z, t.v[q].w) : expand<E4M3>(t.v[q].x, t.v[q].y);
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+          float4_t c = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, hi[n], float4_t{}, 0, 0, 0);
+          c = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, lo[n], c, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) r.o[n][2 * q + m][i] = __builtin_fmaf(t.vs, c[i], r.o[n][2 * q + m][i]);
+        }
+      }
+  }
+};
+
+// A sequence's fp16 tokens behind the packed ones, in order: the open ones, then the new ones.
+struct Plain {
+  const __half *ko, *vo, *kf, *vf;
+  long long kp, vp;                    // from a new token to the next
+  int open;
+  __device__ __forceinline__ const __half* key(int i) const { return i < open ? ko + i * D : kf + (i - open) * kp; }
+  __device__ __forceinline__ const __half* value(int i) const { return i < open ? vo + i * D : vf + (i - open) * vp; }
+};
+
+template <bool E4M3, int NR>
+__global__ void __launch_bounds__(64 * kBlockWaves) block_attention_kernel(BlockAttnArgs a) {
+  using K = Kernel<E4M3, NR>;
+  constexpr int W = kBlockWaves;
+  __shared__ float lds[W * NR * (32 + 2) * 64];
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
+  const unsigned per = (unsigned)a.row_blocks * (unsigned)a.n_splits;
+  const int bh = (int)(blockIdx.x / per), rest = (int)(blockIdx.x % per), row_block = rest / a.n_splits, split = rest % a.n_splits;
+  const int b = bh / a.s.n_kv_heads, h = bh % a.s.n_kv_heads;
+  const BlockSeq s = block_seq(a, b);
+  const int rows = s.t * a.heads_per_kv, row0 = row_block * 16 * NR;
+  if (row0 >= rows) return;                              // (uniform)
+  Rows<NR> r;
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    const int row = row0 + 16 * n + c, i = row / a.heads_per_kv;
+    const __half* src = a.q.p + b * a.q.batch + (h * a.heads_per_kv + row - i * a.heads_per_kv) * a.q.head + i * a.q.token + 32 * g;
+#pragma unroll
+    for (int st = 0; st < 4; ++st) r.q[n][st] = row < rows ? *reinterpret_cast<const half8_t*>(src + 8 * st) : half8_t{};
+#pragma unroll
+    for (int x = 0; x < 8; ++x) r.o[n][x] = float4_t{};
+    r.m[n] = -INFINITY;
+    r.l[n] = 0.f;
+  }
+  const float scale = 0.08838834764831845f * 1.4426950408889634f;
+
+  // this wavefront's share of the tiles: packed ones, then those of fp16 tokens
+  const bool causal = a.k.p != nullptr;
+  const int last_row = (row0 + 16 * NR < rows ? row0 + 16 * NR : rows) - 1;
+  const int open = s.n - s.packed, plain = open + (causal ? last_row / a.heads_per_kv + 1 : 0);
+  const int tiles1 = s.packed / kBlockTile, tiles = tiles1 + (plain + kBlockTile - 1) / kBlockTile;
+  const int parts = a.n_splits * W, part = split * W + wave, share = tiles / parts, more = tiles % parts;
+  const int t0 = part * share + (part < more ? part : more), t1 = t0 + share + (part < more ? 1 : 0);
+
+  const int u1 = t1 < tiles1 ? t1 : tiles1;
+  if (t0 < u1) {
+    // Where 64 tiles lie, and their scales: a tile a lane.  Tiles are loaded two ahead (behind the last one: that one again).
+    long long at = 0;
+    float ks = 0.f, vs = 0.f;
+    int base = -64;
+    auto load = [&](int u, Tile& t) {
+      u = u < u1 ? u : u1 - 1;
+      if (u >= base + 64 || base < 0) {
+        base = u;
+        const int mine = u + lane < u1 ? u + lane : u1 - 1;
+        at = block_tile(a.s, b, h, mine);
+        const long long sc = block_scale(a.s, at);
+        ks = a.s.k.scales[sc];
+        vs = a.s.v.scales[sc];
+      }
+      const int i = u - base;
+      const long long tile = (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(at >> 32), i) << 32) |
+                                         (unsigned)__builtin_amdgcn_readlane((int)at, i));
+      const u32x4* kp = reinterpret_cast<const u32x4*>(a.s.k.codes + tile * kBlockTileBytes);
+      const u32x4* vp = reinterpret_cast<const u32x4*>(a.s.v.codes + tile * kBlockTileBytes);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) t.k[x] = __builtin_nontemporal_load(kp + 64 * x + lane);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) t.v[x] = __builtin_nontemporal_load(vp + 64 * x + lane);
+      t.ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks), i));
+      t.vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs), i));
+    };
+    auto use = [&](const Tile& t) {
+      float4_t sc[NR][2];
+      half8_t hi[NR], lo[NR];
+      K::scores(r, t, sc);
+      weights<NR>(r, sc, t.ks * scale, hi, lo);
+      K::values(r, t, hi, lo);
+    };
+    Tile x, y;
+    load(t0, x);
+    load(t0 + 1, y);
+    for (int u = t0;;) {
+      use(x);
+      if (++u == u1) break;
+      load(u + 1, x);
+      use(y);
+      if (++u == u1) break;
+      load(u + 1, y);
+    }
+  }
+  if (t1 > tiles1) {
+    Plain p;
+    const long long open_at = (long long)bh * a.s.block * D;
+    p.ko = a.s.k.open + open_at;
+    p.vo = a.s.v.open + open_at;
+    p.kf = a.k.p + b * a.k.batch + h * a.k.head;
+    p.vf = a.v.p + b * a.v.batch + h * a.v.head;
+    p.kp = a.k.token;
+    p.vp = a.v.token;
+    p.open = open;
+    for (int u = t0 > tiles1 ? t0 : tiles1; u < t1; ++u) {
+      const int i0 = (u - tiles1) * kBlockTile;
+      auto token = [&](int i) { return i0 + i < plain ? i0 + i : plain - 1; };    // (behind the last one: that one again, masked)
+      float4_t sc[NR][2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const __half* src = p.key(token(16 * x + c)) + 32 * g;
+#pragma unroll
+        for (int n = 0; n < NR; ++n) sc[n][x] = float4_t{};
+#pragma unroll
+        for (int st = 0; st < 4; ++st) {
+          const half8_t k = *reinterpret_cast<const half8_t*>(src + 8 * st);
+#pragma unroll
+          for (int n = 0; n < NR; ++n) sc[n][x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, r.q[n][st], sc[n][x], 0, 0, 0);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        const int row = row0 + 16 * n + c, limit = causal ? open + (row < rows ? row : rows - 1) / a.heads_per_kv : plain - 1;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (i0 + 16 * x + 4 * g + i > limit) sc[n][x][i] = -INFINITY;
+      }
+      half8_t hi[NR], lo[NR];
+      weights<NR>(r, sc, scale, hi, lo);
+      const __half* vsrc[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) vsrc[j] = p.value(token(16 * (j >> 2) + 4 * g + (j & 3))) + 2 * c;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        uint32_t w[8], e[4], o[4];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = *reinterpret_cast<const uint32_t*>(vsrc[j] + 32 * q);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          e[j] = __builtin_amdgcn_perm(w[2 * j + 1], w[2 * j], 0x05040100u);
+          o[j] = __builtin_amdgcn_perm(w[2 * j + 1], w[2 * j], 0x07060302u);
+        }
+        const half8_t v[2] = {__builtin_bit_cast(half8_t, u32x4{e[0], e[1], e[2], e[3]}), __builtin_bit_cast(half8_t, u32x4{o[0], o[1], o[2], o[3]})};
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int n = 0; n < NR; ++n) {
+            r.o[n][2 * q + m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[m], hi[n], r.o[n][2 * q + m], 0, 0, 0);
+            r.o[n][2 * q + m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[m], lo[n], r.o[n][2 * q + m], 0, 0, 0);
+          }
+      }
+    }
+  }
+
+  // the wavefronts' results meet in LDS; wavefront w joins channels 32 w ..
+  static_assert(W == 4);
+  float* ml = lds + W * NR * 32 * 64;
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+#pragma unroll
+    for (int x = 0; x < 8; ++x)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) lds[((wave * NR + n) * 32 + 4 * x + i) * 64 + lane] = r.o[n][x][i];
+    ml[((wave * NR + n) * 2) * 64 + lane] = r.m[n];
+    ml[((wave * NR + n) * 2 + 1) * 64 + lane] = row_sum(r.l[n]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    float top = -INFINITY, l = 0.f, o[8];
+#pragma unroll
+    for (int w = 0; w < W; ++w) top = fmaxf(top, ml[((w * NR + n) * 2) * 64 + lane]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const float m = ml[((w * NR + n) * 2) * 64 + lane];
+      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+      l = __builtin_fmaf(f, ml[((w * NR + n) * 2 + 1) * 64 + lane], l);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] = __builtin_fmaf(f, lds[((w * NR + n) * 32 + 8 * wave + 4 * (i & 1) + i / 2) * 64 + lane], o[i]);
+    }
+    const int row = row0 + 16 * n + c;
+    if (row >= rows) continue;
+    const int channel = 32 * wave + 8 * g;
+    if (a.n_splits > 1) {
+      const long long slot_row = (long long)blockIdx.x * (16 * NR) + 16 * n + c;
+      float* dst = a.ws + a.slots * (16 * NR * 2) + slot_row * D + channel;
+      *reinterpret_cast<float4*>(dst) = float4{o[0], o[1], o[2], o[3]};
+      *reinterpret_cast<float4*>(dst + 4) = float4{o[4], o[5], o[6], o[7]};
+      if (wave == 0 && g == 0) *reinterpret_cast<float2*>(a.ws + slot_row * 2) = float2{top, l};
+      continue;
+    }
+    const float f = l > 0.f ? 1.0f / l : 0.f;            // (no token: zero)
+    const int i = row / a.heads_per_kv;
+    const long long at = b * a.out_batch + (h * a.heads_per_kv + row - i * a.heads_per_kv) * a.out_head + i * a.out_token + channel;
+    if (a.out_is_fp32) {
+      float* dst = static_cast<float*>(a.out) + at;
+      *reinterpret_cast<float4*>(dst) = float4{o[0] * f, o[1] * f, o[2] * f, o[3] * f};
+      *reinterpret_cast<float4*>(dst + 4) = float4{o[4] * f, o[5] * f, o[6] * f, o[7] * f};
+    } else {
+      half8_t x;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = (_Float16)(o[e] * f);
+      *reinterpret_cast<half8_t*>(static_cast<_Float16*>(a.out) + at) = x;
+    }
+  }
+}
+
+// The splits of a row joined: a wavefront a row, a lane two channels; levels and sums of up to 64 splits a load.
+__global__ void __launch_bounds__(256) block_merge_kernel(BlockAttnArgs a, int blocks, int group_rows) {
+  const int lane = (int)threadIdx.x & 63;
+  const int bh = (int)(blockIdx.x / (unsigned)blocks);
+  const int row = (int)(blockIdx.x % (unsigned)blocks) * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int b = bh / a.s.n_kv_heads, h = bh % a.s.n_kv_heads;
+  if (row >= block_seq(a, b).t * a.heads_per_kv) return;
+  const long long slot_row = ((long long)bh * a.row_blocks + row / group_rows) * a.n_splits * group_rows + row % group_rows;
+  const float* ml = a.ws + slot_row * 2;
+  const float* po = a.ws + a.slots * (group_rows * 2) + slot_row * D + 2 * lane;
+  const long long step_ml = group_rows * 2, step_o = (long long)group_rows * D;
+  float level = -INFINITY, den = 0.f;
+  float2 o = {0.f, 0.f};
+  for (int p0 = 0; p0 < a.n_splits; p0 += 64) {
+    const int count = a.n_splits - p0 < 64 ? a.n_splits - p0 : 64;
+    float2 st = {-INFINITY, 0.f};
+    if (lane < count) st = *reinterpret_cast<const float2*>(ml + (p0 + lane) * step_ml);
+    float top = st.x;
+#pragma unroll
+    for (int x = 32; x > 0; x /= 2) top = fmaxf(top, __shfl_xor(top, x));
+    top = fmaxf(top, level);
+    const float old = level == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(level - top);
+    const float f = st.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.x - top);
+    float sum = f * st.y;
+#pragma unroll
+    for (int x = 32; x > 0; x /= 2) sum += __shfl_xor(sum, x);
+    den = __builtin_fmaf(den, old, sum);
+    o.x *= old;
+    o.y *= old;
+    level = top;
+    for (int p = 0; p < count; p += 8) {                 // (eight partial results under way)
+      float2 v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = *reinterpret_cast<const float2*>(po + (p0 + (p + e < count ? p + e : count - 1)) * step_o);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float w = p + e < count ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), (p + e) & 63)) : 0.f;
+        o.x = __builtin_fmaf(w, v[e].x, o.x);
+        o.y = __builtin_fmaf(w, v[e].y, o.y);
+      }
+    }
+  }
+  const float inv = den > 0.f ? 1.0f / den : 0.f;
+  const int i = row / a.heads_per_kv;
+  const long long at = b * a.out_batch + (h * a.heads_per_kv + row - i * a.heads_per_kv) * a.out_head + i * a.out_token + 2 * lane;
+  if (a.out_is_fp32) *reinterpret_cast<float2*>(static_cast<float*>(a.out) + at) = float2{o.x * inv, o.y * inv};
+  else *reinterpret_cast<half2_t*>(static_cast<_Float16*>(a.out) + at) = half2_t{(_Float16)(o.x * inv), (_Float16)(o.y * inv)};
+}
+
+template <bool E4M3>
+hipError_t launch_rows(const BlockAttnArgs& a, int group_rows, hipStream_t stream) {
+  const long long groups = (long long)a.s.batch * a.s.n_kv_heads * a.row_blocks * a.n_splits;
+  if (groups >= (1LL << 31)) return hipErrorInvalidValue;
+  switch (group_rows) {
+    case 16: block_attention_kernel<E4M3, 1><<<(unsigned)groups, 64 * kBlockWaves, 0, stream>>>(a); break;
+    case 32: block_attention_kernel<E4M3, 2><<<(unsigned)groups, 64 * kBlockWaves, 0, stream>>>(a); break;
+    case 64: block_attention_kernel<E4M3, 4><<<(unsigned)groups, 64 * kBlockWaves, 0, stream>>>(a); break;
+    default: return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_block_attention(const BlockAttnArgs& a, bool e4m3, int group_rows, hipStream_t stream) {
+  return e4m3 ? launch_rows<true>(a, group_rows, stream) : launch_rows<false>(a, group_rows, stream);
+}
+
+hipError_t launch_block_merge(const BlockAttnArgs& a, int group_rows, hipStream_t stream) {
+  const long long blocks = ceil_div((long long)a.s.t_new * a.heads_per_kv, 4), all = (long long)a.s.batch * a.s.n_kv_heads * blocks;
+  if (all >= (1LL << 31)) return hipErrorInvalidValue;
+  block_merge_kernel<<<(unsigned)all, 256, 0, stream>>>(a, (int)blocks, group_rows);
+  return hipGetLastError();
+}
+
+}  // namespace innerq
