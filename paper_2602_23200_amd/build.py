@@ -40,6 +40,7 @@ SOURCES = {
     # (defined to the bit by single fp32 operations)
     "block_store.hip": ["-ffp-contract=off"],
     "attention_block.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "attention_block_rows.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],
     "attention_inner_f4.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 

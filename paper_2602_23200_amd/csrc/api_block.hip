@@ -125,7 +125,9 @@ int attention(const innerq_block_config_t& c, const innerq_block_cache_t& k, con
   a.ws = reinterpret_cast<float*>(static_cast<char*>(workspace) + 256);
   a.slots = sizes.heads * sizes.row_blocks * a.n_splits;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  hipError_t e = launch_block_attention(a, c.type == INNERQ_E4M3, sizes.group_rows, stream);
+  const bool e4m3 = c.type == INNERQ_E4M3;
+  hipError_t e = sizes.group_rows <= kBlockFewRows ? launch_block_attention(a, e4m3, sizes.group_rows, stream)
+                                                   : launch_block_rows(a, e4m3, sizes.group_rows, stream);
   if (e == hipSuccess && a.n_splits > 1) e = launch_block_merge(a, sizes.group_rows, stream);
   return e == hipSuccess ? INNERQ_OK : INNERQ_E_HIP;
 }

@@ -63,6 +63,7 @@ struct BlockAttnArgs {
   long long slots;
 };
 hipError_t launch_block_attention(const BlockAttnArgs& a, bool e4m3, int group_rows, hipStream_t stream);
+hipError_t launch_block_rows(const BlockAttnArgs& a, bool e4m3, int group_rows, hipStream_t stream);
 hipError_t launch_block_merge(const BlockAttnArgs& a, int group_rows, hipStream_t stream);
 
 }  // namespace innerq
