@@ -56,12 +56,7 @@ __device__ __forceinline__ void put_packed(char* buf, int wave, int lane, const 
     *reinterpret_cast<half8_t*>(dst) = expand<E4M3>(k.x, k.y);
     *reinterpret_cast<half8_t*>(dst + 512) = expand<E4M3>(k.z, k.w);
   }
-  half8_t even = expand<E4M3>(v.x, v.y), odd = expand<E4M3>(v.z, v.w);
-  if (shrink != 1.f) {                                   // (uniform, rare)
-    const _Float16 f = (_Float16)shrink;
-    even *= f;
-    odd *= f;
-  }
+  const half8_t even = expand_by<E4M3>(v.x, v.y, shrink), odd = expand_by<E4M3>(v.z, v.w, shrink);
   // (the lane's g is that of value_lane: neighbours in LDS are neighbours in the wavefront)
   const int vg = (g >> 1) | (g & 1) << 1;
   char* dst = buf + kUnitValues + wave * 2048 + (vg & 1) * 512 + c * 16 + (vg >> 1) * 8;
@@ -111,18 +106,6 @@ __device__ __forceinline__ void unit_scores(const char* buf, const State<RG>& r,
     for (int n = 0; n < RG; ++n) s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, r.q[n][st], s[n], 0, 0, 0);
   }
 }
-template <int RG>
-__device__ __forceinline__ void unit_values(const char* buf, State<RG>& r, int lane, const half8_t (&p)[RG][2]) {
-  const char* values = buf + kUnitValues + lane * 16;
-#pragma unroll
-  for (int x = 0; x < 4; ++x)
-#pragma unroll
-    for (int st = 0; st < 2; ++st) {
-      const half8_t v = *reinterpret_cast<const half8_t*>(values + 2048 * x + 1024 * st);
-#pragma unroll
-      for (int n = 0; n < RG; ++n) r.o[n][x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[n][st], r.o[n][x], 0, 0, 0);
-    }
-}
 __device__ __forceinline__ float threshold(float m) { return __builtin_fmaf(-kFarShare, __builtin_fabsf(m), m) + kRaise; }
 // Largest of a lane's scores, as exponents.
 template <int RG>
@@ -149,26 +132,21 @@ __device__ __forceinline__ void raise_levels(State<RG>& r, const float (&tops)[R
     r.m[n] = level;
   }
 }
+// Weights of scores 2 e, 2 e + 1 of every row.
 template <int RG>
-__device__ __forceinline__ void unit_weights(State<RG>& r, float16_t (&s)[RG], const Scales& u, half8_t (&p)[RG][2]) {
+__device__ __forceinline__ void two_weights(int e, const float16_t (&s)[RG], float by, const float (&bias)[RG], half8_t (&p)[RG][2], float (&sum)[RG]) {
 #pragma unroll
   for (int n = 0; n < RG; ++n) {
-    const float bias = u.add - (r.m[n] == -INFINITY ? 0.f : r.m[n]);             // (a row that has met no token yet)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) p[n][i / 8][i % 8] = (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i], u.by, bias));
-    float sum = 0.f;
-#pragma unroll
-    for (int st = 0; st < 2; ++st)
-#pragma unroll
-      for (int e = 0; e < 8; e += 2)
-        sum = __builtin_amdgcn_fdot2(half2_t{p[n][st][e], p[n][st][e + 1]}, half2_t{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
-    r.l[n] = __builtin_fmaf(sum, u.inv, r.l[n]);
+    const half2_t w = {(_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[n][2 * e], by, bias[n])), (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[n][2 * e + 1], by, bias[n]))};
+    p[n][e / 4][2 * (e % 4)] = w.x;
+    p[n][e / 4][2 * (e % 4) + 1] = w.y;
+    sum[n] = __builtin_amdgcn_fdot2(w, half2_t{(_Float16)1.0f, (_Float16)1.0f}, sum[n], false);
   }
 }
 
 // Units u0 .. u1 of one kind.  load(u, regs): bring a unit's bytes into registers (and remember where); put(buffer, regs, scales): into LDS;
 // scales(u); mask(u, scores): scores of tokens that a row does not attend to are -infinity.
-template <int RG, typename Load, typename Put, typename Of, typename Mask>
+template <int RG, bool MASKED, typename Load, typename Put, typename Of, typename Mask>
 __device__ __forceinline__ void walk(int u0, int u1, char* lds, State<RG>& r, int lane, Load load, Put put, Of of, Mask mask) {
   if (u0 >= u1) return;
   auto at = [&](int u) { return lds + ((u - u0) % kUnits) * kUnitBytes; };
@@ -186,10 +164,13 @@ __device__ __forceinline__ void walk(int u0, int u1, char* lds, State<RG>& r, in
   float16_t s[RG], t[RG];
   float top[RG];
   unit_scores<RG>(at(u0), r, lane, s);
-  mask(u0, s);
+  if (MASKED) mask(u0, s);
   unit_tops<RG>(s, now, top);
   // s: scores of unit u; x: unit u + 2
   auto step = [&](int u, float16_t (&s)[RG], float16_t (&t)[RG], Staged& x, Scales& sx) {
+    half8_t k[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) k[e] = *reinterpret_cast<const half8_t*>(at(u + 1) + lane * 16 + 1024 * e);
     bool raise = false, far = false;
 #pragma unroll
     for (int n = 0; n < RG; ++n) raise |= top[n] > threshold(r.m[n]);
@@ -208,17 +189,47 @@ __device__ __forceinline__ void walk(int u0, int u1, char* lds, State<RG>& r, in
       now.by = 1.f;
       now.add = 0.f;
     }
-    half8_t p[RG][2];
-    unit_scores<RG>(at(u + 1), r, lane, t);
-    unit_weights<RG>(r, s, now, p);
-    unit_values<RG>(at(u), r, lane, p);
+    // the scores of the next unit and the weights of this one, piece by piece; operands of the second product on their way
+    half8_t p[RG][2], v[8];
+    float bias[RG], sum[RG];
+#pragma unroll
+    for (int n = 0; n < RG; ++n) {
+      bias[n] = now.add - (r.m[n] == -INFINITY ? 0.f : r.m[n]);                  // (a row that has met no token yet)
+      sum[n] = 0.f;
+      t[n] = float16_t{};
+    }
+    const char* values = at(u) + kUnitValues + lane * 16;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+#pragma unroll
+      for (int n = 0; n < RG; ++n) t[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[e], r.q[n][e], t[n], 0, 0, 0);
+      v[e] = *reinterpret_cast<const half8_t*>(values + 2048 * (e % 4) + 1024 * (e / 4));
+      two_weights<RG>(e, s, now.by, bias, p, sum);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int n = 0; n < RG; ++n) r.l[n] = __builtin_fmaf(sum[n], now.inv, r.l[n]);
+    // the second product; a unit into LDS, the largest of the next scores
     put(at(u + 2), x, sx);
     now = next;
     next = sx;
+    if (!MASKED) unit_tops<RG>(t, now, top);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int n = 0; n < RG; ++n) r.o[n][e % 4] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[e], p[n][e / 4], r.o[n][e % 4], 0, 0, 0);
+#pragma unroll
+    for (int e = 0; e < 8 * RG; ++e) {
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x2, 12 / RG, 0);
+    }
+    if (MASKED) {
+      mask(bound(u + 1), t);
+      unit_tops<RG>(t, now, top);
+    }
     load(bound(u + 4), x);
     sx = of(bound(u + 4));
-    mask(bound(u + 1), t);
-    unit_tops<RG>(t, now, top);
     __syncthreads();
   };
   for (int u = u0;;) {
@@ -312,7 +323,7 @@ block_rows_kernel(BlockAttnArgs a) {
       x.a = *(reinterpret_cast<const u32x4*>(a.s.k.codes + tile * kBlockTileBytes) + 64 * wave + lane);
       x.b = *(reinterpret_cast<const u32x4*>(a.s.v.codes + tile * kBlockTileBytes) + 64 * wave + value_lane(lane));
     };
-    walk<RG>(t0, u1, lds, r, lane, load, [&](char* buf, const Staged& x, const Scales& sc) { put_packed<E4M3>(buf, wave, lane, x.a, x.b, sc.shrink); }, of,
+    walk<RG, false>(t0, u1, lds, r, lane, load, [&](char* buf, const Staged& x, const Scales& sc) { put_packed<E4M3>(buf, wave, lane, x.a, x.b, sc.shrink); }, of,
              [](int, float16_t (&)[RG]) {});
   }
   if (t1 > tiles1) {
@@ -341,12 +352,13 @@ block_rows_kernel(BlockAttnArgs a) {
       const int row = row0 + 32 * (RG * wave + n) + (lane & 31);
       limit[n] = causal ? open + (row < rows ? row : rows - 1) / a.heads_per_kv : plain - 1;
     }
-    walk<RG>(t0 > tiles1 ? t0 - tiles1 : 0, t1 - tiles1, lds, r, lane, load, [&](char* buf, const Staged& x, const Scales&) { put_plain(buf, tid, x); },
+    walk<RG, true>(t0 > tiles1 ? t0 - tiles1 : 0, t1 - tiles1, lds, r, lane, load, [&](char* buf, const Staged& x, const Scales&) { put_plain(buf, tid, x); },
              [&](int) { return Scales{scale, 0.f, 1.f, 1.f}; },
              [&](int u, float16_t (&sc)[RG]) {
 #pragma unroll
                for (int n = 0; n < RG; ++n) {
                  const int left = limit[n] - u * kBlockTile - 4 * half;
+                 if (!__builtin_amdgcn_ballot_w64(left < kBlockTile - 1)) continue;
 #pragma unroll
                  for (int i = 0; i < 16; ++i)
                    if (8 * (i / 4) + i % 4 > left) sc[n][i] = -INFINITY;

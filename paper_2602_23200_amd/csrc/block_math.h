@@ -16,15 +16,15 @@ constexpr float kTop = 9.0f, kRaise = 15.0f;
 constexpr float kFar = 0x1p19f;                          // levels beyond: neighbours in fp32 are 2^-4 apart and more
 constexpr float kFarShare = 0x1p-16f;                    // of its own size, by which a level is raised the sooner
 
-// Eight codes as fp16.
+// Eight codes as fp16, times a power of two.
 template <bool E4M3>
-__device__ __forceinline__ half8_t expand(uint32_t a, uint32_t b) {
+__device__ __forceinline__ half8_t expand_by(uint32_t a, uint32_t b, float by) {
   half2_t h[4];
   if constexpr (E4M3) {
-    h[0] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false));
-    h[1] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true));
-    h[2] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, false));
-    h[3] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, true));
+    h[0] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, by, false));
+    h[1] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, by, true));
+    h[2] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, by, false));
+    h[3] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, by, true));
   } else {
     const half2_t bias = {(_Float16)-1152.f, (_Float16)-1152.f};
     a ^= 0x80808080u;
@@ -34,8 +34,11 @@ __device__ __forceinline__ half8_t expand(uint32_t a, uint32_t b) {
     h[2] = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, b, 0x04010400u)) + bias;
     h[3] = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, b, 0x04030402u)) + bias;
   }
-  return half8_t{h[0].x, h[0].y, h[1].x, h[1].y, h[2].x, h[2].y, h[3].x, h[3].y};
+  const half8_t x = {h[0].x, h[0].y, h[1].x, h[1].y, h[2].x, h[2].y, h[3].x, h[3].y};
+  return E4M3 ? x : x * (_Float16)by;
 }
+template <bool E4M3>
+__device__ __forceinline__ half8_t expand(uint32_t a, uint32_t b) { return expand_by<E4M3>(a, b, 1.f); }
 
 struct BlockSeq { int n, t, packed; };
 __device__ __forceinline__ BlockSeq block_seq(const BlockAttnArgs& a, int b) {
