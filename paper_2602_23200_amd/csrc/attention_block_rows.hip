@@ -40,7 +40,9 @@ template <int RG>
 struct State {
   half8_t q[RG][8];
   float16_t o[RG][4];
-  float m[RG], l[RG];
+  float m[RG], l[RG];                  // level, the lane's part of the sum
+  float zero[RG], raise[RG];           // the level (0: none yet), and what raises it
+  bool far;                            // some row's level is
 };
 
 // ---- a unit on its way into LDS
@@ -120,17 +122,22 @@ __device__ __forceinline__ void unit_tops(const float16_t (&s)[RG], const Scales
 }
 template <int RG>
 __device__ __forceinline__ void raise_levels(State<RG>& r, const float (&tops)[RG]) {
+  bool far = false;
 #pragma unroll
   for (int n = 0; n < RG; ++n) {
     const float top = fmaxf(tops[n], other_half(tops[n]));
-    const bool up = top > threshold(r.m[n]);
+    const bool up = top > r.raise[n];
     const float level = up ? fmaxf(r.m[n], __builtin_fabsf(top) > kFar ? top : top - kTop) : r.m[n];
     const float f = up ? __builtin_amdgcn_exp2f(r.m[n] - level) : 1.f;           // (0 from the empty state)
     r.l[n] *= f;
 #pragma unroll
     for (int x = 0; x < 4; ++x) r.o[n][x] *= f;
     r.m[n] = level;
+    r.zero[n] = level == -INFINITY ? 0.f : level;
+    r.raise[n] = threshold(level);
+    far |= __builtin_fabsf(r.zero[n]) > kFar;
   }
+  r.far = __builtin_amdgcn_ballot_w64(far) != 0;
 }
 // Weights of scores 2 e, 2 e + 1 of every row.
 template <int RG>
@@ -144,40 +151,49 @@ __device__ __forceinline__ void two_weights(int e, const float16_t (&s)[RG], flo
   }
 }
 
-// Units u0 .. u1 of one kind.  load(u, regs): bring a unit's bytes into registers (and remember where); put(buffer, regs, scales): into LDS;
-// scales(u); mask(u, scores): scores of tokens that a row does not attend to are -infinity.
-template <int RG, bool MASKED, typename Load, typename Put, typename Of, typename Mask>
-__device__ __forceinline__ void walk(int u0, int u1, char* lds, State<RG>& r, int lane, Load load, Put put, Of of, Mask mask) {
+// Units u0 .. u1 of one kind.  fetch(u, regs, scales): a unit's bytes into registers, and its scales; put(buffer, regs, scales): into LDS; mask(u,
+// scores): scores of tokens that a row does not attend to are -infinity.
+template <int RG, bool MASKED, typename Fetch, typename Put, typename Mask>
+__device__ __forceinline__ void walk(int u0, int u1, char* lds, State<RG>& r, int lane, Fetch fetch, Put put, Mask mask) {
   if (u0 >= u1) return;
   auto at = [&](int u) { return lds + ((u - u0) % kUnits) * kUnitBytes; };
   auto bound = [&](int u) { return u < u1 ? u : u1 - 1; };      // (behind the last unit: that one again)
   Staged x, y;
-  Scales now = of(u0), next = of(bound(u0 + 1)), sx, sy;
-  // units u0 and u0 + 1 into LDS, u0 + 2 and u0 + 3 under way
-  load(u0, x); sx = now;
-  load(bound(u0 + 1), y); sy = next;
-  put(at(u0), x, sx);
-  load(bound(u0 + 2), x); sx = of(bound(u0 + 2));
-  put(at(u0 + 1), y, sy);
-  load(bound(u0 + 3), y); sy = of(bound(u0 + 3));
+  Scales now, next, third, sx, sy;
+  // units u0 .. u0 + 2 into LDS, u0 + 3 and u0 + 4 under way
+  fetch(u0, x, now);
+  fetch(bound(u0 + 1), y, next);
+  put(at(u0), x, now);
+  fetch(bound(u0 + 2), x, third);
+  put(at(u0 + 1), y, next);
+  fetch(bound(u0 + 3), y, sy);
+  put(at(u0 + 2), x, third);
+  fetch(bound(u0 + 4), x, sx);
   __syncthreads();
+  half8_t k[8];
+  auto keys = [&](int u) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) k[e] = *reinterpret_cast<const half8_t*>(at(u) + lane * 16 + 1024 * e);
+  };
   float16_t s[RG], t[RG];
   float top[RG];
-  unit_scores<RG>(at(u0), r, lane, s);
+  keys(u0);
+#pragma unroll
+  for (int n = 0; n < RG; ++n) s[n] = float16_t{};
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+#pragma unroll
+    for (int n = 0; n < RG; ++n) s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[e], r.q[n][e], s[n], 0, 0, 0);
+  keys(u0 + 1);
   if (MASKED) mask(u0, s);
   unit_tops<RG>(s, now, top);
-  // s: scores of unit u; x: unit u + 2
+  // s: scores of unit u; k: keys of unit u + 1; x: unit u + 3
   auto step = [&](int u, float16_t (&s)[RG], float16_t (&t)[RG], Staged& x, Scales& sx) {
-    half8_t k[8];
+    bool raise = false;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) k[e] = *reinterpret_cast<const half8_t*>(at(u + 1) + lane * 16 + 1024 * e);
-    bool raise = false, far = false;
-#pragma unroll
-    for (int n = 0; n < RG; ++n) raise |= top[n] > threshold(r.m[n]);
+    for (int n = 0; n < RG; ++n) raise |= top[n] > r.raise[n];
     if (__builtin_amdgcn_ballot_w64(raise)) raise_levels<RG>(r, top);
-#pragma unroll
-    for (int n = 0; n < RG; ++n) far |= __builtin_fabsf(r.m[n]) > kFar && r.m[n] != -INFINITY;
-    if (__builtin_amdgcn_ballot_w64(far)) {
+    if (r.far) {
       // (the fused form takes the level, which is rounded, from an exact product)
 #pragma unroll
       for (int n = 0; n < RG; ++n)
@@ -194,7 +210,7 @@ __device__ __forceinline__ void walk(int u0, int u1, char* lds, State<RG>& r, in
     float bias[RG], sum[RG];
 #pragma unroll
     for (int n = 0; n < RG; ++n) {
-      bias[n] = now.add - (r.m[n] == -INFINITY ? 0.f : r.m[n]);                  // (a row that has met no token yet)
+      bias[n] = now.add - r.zero[n];
       sum[n] = 0.f;
       t[n] = float16_t{};
     }
@@ -210,10 +226,12 @@ __device__ __forceinline__ void walk(int u0, int u1, char* lds, State<RG>& r, in
     }
 #pragma unroll
     for (int n = 0; n < RG; ++n) r.l[n] = __builtin_fmaf(sum[n], now.inv, r.l[n]);
-    // the second product; a unit into LDS, the largest of the next scores
-    put(at(u + 2), x, sx);
+    // the second product; the keys after the next, a unit into LDS, the largest of the next scores
+    keys(u + 2);
+    put(at(u + 3), x, sx);
     now = next;
-    next = sx;
+    next = third;
+    third = sx;
     if (!MASKED) unit_tops<RG>(t, now, top);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
@@ -222,20 +240,20 @@ __device__ __forceinline__ void walk(int u0, int u1, char* lds, State<RG>& r, in
 #pragma unroll
     for (int e = 0; e < 8 * RG; ++e) {
       __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2 / RG, 0);
       __builtin_amdgcn_sched_group_barrier(0x2, 12 / RG, 0);
     }
     if (MASKED) {
       mask(bound(u + 1), t);
       unit_tops<RG>(t, now, top);
     }
-    load(bound(u + 4), x);
-    sx = of(bound(u + 4));
+    fetch(bound(u + 5), x, sx);
     __syncthreads();
   };
   for (int u = u0;;) {
-    step(u, s, t, x, sx);
+    step(u, s, t, y, sy);
     if (++u == u1) break;
-    step(u, t, s, y, sy);
+    step(u, t, s, x, sx);
     if (++u == u1) break;
   }
 }
@@ -267,9 +285,10 @@ block_rows_kernel(BlockAttnArgs a) {
     for (int st = 0; st < 8; ++st) r.q[n][st] = row < rows ? *reinterpret_cast<const half8_t*>(src + 16 * st) : half8_t{};
 #pragma unroll
     for (int x = 0; x < 4; ++x) r.o[n][x] = float16_t{};
-    r.m[n] = -INFINITY;
-    r.l[n] = 0.f;
+    r.m[n] = r.raise[n] = -INFINITY;
+    r.l[n] = r.zero[n] = 0.f;
   }
+  r.far = false;
   const float scale = 0.08838834764831845f * 1.4426950408889634f;
 
   const bool causal = a.k.p != nullptr;
@@ -310,27 +329,25 @@ block_rows_kernel(BlockAttnArgs a) {
       inv = 1.0f / eff;
     };
     auto lane_of = [&](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
-    auto of = [&](int u) {
-      look(u);
-      const int i = u - base;
-      return Scales{lane_of(by, i), lane_of(add, i), lane_of(inv, i), lane_of(shrink, i)};
-    };
-    auto load = [&](int u, Staged& x) {
+    const uint32_t k_at = (uint32_t)(64 * wave + lane) * 16, v_at = (uint32_t)(64 * wave + value_lane(lane)) * 16;
+    auto fetch = [&](int u, Staged& x, Scales& sc) {
       look(u);
       const int i = u - base;
       const long long tile = (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(at >> 32), i) << 32) |
-                                         (unsigned)__builtin_amdgcn_readlane((int)at, i));
-      x.a = *(reinterpret_cast<const u32x4*>(a.s.k.codes + tile * kBlockTileBytes) + 64 * wave + lane);
-      x.b = *(reinterpret_cast<const u32x4*>(a.s.v.codes + tile * kBlockTileBytes) + 64 * wave + value_lane(lane));
+                                         (unsigned)__builtin_amdgcn_readlane((int)at, i)) * kBlockTileBytes;
+      x.a = *reinterpret_cast<const u32x4*>(a.s.k.codes + tile + k_at);
+      x.b = *reinterpret_cast<const u32x4*>(a.s.v.codes + tile + v_at);
+      sc = Scales{lane_of(by, i), lane_of(add, i), lane_of(inv, i), lane_of(shrink, i)};
     };
-    walk<RG, false>(t0, u1, lds, r, lane, load, [&](char* buf, const Staged& x, const Scales& sc) { put_packed<E4M3>(buf, wave, lane, x.a, x.b, sc.shrink); }, of,
-             [](int, float16_t (&)[RG]) {});
+    walk<RG, false>(t0, u1, lds, r, lane, fetch, [&](char* buf, const Staged& x, const Scales& sc) { put_packed<E4M3>(buf, wave, lane, x.a, x.b, sc.shrink); },
+                    [](int, float16_t (&)[RG]) {});
   }
   if (t1 > tiles1) {
     const long long open_at = (long long)bh * a.s.block * D;
     const __half *ko = a.s.k.open + open_at, *vo = a.s.v.open + open_at;
     const __half *kf = a.k.p + b * a.k.batch + h * a.k.head, *vf = a.v.p + b * a.v.batch + h * a.v.head;
-    auto load = [&](int u, Staged& x) {
+    auto fetch = [&](int u, Staged& x, Scales& sc) {
+      sc = Scales{scale, 0.f, 1.f, 1.f};
       const int i0 = u * kBlockTile;
       auto token = [&](int i) { return i0 + i < plain ? i0 + i : plain - 1; };   // (behind the last one: that one again, masked)
       const int i = token(tid >> 3);
@@ -352,8 +369,7 @@ block_rows_kernel(BlockAttnArgs a) {
       const int row = row0 + 32 * (RG * wave + n) + (lane & 31);
       limit[n] = causal ? open + (row < rows ? row : rows - 1) / a.heads_per_kv : plain - 1;
     }
-    walk<RG, true>(t0 > tiles1 ? t0 - tiles1 : 0, t1 - tiles1, lds, r, lane, load, [&](char* buf, const Staged& x, const Scales&) { put_plain(buf, tid, x); },
-             [&](int) { return Scales{scale, 0.f, 1.f, 1.f}; },
+    walk<RG, true>(t0 > tiles1 ? t0 - tiles1 : 0, t1 - tiles1, lds, r, lane, fetch, [&](char* buf, const Staged& x, const Scales&) { put_plain(buf, tid, x); },
              [&](int u, float16_t (&sc)[RG]) {
 #pragma unroll
                for (int n = 0; n < RG; ++n) {

@@ -26,16 +26,16 @@ __device__ __forceinline__ half8_t expand_by(uint32_t a, uint32_t b, float by) {
     h[2] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, by, false));
     h[3] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, by, true));
   } else {
-    const half2_t bias = {(_Float16)-1152.f, (_Float16)-1152.f};
+    // (1024 + 128 + code under the exponent of 1024; exact for every power of two up to 1)
+    const half2_t f = {(_Float16)by, (_Float16)by}, bias = f * (_Float16)-1152.f;
     a ^= 0x80808080u;
     b ^= 0x80808080u;
-    h[0] = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, a, 0x04010400u)) + bias;
-    h[1] = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, a, 0x04030402u)) + bias;
-    h[2] = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, b, 0x04010400u)) + bias;
-    h[3] = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, b, 0x04030402u)) + bias;
+    h[0] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, a, 0x04010400u)), f, bias);
+    h[1] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, a, 0x04030402u)), f, bias);
+    h[2] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, b, 0x04010400u)), f, bias);
+    h[3] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, b, 0x04030402u)), f, bias);
   }
-  const half8_t x = {h[0].x, h[0].y, h[1].x, h[1].y, h[2].x, h[2].y, h[3].x, h[3].y};
-  return E4M3 ? x : x * (_Float16)by;
+  return half8_t{h[0].x, h[0].y, h[1].x, h[1].y, h[2].x, h[2].y, h[3].x, h[3].y};
 }
 template <bool E4M3>
 __device__ __forceinline__ half8_t expand(uint32_t a, uint32_t b) { return expand_by<E4M3>(a, b, 1.f); }
