@@ -136,16 +136,23 @@ struct Plain {
 };
 
 template <bool E4M3, int NR>
-__global__ void __launch_bounds__(64 * kBlockWaves) block_attention_kernel(BlockAttnArgs a) {
+__global__ void __launch_bounds__(64 * kBlockWaves) __attribute__((amdgpu_waves_per_eu(NR == 4 ? 1 : 2))) block_attention_kernel(BlockAttnArgs a) {
   using K = Kernel<E4M3, NR>;
   constexpr int W = kBlockWaves;
   __shared__ float lds[W * NR * (32 + 2) * 64];
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
-  const unsigned per = (unsigned)a.row_blocks * (unsigned)a.n_splits;
-  const int bh = (int)(blockIdx.x / per), rest = (int)(blockIdx.x % per), row_block = rest / a.n_splits, split = rest % a.n_splits;
-  const int b = bh / a.s.n_kv_heads, h = bh % a.s.n_kv_heads;
+  BlockWork work;
+  if (a.table) {
+    if (!find_work<16 * NR>(a, work)) return;            // (uniform)
+  } else {
+    const unsigned per = (unsigned)a.row_blocks * (unsigned)a.n_splits, bh = blockIdx.x / per, rest = blockIdx.x % per;
+    work = {(int)(bh / (unsigned)a.s.n_kv_heads), (int)(bh % (unsigned)a.s.n_kv_heads), (int)(rest / (unsigned)a.n_splits),
+            (int)(rest % (unsigned)a.n_splits), a.n_splits, (long long)blockIdx.x};
+  }
+  const int b = work.b, h = work.h;
+  const long long bh = (long long)b * a.s.n_kv_heads + h;
   const BlockSeq s = block_seq(a, b);
-  const int rows = s.t * a.heads_per_kv, row0 = row_block * 16 * NR;
+  const int rows = s.t * a.heads_per_kv, row0 = work.row_block * 16 * NR;
   if (row0 >= rows) return;                              // (uniform)
   Rows<NR> r;
 #pragma unroll
@@ -166,7 +173,7 @@ __global__ void __launch_bounds__(64 * kBlockWaves) block_attention_kernel(Block
   const int last_row = (row0 + 16 * NR < rows ? row0 + 16 * NR : rows) - 1;
   const int open = s.n - s.packed, plain = open + (causal ? last_row / a.heads_per_kv + 1 : 0);
   const int tiles1 = s.packed / kBlockTile, tiles = tiles1 + (plain + kBlockTile - 1) / kBlockTile;
-  const int parts = a.n_splits * W, part = split * W + wave, share = tiles / parts, more = tiles % parts;
+  const int parts = work.n_splits * W, part = work.split * W + wave, share = tiles / parts, more = tiles % parts;
   const int t0 = part * share + (part < more ? part : more), t1 = t0 + share + (part < more ? 1 : 0);
 
   const int u1 = t1 < tiles1 ? t1 : tiles1;
@@ -218,7 +225,7 @@ __global__ void __launch_bounds__(64 * kBlockWaves) block_attention_kernel(Block
   }
   if (t1 > tiles1) {
     Plain p;
-    const long long open_at = (long long)bh * a.s.block * D;
+    const long long open_at = bh * a.s.block * D;
     p.ko = a.s.k.open + open_at;
     p.vo = a.s.v.open + open_at;
     p.kf = a.k.p + b * a.k.batch + h * a.k.head;
@@ -309,8 +316,8 @@ __global__ void __launch_bounds__(64 * kBlockWaves) block_attention_kernel(Block
     const int row = row0 + 16 * n + c;
     if (row >= rows) continue;
     const int channel = 32 * wave + 8 * g;
-    if (a.n_splits > 1) {
-      const long long slot_row = (long long)blockIdx.x * (16 * NR) + 16 * n + c;
+    if (work.n_splits > 1) {
+      const long long slot_row = work.slot * (16 * NR) + 16 * n + c;
       float* dst = a.ws + a.slots * (16 * NR * 2) + slot_row * D + channel;
       *reinterpret_cast<float4*>(dst) = float4{o[0], o[1], o[2], o[3]};
       *reinterpret_cast<float4*>(dst + 4) = float4{o[4], o[5], o[6], o[7]};
@@ -339,15 +346,35 @@ __global__ void __launch_bounds__(256) block_merge_kernel(BlockAttnArgs a, int b
   const int bh = (int)(blockIdx.x / (unsigned)blocks);
   const int row = (int)(blockIdx.x % (unsigned)blocks) * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int b = bh / a.s.n_kv_heads, h = bh % a.s.n_kv_heads;
-  if (row >= block_seq(a, b).t * a.heads_per_kv) return;
-  const long long slot_row = ((long long)bh * a.row_blocks + row / group_rows) * a.n_splits * group_rows + row % group_rows;
-  const float* ml = a.ws + slot_row * 2;
-  const float* po = a.ws + a.slots * (group_rows * 2) + slot_row * D + 2 * lane;
-  const long long step_ml = group_rows * 2, step_o = (long long)group_rows * D;
+  int step_rows;                                         // rows from one split to the next
+  const int own = block_seq(a, b).t * a.heads_per_kv;
+  if (row >= own) return;
+  int n_splits = a.n_splits;
+  const float* ws = a.ws;
+  long long slots = a.slots, slot_row;
+  if (a.table) {
+    n_splits = a.table[2 * b + 1];
+    if (n_splits == 1) return;                           // (written already)
+    const bool few = own <= a.few_most;
+    if (few) {
+      group_rows = a.few_rows;
+      ws = a.ws_few;
+    }
+    slots = kBlockListItems;
+    const int blocks_of = (own + group_rows - 1) / group_rows;
+    slot_row = ((long long)a.table[2 * b] + (long long)h * blocks_of * n_splits + row / group_rows) * group_rows + row % group_rows;
+    step_rows = blocks_of * group_rows;
+  } else {
+    slot_row = ((long long)bh * a.row_blocks + row / group_rows) * n_splits * group_rows + row % group_rows;
+    step_rows = group_rows;
+  }
+  const float* ml = ws + slot_row * 2;
+  const float* po = ws + slots * (group_rows * 2) + slot_row * D + 2 * lane;
+  const long long step_ml = step_rows * 2, step_o = (long long)step_rows * D;
   float level = -INFINITY, den = 0.f;
   float2 o = {0.f, 0.f};
-  for (int p0 = 0; p0 < a.n_splits; p0 += 64) {
-    const int count = a.n_splits - p0 < 64 ? a.n_splits - p0 : 64;
+  for (int p0 = 0; p0 < n_splits; p0 += 64) {
+    const int count = n_splits - p0 < 64 ? n_splits - p0 : 64;
     float2 st = {-INFINITY, 0.f};
     if (lane < count) st = *reinterpret_cast<const float2*>(ml + (p0 + lane) * step_ml);
     float top = st.x;
@@ -384,7 +411,7 @@ __global__ void __launch_bounds__(256) block_merge_kernel(BlockAttnArgs a, int b
 
 template <bool E4M3>
 hipError_t launch_rows(const BlockAttnArgs& a, int group_rows, hipStream_t stream) {
-  const long long groups = (long long)a.s.batch * a.s.n_kv_heads * a.row_blocks * a.n_splits;
+  const long long groups = a.table ? a.list_groups : (long long)a.s.batch * a.s.n_kv_heads * a.row_blocks * a.n_splits;
   if (groups >= (1LL << 31)) return hipErrorInvalidValue;
   switch (group_rows) {
     case 16: block_attention_kernel<E4M3, 1><<<(unsigned)groups, 64 * kBlockWaves, 0, stream>>>(a); break;

@@ -1,15 +1,15 @@
 // Attention over the cache in 8 bits with block scales, many rows of a kv head (chunks of a prompt, a decoder's prompt).
 //
-// A work-group of four wavefronts, one a SIMD, has 128 RG rows of a kv head, 32 RG of them a wavefront, and walks over the tokens in units of 32:
+// A work-group of eight wavefronts (or four) has 32 rows of a kv head a wavefront and walks over the tokens in units of 32:
 //   S^T = K Q^T   (32 x 32 x 16 instructions: rows are tokens, columns query rows)
 //   O^T = V^T P^T (rows are channels)
-// Every unit is brought to fp16 once, in LDS, in the order of the operands (a wavefront's reads are whole kilobytes), a wavefront a quarter of it.
-// A lane's scores are those of 16 tokens of one query row (two: RG = 2), which, as weights rounded to fp16, are the second product's operand
-// where they stand.
+// Every unit is brought to fp16 once, in LDS, in the order of the operands (a wavefront's reads are whole kilobytes), an equal part of it by every
+// wavefront.  A lane's scores are those of 16 tokens of one query row, which, as weights rounded to fp16, are the second product's operand where
+// they stand.
 //
-// Matrix and vector instructions are to run side by side: the scores of the next unit are formed while the weights of this one are, and what
-// is left of the vector work, the next unit's level and the decoding of the one after it, stands between the matrix instructions of the
-// second product.  That wants 400 registers, so there is one wavefront a SIMD.
+// Matrix and vector instructions run side by side: the scores of the next unit are formed while the weights of this one are, and what
+// is left of the vector work, the next unit's level and the decoding of the one after, stands between the matrix instructions of the
+// second product, with the keys of the unit after the next on their way to registers.
 //
 // Codes are exact in fp16.  The scale of a block of keys is a factor of its scores, that of a block of values a summand of the exponent,
 // so a weight carries it: w = 2^(s + log2 S_v - level), O = sum w code, and the normaliser is l = sum w / S_v of the same rounded weights.  A block
@@ -36,57 +36,51 @@ __device__ __forceinline__ float other_half(float x) {   // lane ^ 32
 // What is uniform over a unit: factor of the scores, summand of the exponent, 1 / S_v, 2^-k.
 struct Scales { float by, add, inv, shrink; };
 
-template <int RG>
 struct State {
-  half8_t q[RG][8];
-  float16_t o[RG][4];
-  float m[RG], l[RG];                  // level, the lane's part of the sum
-  float zero[RG], raise[RG];           // the level (0: none yet), and what raises it
+  half8_t q[8];
+  float16_t o[4];
+  float m, l;                  // level, the lane's part of the sum
+  float zero, raise;           // the level (0: none yet), and what raises it
   bool far;                            // some row's level is
 };
 
 // ---- a unit on its way into LDS
+//
+// Keys: [channel octet 16][row 32] of 16 bytes; values: [channels 32 x][tokens, two parts][half][channel 16 m + c] of 16 bytes.  The row of a token
+// is its number with bits 3 and 4 exchanged: then a lane's scores 8 e .. 8 e + 7 are those of tokens 4 g + j and 16 + 4 g + j, g = 2 e + half, which
+// is how values lie in the store.
+__device__ __forceinline__ int row_of(int token) { return (token & 7) | (token & 8) << 1 | (token & 16) >> 1; }
+__device__ __forceinline__ int token_of(int i, int half) { return (i & 4) << 2 | (i >> 3) << 3 | half << 2 | (i & 3); }
 
 struct Staged { u32x4 a, b, c, d; };                     // packed: keys, values; fp16: two pieces of a key row, four of values
 
-template <bool E4M3>
-__device__ __forceinline__ void put_packed(char* buf, int wave, int lane, const u32x4& k, const u32x4& v, float shrink) {
+// Sixteen codes: number `lane` of the kilobyte `part` (0 .. 3) of a tensor's tile.
+__device__ __forceinline__ int put_at(bool keys, int part, int lane) {
   const int g = lane >> 4, c = lane & 15;
-  {
-    // tokens 16 a + c, channels 32 g + 16 h + ..
-    char* dst = buf + (2 * g + (wave & 1)) * 1024 + (16 * (wave >> 1) + c) * 16;
-    *reinterpret_cast<half8_t*>(dst) = expand<E4M3>(k.x, k.y);
-    *reinterpret_cast<half8_t*>(dst + 512) = expand<E4M3>(k.z, k.w);
-  }
-  const half8_t even = expand_by<E4M3>(v.x, v.y, shrink), odd = expand_by<E4M3>(v.z, v.w, shrink);
-  // (the lane's g is that of value_lane: neighbours in LDS are neighbours in the wavefront)
-  const int vg = (g >> 1) | (g & 1) << 1;
-  char* dst = buf + kUnitValues + wave * 2048 + (vg & 1) * 512 + c * 16 + (vg >> 1) * 8;
-  const u32x4 e = __builtin_bit_cast(u32x4, even), o = __builtin_bit_cast(u32x4, odd);
-  *reinterpret_cast<u32x2*>(dst) = u32x2{e.x, e.y};
-  *reinterpret_cast<u32x2*>(dst + 1024) = u32x2{e.z, e.w};
-  *reinterpret_cast<u32x2*>(dst + 256) = u32x2{o.x, o.y};
-  *reinterpret_cast<u32x2*>(dst + 1024 + 256) = u32x2{o.z, o.w};
+  if (keys) return (2 * g + (part & 1)) * 1024 + row_of(16 * (part >> 1) + c) * 16;        // channels 32 g + 16 h + ..
+  return kUnitValues + part * 2048 + (g >> 1) * 1024 + (g & 1) * 512 + c * 16;
 }
-// Which sixteen bytes of a kilobyte of value codes a lane takes: those of groups 0, 2, 1, 3.
-__device__ __forceinline__ int value_lane(int lane) {
-  const int g = lane >> 4;
-  return ((g >> 1) | (g & 1) << 1) * 16 + (lane & 15);
+template <bool E4M3>
+__device__ __forceinline__ void put_codes(char* dst, int apart, const u32x4& w, float by) {
+  *reinterpret_cast<half8_t*>(dst) = expand_by<E4M3>(w.x, w.y, by);
+  *reinterpret_cast<half8_t*>(dst + apart) = expand_by<E4M3>(w.z, w.w, by);
 }
 
-// fp16 rows.  Keys: thread tid has sixteen channels of a token; values: four channels of four tokens.
+// fp16 rows.  Keys: a thread has 32 / WAVES octets of a token ..; values: four tokens of 8 / WAVES pairs of channels.
+template <int WAVES>
 __device__ __forceinline__ void put_plain(char* buf, int tid, const Staged& x) {
+  constexpr int N = 8 / WAVES, PER = 16 / N;             // octets of a thread, threads of a token
   {
-    char* dst = buf + (tid & 7) * 1024 + (tid >> 3) * 16;
+    char* dst = buf + tid % PER * N * 512 + row_of(tid / PER) * 16;
     *reinterpret_cast<u32x4*>(dst) = x.a;
-    *reinterpret_cast<u32x4*>(dst + 512) = x.b;
+    if (N == 2) *reinterpret_cast<u32x4*>(dst + 512) = x.b;
   }
-  const int quad = tid >> 5, ch = (tid & 31) * 4;        // tokens 4 quad ..
-  const int g = quad & 3;
-  char* dst = buf + kUnitValues + (ch >> 5) * 2048 + (quad >> 2) * 1024 + (g & 1) * 512 + (g >> 1) * 8 + ((ch & 31) >> 1) * 16;
+  constexpr int PAIRS = 64 / N;                          // threads of four tokens
+  const int quad = tid / PAIRS, ch = tid % PAIRS * 2 * N, g = quad & 3;                    // tokens 4 quad .. = 16 i + 4 g ..
+  char* dst = buf + kUnitValues + (ch >> 5) * 2048 + (g >> 1) * 1024 + (g & 1) * 512 + (quad >> 2) * 8 + ((ch & 31) >> 1) * 16;
   const uint32_t w[4][2] = {{x.c.x, x.c.y}, {x.c.z, x.c.w}, {x.d.x, x.d.y}, {x.d.z, x.d.w}};
 #pragma unroll
-  for (int p = 0; p < 2; ++p) {                          // channels ch + 2 p, ch + 2 p + 1
+  for (int p = 0; p < N; ++p) {                          // channels ch + 2 p, ch + 2 p + 1
     const u32x2 even = {__builtin_amdgcn_perm(w[1][p], w[0][p], 0x05040100u), __builtin_amdgcn_perm(w[3][p], w[2][p], 0x05040100u)};
     const u32x2 odd = {__builtin_amdgcn_perm(w[1][p], w[0][p], 0x07060302u), __builtin_amdgcn_perm(w[3][p], w[2][p], 0x07060302u)};
     *reinterpret_cast<u32x2*>(dst + 16 * p) = even;
@@ -96,65 +90,39 @@ __device__ __forceinline__ void put_plain(char* buf, int tid, const Staged& x) {
 
 // ---- the two products and what is between them
 
-template <int RG>
-__device__ __forceinline__ void unit_scores(const char* buf, const State<RG>& r, int lane, float16_t (&s)[RG]) {
-  const char* keys = buf + lane * 16;
-#pragma unroll
-  for (int n = 0; n < RG; ++n) s[n] = float16_t{};
-#pragma unroll
-  for (int st = 0; st < 8; ++st) {
-    const half8_t k = *reinterpret_cast<const half8_t*>(keys + 1024 * st);
-#pragma unroll
-    for (int n = 0; n < RG; ++n) s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, r.q[n][st], s[n], 0, 0, 0);
-  }
-}
 __device__ __forceinline__ float threshold(float m) { return __builtin_fmaf(-kFarShare, __builtin_fabsf(m), m) + kRaise; }
-// Largest of a lane's scores, as exponents.
-template <int RG>
-__device__ __forceinline__ void unit_tops(const float16_t (&s)[RG], const Scales& u, float (&top)[RG]) {
+// Largest of a lane's scores, as an exponent.
+__device__ __forceinline__ float unit_top(const float16_t& s, const Scales& u) {
+  float t = s[0];
 #pragma unroll
-  for (int n = 0; n < RG; ++n) {
-    float t = s[n][0];
-#pragma unroll
-    for (int i = 1; i < 16; ++i) t = fmaxf(t, s[n][i]);
-    top[n] = __builtin_fmaf(t, u.by, u.add);
-  }
+  for (int i = 1; i < 16; ++i) t = fmaxf(t, s[i]);
+  return __builtin_fmaf(t, u.by, u.add);
 }
-template <int RG>
-__device__ __forceinline__ void raise_levels(State<RG>& r, const float (&tops)[RG]) {
-  bool far = false;
+__device__ __forceinline__ void raise_level(State& r, float mine) {
+  const float top = fmaxf(mine, other_half(mine));
+  const bool up = top > r.raise;
+  const float level = up ? fmaxf(r.m, __builtin_fabsf(top) > kFar ? top : top - kTop) : r.m;
+  const float f = up ? __builtin_amdgcn_exp2f(r.m - level) : 1.f;                // (0 from the empty state)
+  r.l *= f;
 #pragma unroll
-  for (int n = 0; n < RG; ++n) {
-    const float top = fmaxf(tops[n], other_half(tops[n]));
-    const bool up = top > r.raise[n];
-    const float level = up ? fmaxf(r.m[n], __builtin_fabsf(top) > kFar ? top : top - kTop) : r.m[n];
-    const float f = up ? __builtin_amdgcn_exp2f(r.m[n] - level) : 1.f;           // (0 from the empty state)
-    r.l[n] *= f;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) r.o[n][x] *= f;
-    r.m[n] = level;
-    r.zero[n] = level == -INFINITY ? 0.f : level;
-    r.raise[n] = threshold(level);
-    far |= __builtin_fabsf(r.zero[n]) > kFar;
-  }
-  r.far = __builtin_amdgcn_ballot_w64(far) != 0;
+  for (int x = 0; x < 4; ++x) r.o[x] *= f;
+  r.m = level;
+  r.zero = level == -INFINITY ? 0.f : level;
+  r.raise = threshold(level);
+  r.far = __builtin_amdgcn_ballot_w64(__builtin_fabsf(r.zero) > kFar) != 0;
 }
-// Weights of scores 2 e, 2 e + 1 of every row.
-template <int RG>
-__device__ __forceinline__ void two_weights(int e, const float16_t (&s)[RG], float by, const float (&bias)[RG], half8_t (&p)[RG][2], float (&sum)[RG]) {
-#pragma unroll
-  for (int n = 0; n < RG; ++n) {
-    const half2_t w = {(_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[n][2 * e], by, bias[n])), (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[n][2 * e + 1], by, bias[n]))};
-    p[n][e / 4][2 * (e % 4)] = w.x;
-    p[n][e / 4][2 * (e % 4) + 1] = w.y;
-    sum[n] = __builtin_amdgcn_fdot2(w, half2_t{(_Float16)1.0f, (_Float16)1.0f}, sum[n], false);
-  }
+// Weights of scores 2 e, 2 e + 1.
+__device__ __forceinline__ void two_weights(int e, const float16_t& s, float by, float bias, half8_t (&p)[2], float& sum) {
+  const half2_t w = {(_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * e], by, bias)), (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * e + 1], by, bias))};
+  p[e / 4][2 * (e % 4)] = w.x;
+  p[e / 4][2 * (e % 4) + 1] = w.y;
+  sum = __builtin_amdgcn_fdot2(w, half2_t{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
 }
 
 // Units u0 .. u1 of one kind.  fetch(u, regs, scales): a unit's bytes into registers, and its scales; put(buffer, regs, scales): into LDS; mask(u,
 // scores): scores of tokens that a row does not attend to are -infinity.
-template <int RG, bool MASKED, typename Fetch, typename Put, typename Mask>
-__device__ __forceinline__ void walk(int u0, int u1, char* lds, State<RG>& r, int lane, Fetch fetch, Put put, Mask mask) {
+template <bool MASKED, typename Fetch, typename Put, typename Mask>
+__device__ __forceinline__ void walk(int u0, int u1, char* lds, State& r, int lane, Fetch fetch, Put put, Mask mask) {
   if (u0 >= u1) return;
   auto at = [&](int u) { return lds + ((u - u0) % kUnits) * kUnitBytes; };
   auto bound = [&](int u) { return u < u1 ? u : u1 - 1; };      // (behind the last unit: that one again)
@@ -175,77 +143,61 @@ __device__ __forceinline__ void walk(int u0, int u1, char* lds, State<RG>& r, in
 #pragma unroll
     for (int e = 0; e < 8; ++e) k[e] = *reinterpret_cast<const half8_t*>(at(u) + lane * 16 + 1024 * e);
   };
-  float16_t s[RG], t[RG];
-  float top[RG];
+  float16_t s, t;
+  float top;
   keys(u0);
+  s = float16_t{};
 #pragma unroll
-  for (int n = 0; n < RG; ++n) s[n] = float16_t{};
-#pragma unroll
-  for (int e = 0; e < 8; ++e)
-#pragma unroll
-    for (int n = 0; n < RG; ++n) s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[e], r.q[n][e], s[n], 0, 0, 0);
+  for (int e = 0; e < 8; ++e) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[e], r.q[e], s, 0, 0, 0);
   keys(u0 + 1);
   if (MASKED) mask(u0, s);
-  unit_tops<RG>(s, now, top);
+  top = unit_top(s, now);
   // s: scores of unit u; k: keys of unit u + 1; x: unit u + 3
-  auto step = [&](int u, float16_t (&s)[RG], float16_t (&t)[RG], Staged& x, Scales& sx) {
-    bool raise = false;
-#pragma unroll
-    for (int n = 0; n < RG; ++n) raise |= top[n] > r.raise[n];
-    if (__builtin_amdgcn_ballot_w64(raise)) raise_levels<RG>(r, top);
+  auto step = [&](int u, float16_t& s, float16_t& t, Staged& x, Scales& sx) {
+    if (__builtin_amdgcn_ballot_w64(top > r.raise)) raise_level(r, top);
     if (r.far) {
       // (the fused form takes the level, which is rounded, from an exact product)
 #pragma unroll
-      for (int n = 0; n < RG; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[n][i] = __builtin_fmaf(s[n][i], now.by, now.add);
-          asm volatile("" : "+v"(s[n][i]));
-        }
+      for (int i = 0; i < 16; ++i) {
+        s[i] = __builtin_fmaf(s[i], now.by, now.add);
+        asm volatile("" : "+v"(s[i]));
+      }
       now.by = 1.f;
       now.add = 0.f;
     }
     // the scores of the next unit and the weights of this one, piece by piece; operands of the second product on their way
-    half8_t p[RG][2], v[8];
-    float bias[RG], sum[RG];
-#pragma unroll
-    for (int n = 0; n < RG; ++n) {
-      bias[n] = now.add - r.zero[n];
-      sum[n] = 0.f;
-      t[n] = float16_t{};
-    }
+    half8_t p[2], v[8];
+    const float bias = now.add - r.zero;
+    float sum = 0.f;
+    t = float16_t{};
     const char* values = at(u) + kUnitValues + lane * 16;
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-#pragma unroll
-      for (int n = 0; n < RG; ++n) t[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[e], r.q[n][e], t[n], 0, 0, 0);
+      t = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[e], r.q[e], t, 0, 0, 0);
       v[e] = *reinterpret_cast<const half8_t*>(values + 2048 * (e % 4) + 1024 * (e / 4));
-      two_weights<RG>(e, s, now.by, bias, p, sum);
+      two_weights(e, s, now.by, bias, p, sum);
       __builtin_amdgcn_sched_barrier(0);
     }
-#pragma unroll
-    for (int n = 0; n < RG; ++n) r.l[n] = __builtin_fmaf(sum[n], now.inv, r.l[n]);
+    r.l = __builtin_fmaf(sum, now.inv, r.l);
     // the second product; the keys after the next, a unit into LDS, the largest of the next scores
     keys(u + 2);
     put(at(u + 3), x, sx);
     now = next;
     next = third;
     third = sx;
-    if (!MASKED) unit_tops<RG>(t, now, top);
+    if (!MASKED) top = unit_top(t, now);
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int e = 0; e < 8; ++e) r.o[e % 4] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[e], p[e / 4], r.o[e % 4], 0, 0, 0);
 #pragma unroll
-      for (int n = 0; n < RG; ++n) r.o[n][e % 4] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[e], p[n][e / 4], r.o[n][e % 4], 0, 0, 0);
-#pragma unroll
-    for (int e = 0; e < 8 * RG; ++e) {
+    for (int e = 0; e < 8; ++e) {
       __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 2 / RG, 0);
-      __builtin_amdgcn_sched_group_barrier(0x2, 12 / RG, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x2, 12, 0);
     }
     if (MASKED) {
       mask(bound(u + 1), t);
-      unit_tops<RG>(t, now, top);
+      top = unit_top(t, now);
     }
     fetch(bound(u + 5), x, sx);
     __syncthreads();
@@ -258,36 +210,46 @@ __device__ __forceinline__ void walk(int u0, int u1, char* lds, State<RG>& r, in
   }
 }
 
-template <bool E4M3, int RG>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RG == 2 ? 1 : 2, RG == 2 ? 1 : 2)))
+template <bool E4M3, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 2)))
 block_rows_kernel(BlockAttnArgs a) {
   __shared__ __align__(16) char lds[kUnits * kUnitBytes];
-  constexpr int ROWS = 128 * RG;
-  const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-  // Sequence-heads that can be shared out evenly stay on one XCD (its L2 then brings every unit from memory once); the last rows, which have the
-  // most keys, go first.
-  const unsigned heads = (unsigned)(a.s.batch * a.s.n_kv_heads);
-  const bool pinned = heads % 8u == 0u;
-  const unsigned slot = pinned ? blockIdx.x / 8u : blockIdx.x, mine_heads = pinned ? heads / 8u : heads;
-  const unsigned rank = slot / (mine_heads * (unsigned)a.n_splits), rest = slot % (mine_heads * (unsigned)a.n_splits);
-  const int bh = (int)(rest / (unsigned)a.n_splits + (pinned ? blockIdx.x % 8u * mine_heads : 0u)), split = (int)(rest % (unsigned)a.n_splits);
-  const int row_block = a.row_blocks - 1 - (int)rank;
-  const int b = bh / a.s.n_kv_heads, h = bh % a.s.n_kv_heads;
-  const BlockSeq s = block_seq(a, b);
-  const int rows = s.t * a.heads_per_kv, row0 = row_block * ROWS;
-  if (row0 >= rows) return;                              // (uniform)
-  State<RG> r;
-#pragma unroll
-  for (int n = 0; n < RG; ++n) {
-    const int row = row0 + 32 * (RG * wave + n) + (lane & 31), i = row / a.heads_per_kv;
-    const __half* src = a.q.p + b * a.q.batch + (h * a.heads_per_kv + row - i * a.heads_per_kv) * a.q.head + i * a.q.token + 8 * half;
-#pragma unroll
-    for (int st = 0; st < 8; ++st) r.q[n][st] = row < rows ? *reinterpret_cast<const half8_t*>(src + 16 * st) : half8_t{};
-#pragma unroll
-    for (int x = 0; x < 4; ++x) r.o[n][x] = float16_t{};
-    r.m[n] = r.raise[n] = -INFINITY;
-    r.l[n] = r.zero[n] = 0.f;
+  constexpr int ROWS = 32 * WAVES;
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  BlockWork w;
+  if (a.table) {
+    if (!find_work<ROWS>(a, w)) return;                  // (uniform)
+  } else {
+    // Sequence-heads that can be shared out evenly stay on one XCD (its L2 then brings every unit from memory once); the last rows, which have
+    // the most keys, go first.
+    const unsigned heads = (unsigned)(a.s.batch * a.s.n_kv_heads);
+    const bool pinned = heads % 8u == 0u;
+    const unsigned slot = pinned ? blockIdx.x / 8u : blockIdx.x, mine_heads = pinned ? heads / 8u : heads;
+    const unsigned rank = slot / (mine_heads * (unsigned)a.n_splits), rest = slot % (mine_heads * (unsigned)a.n_splits);
+    const unsigned bh = rest / (unsigned)a.n_splits + (pinned ? blockIdx.x % 8u * mine_heads : 0u);
+    w.split = (int)(rest % (unsigned)a.n_splits);
+    w.n_splits = a.n_splits;
+    w.row_block = a.row_blocks - 1 - (int)rank;
+    w.b = (int)(bh / (unsigned)a.s.n_kv_heads);
+    w.h = (int)(bh % (unsigned)a.s.n_kv_heads);
+    w.slot = ((long long)bh * a.row_blocks + w.row_block) * a.n_splits + w.split;
   }
+  const int b = w.b, h = w.h, n_splits = w.n_splits;
+  const long long bh = (long long)b * a.s.n_kv_heads + h;
+  const BlockSeq s = block_seq(a, b);
+  const int rows = s.t * a.heads_per_kv, row0 = w.row_block * ROWS;
+  if (row0 >= rows) return;                              // (uniform)
+  State r;
+  {
+    const int row = row0 + 32 * wave + (lane & 31), i = row / a.heads_per_kv;
+    const __half* src = a.q.p + b * a.q.batch + (h * a.heads_per_kv + row - i * a.heads_per_kv) * a.q.head + i * a.q.token + 8 * (lane >> 5);
+#pragma unroll
+    for (int st = 0; st < 8; ++st) r.q[st] = row < rows ? *reinterpret_cast<const half8_t*>(src + 16 * st) : half8_t{};
+  }
+#pragma unroll
+  for (int x = 0; x < 4; ++x) r.o[x] = float16_t{};
+  r.m = r.raise = -INFINITY;
+  r.l = r.zero = 0.f;
   r.far = false;
   const float scale = 0.08838834764831845f * 1.4426950408889634f;
 
@@ -295,8 +257,8 @@ block_rows_kernel(BlockAttnArgs a) {
   const int last_row = (row0 + ROWS < rows ? row0 + ROWS : rows) - 1;
   const int open = s.n - s.packed, plain = open + (causal ? last_row / a.heads_per_kv + 1 : 0);
   const int tiles1 = s.packed / kBlockTile, tiles = tiles1 + (plain + kBlockTile - 1) / kBlockTile;
-  const int share = tiles / a.n_splits, more = tiles % a.n_splits;
-  const int t0 = split * share + (split < more ? split : more), t1 = t0 + share + (split < more ? 1 : 0);
+  const int share = tiles / n_splits, more = tiles % n_splits;
+  const int t0 = w.split * share + (w.split < more ? w.split : more), t1 = t0 + share + (w.split < more ? 1 : 0);
 
   const int u1 = t1 < tiles1 ? t1 : tiles1;
   if (t0 < u1) {
@@ -329,113 +291,117 @@ block_rows_kernel(BlockAttnArgs a) {
       inv = 1.0f / eff;
     };
     auto lane_of = [&](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
-    const uint32_t k_at = (uint32_t)(64 * wave + lane) * 16, v_at = (uint32_t)(64 * wave + value_lane(lane)) * 16;
+    // (eight wavefronts: half of them bring keys, half values)
+    const bool keys = WAVES == 4 || wave < 4;
+    const uint32_t mine_at = (uint32_t)(64 * (wave & 3) + lane) * 16;
+    const int to = put_at(keys, wave & 3, lane), apart = keys ? 512 : 256;
+    const uint8_t* codes = keys ? a.s.k.codes : a.s.v.codes;
     auto fetch = [&](int u, Staged& x, Scales& sc) {
       look(u);
       const int i = u - base;
       const long long tile = (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(at >> 32), i) << 32) |
                                          (unsigned)__builtin_amdgcn_readlane((int)at, i)) * kBlockTileBytes;
-      x.a = *reinterpret_cast<const u32x4*>(a.s.k.codes + tile + k_at);
-      x.b = *reinterpret_cast<const u32x4*>(a.s.v.codes + tile + v_at);
+      x.a = *reinterpret_cast<const u32x4*>(codes + tile + mine_at);
+      if (WAVES == 4) x.b = *reinterpret_cast<const u32x4*>(a.s.v.codes + tile + mine_at);
       sc = Scales{lane_of(by, i), lane_of(add, i), lane_of(inv, i), lane_of(shrink, i)};
     };
-    walk<RG, false>(t0, u1, lds, r, lane, fetch, [&](char* buf, const Staged& x, const Scales& sc) { put_packed<E4M3>(buf, wave, lane, x.a, x.b, sc.shrink); },
-                    [](int, float16_t (&)[RG]) {});
+    auto put = [&](char* buf, const Staged& x, const Scales& sc) {
+      put_codes<E4M3>(buf + to, apart, x.a, keys ? 1.f : sc.shrink);
+      if (WAVES == 4) put_codes<E4M3>(buf + put_at(false, wave, lane), 256, x.b, sc.shrink);
+    };
+    walk<false>(t0, u1, lds, r, lane, fetch, put, [](int, float16_t&) {});
   }
   if (t1 > tiles1) {
-    const long long open_at = (long long)bh * a.s.block * D;
+    const long long open_at = bh * a.s.block * D;
     const __half *ko = a.s.k.open + open_at, *vo = a.s.v.open + open_at;
     const __half *kf = a.k.p + b * a.k.batch + h * a.k.head, *vf = a.v.p + b * a.v.batch + h * a.v.head;
     auto fetch = [&](int u, Staged& x, Scales& sc) {
       sc = Scales{scale, 0.f, 1.f, 1.f};
       const int i0 = u * kBlockTile;
       auto token = [&](int i) { return i0 + i < plain ? i0 + i : plain - 1; };   // (behind the last one: that one again, masked)
-      const int i = token(tid >> 3);
-      const __half* k = (i < open ? ko + i * D : kf + (i - open) * a.k.token) + 16 * (tid & 7);
+      constexpr int N = 8 / WAVES, PER = 16 / N, PAIRS = 64 / N;                 // (as put_plain)
+      const int i = token(tid / PER);
+      const __half* k = (i < open ? ko + i * D : kf + (i - open) * a.k.token) + tid % PER * 8 * N;
       x.a = *reinterpret_cast<const u32x4*>(k);
-      x.b = *reinterpret_cast<const u32x4*>(k + 8);
+      if (N == 2) x.b = *reinterpret_cast<const u32x4*>(k + 8);
       u32x2 w[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int j = token(4 * (tid >> 5) + e);
-        w[e] = *reinterpret_cast<const u32x2*>((j < open ? vo + j * D : vf + (j - open) * a.v.token) + 4 * (tid & 31));
+        const int j = token(4 * (tid / PAIRS) + e);
+        const __half* v = (j < open ? vo + j * D : vf + (j - open) * a.v.token) + tid % PAIRS * 2 * N;
+        if (N == 2) w[e] = *reinterpret_cast<const u32x2*>(v);
+        else w[e] = u32x2{*reinterpret_cast<const uint32_t*>(v), 0u};
       }
       x.c = u32x4{w[0].x, w[0].y, w[1].x, w[1].y};
       x.d = u32x4{w[2].x, w[2].y, w[3].x, w[3].y};
     };
-    int limit[RG];                                       // last token that the lane's row attends to
+    const int row = row0 + 32 * wave + (lane & 31), half = lane >> 5;
+    const int limit = causal ? open + (row < rows ? row : rows - 1) / a.heads_per_kv : plain - 1;      // last token that the lane's row attends to
+    auto mask = [&](int u, float16_t& sc) {
+      const int left = limit - u * kBlockTile;
+      if (!__builtin_amdgcn_ballot_w64(left < kBlockTile - 1)) return;
 #pragma unroll
-    for (int n = 0; n < RG; ++n) {
-      const int row = row0 + 32 * (RG * wave + n) + (lane & 31);
-      limit[n] = causal ? open + (row < rows ? row : rows - 1) / a.heads_per_kv : plain - 1;
-    }
-    walk<RG, true>(t0 > tiles1 ? t0 - tiles1 : 0, t1 - tiles1, lds, r, lane, fetch, [&](char* buf, const Staged& x, const Scales&) { put_plain(buf, tid, x); },
-             [&](int u, float16_t (&sc)[RG]) {
-#pragma unroll
-               for (int n = 0; n < RG; ++n) {
-                 const int left = limit[n] - u * kBlockTile - 4 * half;
-                 if (!__builtin_amdgcn_ballot_w64(left < kBlockTile - 1)) continue;
-#pragma unroll
-                 for (int i = 0; i < 16; ++i)
-                   if (8 * (i / 4) + i % 4 > left) sc[n][i] = -INFINITY;
-               }
-             });
+      for (int i = 0; i < 16; ++i)
+        if (token_of(i, half) > left) sc[i] = -INFINITY;
+    };
+    walk<true>(t0 > tiles1 ? t0 - tiles1 : 0, t1 - tiles1, lds, r, lane, fetch, [&](char* buf, const Staged& x, const Scales&) { put_plain<WAVES>(buf, tid, x); },
+               mask);
   }
 
-  // results: a lane has channels 32 x + 16 y + 8 half + 2 i + m of its rows, at o[x][4 y + 8 m + i]
-#pragma unroll
-  for (int n = 0; n < RG; ++n) {
-    const float l = r.l[n] + other_half(r.l[n]);
-    const int in_block = 32 * (RG * wave + n) + (lane & 31), row = row0 + in_block;
-    if (row >= rows) continue;
-    if (a.n_splits > 1) {
-      const long long slot_row = (((long long)bh * a.row_blocks + row_block) * a.n_splits + split) * ROWS + in_block;
-      float* dst = a.ws + a.slots * (ROWS * 2) + slot_row * D + 8 * half;
-#pragma unroll
-      for (int x = 0; x < 4; ++x)
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const float16_t& o = r.o[n][x];
-          *reinterpret_cast<float4*>(dst + 32 * x + 16 * y) = float4{o[4 * y], o[4 * y + 8], o[4 * y + 1], o[4 * y + 9]};
-          *reinterpret_cast<float4*>(dst + 32 * x + 16 * y + 4) = float4{o[4 * y + 2], o[4 * y + 10], o[4 * y + 3], o[4 * y + 11]};
-        }
-      if (half == 0) *reinterpret_cast<float2*>(a.ws + slot_row * 2) = float2{r.m[n], l};
-      continue;
-    }
-    const float f = l > 0.f ? 1.0f / l : 0.f;            // (no token: zero)
-    const int i = row / a.heads_per_kv;
-    const long long out = b * a.out_batch + (h * a.heads_per_kv + row - i * a.heads_per_kv) * a.out_head + i * a.out_token + 8 * half;
+  // results: a lane has channels 32 x + 16 y + 8 half + 2 i + m of its row, at o[x][4 y + 8 m + i]
+  const float l = r.l + other_half(r.l);
+  int again = (int)threadIdx.x;
+  asm("" : "+v"(again));                                 // (where its row is, is found anew: registers held over the loops would be spilled)
+  const int row = row0 + 32 * (again >> 6) + (again & 31), half = again >> 5 & 1;
+  if (row >= rows) return;
+  const int row_token = row / a.heads_per_kv, row_head = h * a.heads_per_kv + row - row_token * a.heads_per_kv;
+  if (n_splits > 1) {
+    const long long slot_row = w.slot * ROWS + row - row0;
+    float* dst = a.ws + a.slots * (ROWS * 2) + slot_row * D + 8 * half;
 #pragma unroll
     for (int x = 0; x < 4; ++x)
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        const float16_t& o = r.o[n][x];
-        const float c[8] = {o[4 * y] * f, o[4 * y + 8] * f, o[4 * y + 1] * f, o[4 * y + 9] * f, o[4 * y + 2] * f, o[4 * y + 10] * f, o[4 * y + 3] * f, o[4 * y + 11] * f};
-        if (a.out_is_fp32) {
-          float* dst = static_cast<float*>(a.out) + out + 32 * x + 16 * y;
-          *reinterpret_cast<float4*>(dst) = float4{c[0], c[1], c[2], c[3]};
-          *reinterpret_cast<float4*>(dst + 4) = float4{c[4], c[5], c[6], c[7]};
-        } else {
-          half8_t w;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) w[e] = (_Float16)c[e];
-          *reinterpret_cast<half8_t*>(static_cast<_Float16*>(a.out) + out + 32 * x + 16 * y) = w;
-        }
+        const float16_t& o = r.o[x];
+        *reinterpret_cast<float4*>(dst + 32 * x + 16 * y) = float4{o[4 * y], o[4 * y + 8], o[4 * y + 1], o[4 * y + 9]};
+        *reinterpret_cast<float4*>(dst + 32 * x + 16 * y + 4) = float4{o[4 * y + 2], o[4 * y + 10], o[4 * y + 3], o[4 * y + 11]};
       }
+    if (half == 0) *reinterpret_cast<float2*>(a.ws + slot_row * 2) = float2{r.m, l};
+    return;
   }
+  const float f = l > 0.f ? 1.0f / l : 0.f;              // (no token: zero)
+  const long long out = b * a.out_batch + row_head * a.out_head + row_token * a.out_token + 8 * half;
+#pragma unroll
+  for (int x = 0; x < 4; ++x)
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const float16_t& o = r.o[x];
+      const float c[8] = {o[4 * y] * f,     o[4 * y + 8] * f,  o[4 * y + 1] * f, o[4 * y + 9] * f,
+                          o[4 * y + 2] * f, o[4 * y + 10] * f, o[4 * y + 3] * f, o[4 * y + 11] * f};
+      if (a.out_is_fp32) {
+        float* dst = static_cast<float*>(a.out) + out + 32 * x + 16 * y;
+        *reinterpret_cast<float4*>(dst) = float4{c[0], c[1], c[2], c[3]};
+        *reinterpret_cast<float4*>(dst + 4) = float4{c[4], c[5], c[6], c[7]};
+      } else {
+        half8_t v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (_Float16)c[e];
+        *reinterpret_cast<half8_t*>(static_cast<_Float16*>(a.out) + out + 32 * x + 16 * y) = v;
+      }
+    }
 }
 
 }  // namespace
 
 hipError_t launch_block_rows(const BlockAttnArgs& a, bool e4m3, int group_rows, hipStream_t stream) {
-  const long long groups = (long long)a.s.batch * a.s.n_kv_heads * a.row_blocks * a.n_splits;
+  const long long groups = a.table ? a.list_groups : (long long)a.s.batch * a.s.n_kv_heads * a.row_blocks * a.n_splits;
   if (groups >= (1LL << 31)) return hipErrorInvalidValue;
   if (group_rows == 128) {
-    if (e4m3) block_rows_kernel<true, 1><<<(unsigned)groups, 256, 0, stream>>>(a);
-    else block_rows_kernel<false, 1><<<(unsigned)groups, 256, 0, stream>>>(a);
+    if (e4m3) block_rows_kernel<true, 4><<<(unsigned)groups, 256, 0, stream>>>(a);
+    else block_rows_kernel<false, 4><<<(unsigned)groups, 256, 0, stream>>>(a);
   } else if (group_rows == 256) {
-    if (e4m3) block_rows_kernel<true, 2><<<(unsigned)groups, 256, 0, stream>>>(a);
-    else block_rows_kernel<false, 2><<<(unsigned)groups, 256, 0, stream>>>(a);
+    if (e4m3) block_rows_kernel<true, 8><<<(unsigned)groups, 512, 0, stream>>>(a);
+    else block_rows_kernel<false, 8><<<(unsigned)groups, 512, 0, stream>>>(a);
   } else {
     return hipErrorInvalidValue;
   }

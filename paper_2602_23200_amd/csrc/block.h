@@ -59,8 +59,14 @@ struct BlockAttnArgs {
   int out_is_fp32;
   int heads_per_kv;
   int row_blocks, n_splits;
+  int* table;                          // a list: first slot and splits of every sequence are left here for the merge; else null
+  int list_groups;                     // work-groups of the launch
+  int rows_from, rows_to;              // sequences of this launch: with that many rows (from excluded, to included)
   float* ws;                           // slots: (level in the log2 domain, sum) of every row, then 128 sums of every row
-  long long slots;
+  long long slots;                     // that ws holds
+  float* ws_few;                       // merge of a list: the slots of the sequences of few rows (ws: of the others)
+  int few_rows;                        // rows of such a slot; of the sequences that have them
+  int few_most;
 };
 hipError_t launch_block_attention(const BlockAttnArgs& a, bool e4m3, int group_rows, hipStream_t stream);
 hipError_t launch_block_rows(const BlockAttnArgs& a, bool e4m3, int group_rows, hipStream_t stream);

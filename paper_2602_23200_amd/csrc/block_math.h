@@ -54,4 +54,83 @@ __device__ __forceinline__ BlockSeq block_seq(const BlockAttnArgs& a, int b) {
   return s;
 }
 
+// What a work-group does.
+struct BlockWork { int b, h, row_block, split, n_splits; long long slot; };
+
+__device__ __forceinline__ int wave_sum(int x) {
+#pragma unroll
+  for (int i = 1; i < 64; i *= 2) x += __shfl_xor(x, i);
+  return x;
+}
+// A ragged batch: work-groups find their work from the counts of all sequences (four a lane; the arithmetic is the plan's), every wavefront
+// the same.  Neighbours in the list, which share keys, go to one XCD.
+template <int ROWS>
+__device__ __forceinline__ bool find_work(const BlockAttnArgs& a, BlockWork& w) {
+  constexpr int N = kBlockListMost / 64;
+  const int lane = (int)threadIdx.x & 63, per = a.list_groups / 8;
+  const int item = (int)blockIdx.x < 8 * per ? (int)blockIdx.x % 8 * per + (int)blockIdx.x / 8 : (int)blockIdx.x;
+  int units[N], tiles[N];                                // of the lane's sequences
+  int most = 1;
+  float work = 0.f;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int b = N * lane + j;
+    units[j] = tiles[j] = 0;
+    if (b < a.s.batch) {
+      const BlockSeq s = block_seq(a, b);
+      const BlockShare share = block_share(s.n, s.t, a.k.p != nullptr, a.heads_per_kv, a.s.n_kv_heads, a.rows_from, a.rows_to, ROWS);
+      units[j] = share.units;
+      tiles[j] = share.tiles;
+    }
+    most = tiles[j] > most ? tiles[j] : most;
+    work += (float)units[j] * (float)tiles[j];
+  }
+#pragma unroll
+  for (int i = 1; i < 64; i *= 2) {
+    const int x = __shfl_xor(most, i);
+    most = x > most ? x : most;
+    work += __shfl_xor(work, i);
+  }
+  most = __builtin_amdgcn_readfirstlane(most);
+  int length = __builtin_amdgcn_readfirstlane(block_first_length(work));
+  int mine;
+  for (;; length = block_next_length(length)) {
+    mine = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) mine += units[j] * block_ranges(tiles[j], length);
+    if (block_length_fits(length, most, __builtin_amdgcn_readfirstlane(wave_sum(mine)))) break;
+  }
+  // the sequence whose items hold this one
+  int before = mine;
+#pragma unroll
+  for (int i = 1; i < 64; i *= 2) {
+    const int x = __shfl_up(before, i);
+    if (lane >= i) before += x;
+  }
+  const unsigned long long reach = __builtin_amdgcn_ballot_w64(before > item);
+  if (reach == 0) return false;                          // (uniform)
+  const int owner = __builtin_ctzll(reach);
+  int first = __builtin_amdgcn_readlane(before - mine, owner);
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int u = __builtin_amdgcn_readlane(units[j], owner), splits = block_ranges(__builtin_amdgcn_readlane(tiles[j], owner), length), all = u * splits;
+    if (item >= first && item < first + all) {
+      const BlockPlace at = block_place(item - first, u, a.s.n_kv_heads, splits);
+      w.b = N * owner + j;
+      w.h = at.h;
+      w.row_block = at.row_block;
+      w.split = at.split;
+      w.n_splits = splits;
+      w.slot = item;
+      if (item == first && threadIdx.x == 0) {
+        a.table[2 * w.b] = item;
+        a.table[2 * w.b + 1] = splits;
+      }
+      return true;
+    }
+    first += all;
+  }
+  return false;
+}
+
 }  // namespace innerq

@@ -146,7 +146,7 @@ int main() {
     if (t > cap || (long long)b * h > 65535) continue;
     innerq_block_config_t c = {};
     c.batch = b; c.n_kv_heads = h; c.n_q_heads = h * r; c.head_dim = 128; c.capacity_tokens = cap; c.block = 32;
-    const long long room = (long long)block_workspace_bytes(c, t) - 256;
+    const long long room = (long long)block_workspace_bytes(c, t) - kBlockTableBytes;
     for (long long n = 0; n <= cap; n = n * 5 / 3 + 1) {
       const BlockSizes s = block_sizes(c, t);
       const long long splits = block_splits(s, n), slots = s.heads * s.row_blocks * splits;
