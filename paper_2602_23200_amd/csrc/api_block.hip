@@ -127,20 +127,21 @@ int attention(const innerq_block_config_t& c, const innerq_block_cache_t& k, con
   a.rows_from = 0; a.rows_to = 0x7fffffff;
   a.ws = a.ws_few = reinterpret_cast<float*>(static_cast<char*>(workspace) + kBlockTableBytes);
   a.slots = sizes.heads * sizes.row_blocks * a.n_splits;
-  a.few_rows = sizes.group_rows; a.few_most = 0;
+  a.few_slots = a.few_rows = a.few_most = 0;
   const bool e4m3 = c.type == INNERQ_E4M3;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   auto launch = [&](int group_rows) { return group_rows <= kBlockFewRows ? launch_block_attention(a, e4m3, group_rows, stream) : launch_block_rows(a, e4m3, group_rows, stream); };
-  if (n_dev && c.batch <= kBlockListMost) {
-    const BlockList list = block_list(c, t_new);
+  const BlockList list = block_list(c, t_new);
+  if (n_dev && list.use) {
     a.table = static_cast<int*>(workspace);
-    a.slots = kBlockListItems;
+    a.few_slots = a.slots = block_round(list.few_rows);
     a.few_rows = list.few_rows;
     a.few_most = a.rows_to = kBlockFewRows;
     a.list_groups = (int)list.few;
     hipError_t e = launch(list.few_rows);
     if (e == hipSuccess && list.many) {
-      a.ws = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ws) + (size_t)kBlockListItems * block_slot_bytes(list.few_rows));
+      a.ws = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ws) + (size_t)a.few_slots * block_slot_bytes(list.few_rows));
+      a.slots = block_round(kBlockListRows);
       a.rows_from = kBlockFewRows; a.rows_to = 0x7fffffff;
       a.list_groups = (int)list.many;
       e = launch(kBlockListRows);

@@ -31,6 +31,16 @@ __device__ __forceinline__ float row_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
+// Four channels of the output.
+__device__ __forceinline__ void store_four(const BlockAttnArgs& a, long long at, float w, float x, float y, float z) {
+  if (a.out_is_fp32) {
+    *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = float4{w, x, y, z};
+  } else {
+    const half2_t lo = {(_Float16)w, (_Float16)x}, hi = {(_Float16)y, (_Float16)z};
+    *reinterpret_cast<u32x2*>(static_cast<_Float16*>(a.out) + at) = u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+  }
+}
+
 // A wavefront's 16 NR query rows (lane: row lane % 16 of each sixteen; channels 32 (lane / 16) + 8 s + ..): operands, outputs (two
 // accumulators of 4: channels 32 q + 8 (lane / 16) + 2 i + m at o[2 q + m][i]), level, the lane's part of the sum.
 template <int NR>
@@ -136,9 +146,9 @@ struct Plain {
 };
 
 template <bool E4M3, int NR>
-__global__ void __launch_bounds__(64 * kBlockWaves) __attribute__((amdgpu_waves_per_eu(NR == 4 ? 1 : 2))) block_attention_kernel(BlockAttnArgs a) {
+__global__ void __launch_bounds__(64 * block_waves(16 * NR)) __attribute__((amdgpu_waves_per_eu(NR == 4 ? 1 : 2))) block_attention_kernel(BlockAttnArgs a) {
   using K = Kernel<E4M3, NR>;
-  constexpr int W = kBlockWaves;
+  constexpr int W = block_waves(16 * NR);
   __shared__ float lds[W * NR * (32 + 2) * 64];
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
   BlockWork work;
@@ -285,8 +295,8 @@ __global__ void __launch_bounds__(64 * kBlockWaves) __attribute__((amdgpu_waves_
     }
   }
 
-  // the wavefronts' results meet in LDS; wavefront w joins channels 32 w ..
-  static_assert(W == 4);
+  // the wavefronts' results meet in LDS, each joins CH channels of a lane's eight in channels 32 q ..
+  constexpr int CH = 32 / W;
   float* ml = lds + W * NR * 32 * 64;
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
@@ -298,115 +308,98 @@ __global__ void __launch_bounds__(64 * kBlockWaves) __attribute__((amdgpu_waves_
     ml[((wave * NR + n) * 2 + 1) * 64 + lane] = row_sum(r.l[n]);
   }
   __syncthreads();
+  const int q = wave * CH / 8, from = wave * CH % 8;     // (channel 2 i + m of the eight is o[2 q + m][i])
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
-    float top = -INFINITY, l = 0.f, o[8];
+    float top = -INFINITY, l = 0.f, o[CH];
 #pragma unroll
     for (int w = 0; w < W; ++w) top = fmaxf(top, ml[((w * NR + n) * 2) * 64 + lane]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = 0.f;
+    for (int i = 0; i < CH; ++i) o[i] = 0.f;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
       const float m = ml[((w * NR + n) * 2) * 64 + lane];
       const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
       l = __builtin_fmaf(f, ml[((w * NR + n) * 2 + 1) * 64 + lane], l);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) o[i] = __builtin_fmaf(f, lds[((w * NR + n) * 32 + 8 * wave + 4 * (i & 1) + i / 2) * 64 + lane], o[i]);
+      for (int i = 0; i < CH; ++i) o[i] = __builtin_fmaf(f, lds[((w * NR + n) * 32 + 8 * q + 4 * (i & 1) + (from + i) / 2) * 64 + lane], o[i]);
     }
     const int row = row0 + 16 * n + c;
     if (row >= rows) continue;
-    const int channel = 32 * wave + 8 * g;
+    const int channel = 32 * q + 8 * g + from;
     if (work.n_splits > 1) {
       const long long slot_row = work.slot * (16 * NR) + 16 * n + c;
       float* dst = a.ws + a.slots * (16 * NR * 2) + slot_row * D + channel;
-      *reinterpret_cast<float4*>(dst) = float4{o[0], o[1], o[2], o[3]};
-      *reinterpret_cast<float4*>(dst + 4) = float4{o[4], o[5], o[6], o[7]};
+#pragma unroll
+      for (int i = 0; i < CH; i += 4) *reinterpret_cast<float4*>(dst + i) = float4{o[i], o[i + 1], o[i + 2], o[i + 3]};
       if (wave == 0 && g == 0) *reinterpret_cast<float2*>(a.ws + slot_row * 2) = float2{top, l};
       continue;
     }
     const float f = l > 0.f ? 1.0f / l : 0.f;            // (no token: zero)
     const int i = row / a.heads_per_kv;
     const long long at = b * a.out_batch + (h * a.heads_per_kv + row - i * a.heads_per_kv) * a.out_head + i * a.out_token + channel;
-    if (a.out_is_fp32) {
-      float* dst = static_cast<float*>(a.out) + at;
-      *reinterpret_cast<float4*>(dst) = float4{o[0] * f, o[1] * f, o[2] * f, o[3] * f};
-      *reinterpret_cast<float4*>(dst + 4) = float4{o[4] * f, o[5] * f, o[6] * f, o[7] * f};
-    } else {
-      half8_t x;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = (_Float16)(o[e] * f);
-      *reinterpret_cast<half8_t*>(static_cast<_Float16*>(a.out) + at) = x;
-    }
+    for (int e = 0; e < CH; e += 4) store_four(a, at + e, o[e] * f, o[e + 1] * f, o[e + 2] * f, o[e + 3] * f);
   }
 }
 
-// The splits of a row joined: a wavefront a row, a lane two channels; levels and sums of up to 64 splits a load.
+// The splits of a row joined: half a wavefront a row, a lane four channels, eight splits under way.
+constexpr int kMergeRows = 8;                            // of a work-group
 __global__ void __launch_bounds__(256) block_merge_kernel(BlockAttnArgs a, int blocks, int group_rows) {
-  const int lane = (int)threadIdx.x & 63;
-  const int bh = (int)(blockIdx.x / (unsigned)blocks);
-  const int row = (int)(blockIdx.x % (unsigned)blocks) * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int b = bh / a.s.n_kv_heads, h = bh % a.s.n_kv_heads;
-  int step_rows;                                         // rows from one split to the next
+  const int bh = (int)(blockIdx.x / (unsigned)blocks), row = (int)(blockIdx.x % (unsigned)blocks) * kMergeRows + ((int)threadIdx.x >> 5);
+  const int b = bh / a.s.n_kv_heads, h = bh % a.s.n_kv_heads, channel = 4 * ((int)threadIdx.x & 31);
   const int own = block_seq(a, b).t * a.heads_per_kv;
   if (row >= own) return;
-  int n_splits = a.n_splits;
+  int n_splits = a.n_splits, step_rows = group_rows;     // rows from one split to the next
   const float* ws = a.ws;
   long long slots = a.slots, slot_row;
   if (a.table) {
     n_splits = a.table[2 * b + 1];
     if (n_splits == 1) return;                           // (written already)
-    const bool few = own <= a.few_most;
-    if (few) {
+    if (own <= a.few_most) {
       group_rows = a.few_rows;
       ws = a.ws_few;
+      slots = a.few_slots;
     }
-    slots = kBlockListItems;
     const int blocks_of = (own + group_rows - 1) / group_rows;
     slot_row = ((long long)a.table[2 * b] + (long long)h * blocks_of * n_splits + row / group_rows) * group_rows + row % group_rows;
     step_rows = blocks_of * group_rows;
   } else {
     slot_row = ((long long)bh * a.row_blocks + row / group_rows) * n_splits * group_rows + row % group_rows;
-    step_rows = group_rows;
   }
   const float* ml = ws + slot_row * 2;
-  const float* po = ws + slots * (group_rows * 2) + slot_row * D + 2 * lane;
+  const float* po = ws + slots * (group_rows * 2) + slot_row * D + channel;
   const long long step_ml = step_rows * 2, step_o = (long long)step_rows * D;
   float level = -INFINITY, den = 0.f;
-  float2 o = {0.f, 0.f};
-  for (int p0 = 0; p0 < n_splits; p0 += 64) {
-    const int count = n_splits - p0 < 64 ? n_splits - p0 : 64;
-    float2 st = {-INFINITY, 0.f};
-    if (lane < count) st = *reinterpret_cast<const float2*>(ml + (p0 + lane) * step_ml);
-    float top = st.x;
+  float4_t o = {};
+  for (int p0 = 0; p0 < n_splits; p0 += 8) {
+    float2 st[8];
+    float4_t v[8];
 #pragma unroll
-    for (int x = 32; x > 0; x /= 2) top = fmaxf(top, __shfl_xor(top, x));
-    top = fmaxf(top, level);
+    for (int e = 0; e < 8; ++e) {
+      const int p = p0 + e < n_splits ? p0 + e : n_splits - 1;
+      st[e] = *reinterpret_cast<const float2*>(ml + p * step_ml);
+      v[e] = *reinterpret_cast<const float4_t*>(po + p * step_o);
+    }
+    float top = level;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = fmaxf(top, st[e].x);
     const float old = level == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(level - top);
-    const float f = st.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.x - top);
-    float sum = f * st.y;
-#pragma unroll
-    for (int x = 32; x > 0; x /= 2) sum += __shfl_xor(sum, x);
-    den = __builtin_fmaf(den, old, sum);
-    o.x *= old;
-    o.y *= old;
+    den *= old;
+    o *= old;
     level = top;
-    for (int p = 0; p < count; p += 8) {                 // (eight partial results under way)
-      float2 v[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = *reinterpret_cast<const float2*>(po + (p0 + (p + e < count ? p + e : count - 1)) * step_o);
+    for (int e = 0; e < 8; ++e) {
+      const float f = p0 + e >= n_splits || st[e].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[e].x - top);
+      den = __builtin_fmaf(f, st[e].y, den);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float w = p + e < count ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), (p + e) & 63)) : 0.f;
-        o.x = __builtin_fmaf(w, v[e].x, o.x);
-        o.y = __builtin_fmaf(w, v[e].y, o.y);
-      }
+      for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(f, v[e][i], o[i]);
     }
   }
   const float inv = den > 0.f ? 1.0f / den : 0.f;
   const int i = row / a.heads_per_kv;
-  const long long at = b * a.out_batch + (h * a.heads_per_kv + row - i * a.heads_per_kv) * a.out_head + i * a.out_token + 2 * lane;
-  if (a.out_is_fp32) *reinterpret_cast<float2*>(static_cast<float*>(a.out) + at) = float2{o.x * inv, o.y * inv};
-  else *reinterpret_cast<half2_t*>(static_cast<_Float16*>(a.out) + at) = half2_t{(_Float16)(o.x * inv), (_Float16)(o.y * inv)};
+  const long long at = b * a.out_batch + (h * a.heads_per_kv + row - i * a.heads_per_kv) * a.out_head + i * a.out_token + channel;
+  store_four(a, at, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
 }
 
 template <bool E4M3>
@@ -414,9 +407,9 @@ hipError_t launch_rows(const BlockAttnArgs& a, int group_rows, hipStream_t strea
   const long long groups = a.table ? a.list_groups : (long long)a.s.batch * a.s.n_kv_heads * a.row_blocks * a.n_splits;
   if (groups >= (1LL << 31)) return hipErrorInvalidValue;
   switch (group_rows) {
-    case 16: block_attention_kernel<E4M3, 1><<<(unsigned)groups, 64 * kBlockWaves, 0, stream>>>(a); break;
-    case 32: block_attention_kernel<E4M3, 2><<<(unsigned)groups, 64 * kBlockWaves, 0, stream>>>(a); break;
-    case 64: block_attention_kernel<E4M3, 4><<<(unsigned)groups, 64 * kBlockWaves, 0, stream>>>(a); break;
+    case 16: block_attention_kernel<E4M3, 1><<<(unsigned)groups, 64 * block_waves(group_rows), 0, stream>>>(a); break;
+    case 32: block_attention_kernel<E4M3, 2><<<(unsigned)groups, 64 * block_waves(group_rows), 0, stream>>>(a); break;
+    case 64: block_attention_kernel<E4M3, 4><<<(unsigned)groups, 64 * block_waves(group_rows), 0, stream>>>(a); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
@@ -429,7 +422,7 @@ hipError_t launch_block_attention(const BlockAttnArgs& a, bool e4m3, int group_r
 }
 
 hipError_t launch_block_merge(const BlockAttnArgs& a, int group_rows, hipStream_t stream) {
-  const long long blocks = ceil_div((long long)a.s.t_new * a.heads_per_kv, 4), all = (long long)a.s.batch * a.s.n_kv_heads * blocks;
+  const long long blocks = ceil_div((long long)a.s.t_new * a.heads_per_kv, kMergeRows), all = (long long)a.s.batch * a.s.n_kv_heads * blocks;
   if (all >= (1LL << 31)) return hipErrorInvalidValue;
   block_merge_kernel<<<(unsigned)all, 256, 0, stream>>>(a, (int)blocks, group_rows);
   return hipGetLastError();

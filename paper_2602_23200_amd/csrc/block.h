@@ -65,8 +65,8 @@ struct BlockAttnArgs {
   float* ws;                           // slots: (level in the log2 domain, sum) of every row, then 128 sums of every row
   long long slots;                     // that ws holds
   float* ws_few;                       // merge of a list: the slots of the sequences of few rows (ws: of the others)
-  int few_rows;                        // rows of such a slot; of the sequences that have them
-  int few_most;
+  long long few_slots;
+  int few_rows, few_most;              // rows of such a slot; most rows of a sequence that has them
 };
 hipError_t launch_block_attention(const BlockAttnArgs& a, bool e4m3, int group_rows, hipStream_t stream);
 hipError_t launch_block_rows(const BlockAttnArgs& a, bool e4m3, int group_rows, hipStream_t stream);

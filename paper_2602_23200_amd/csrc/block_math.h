@@ -67,6 +67,7 @@ __device__ __forceinline__ int wave_sum(int x) {
 template <int ROWS>
 __device__ __forceinline__ bool find_work(const BlockAttnArgs& a, BlockWork& w) {
   constexpr int N = kBlockListMost / 64;
+  constexpr int ITEMS = block_round(ROWS);
   const int lane = (int)threadIdx.x & 63, per = a.list_groups / 8;
   const int item = (int)blockIdx.x < 8 * per ? (int)blockIdx.x % 8 * per + (int)blockIdx.x / 8 : (int)blockIdx.x;
   int units[N], tiles[N];                                // of the lane's sequences
@@ -92,13 +93,15 @@ __device__ __forceinline__ bool find_work(const BlockAttnArgs& a, BlockWork& w) 
     work += __shfl_xor(work, i);
   }
   most = __builtin_amdgcn_readfirstlane(most);
-  int length = __builtin_amdgcn_readfirstlane(block_first_length(work));
+  int length = __builtin_amdgcn_readfirstlane(block_first_length(work, ITEMS));
   int mine;
-  for (;; length = block_next_length(length)) {
+  while (true) {
     mine = 0;
 #pragma unroll
     for (int j = 0; j < N; ++j) mine += units[j] * block_ranges(tiles[j], length);
-    if (block_length_fits(length, most, __builtin_amdgcn_readfirstlane(wave_sum(mine)))) break;
+    const int ranges = __builtin_amdgcn_readfirstlane(wave_sum(mine));
+    if (block_length_fits(length, most, ranges, ITEMS)) break;
+    length = __builtin_amdgcn_readfirstlane(block_next_length(length, ranges, ITEMS));
   }
   // the sequence whose items hold this one
   int before = mine;

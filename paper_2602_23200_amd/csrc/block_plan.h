@@ -15,14 +15,14 @@ constexpr long long block_packed(long long n, int block) { return n - n % block;
 
 // ---- attention.  A row: one query head of one new token; the rows of a kv head share its keys.
 
-constexpr int kBlockWaves = 4;          // wavefronts of a work-group, each with tiles of its own and the same rows
 constexpr int kBlockSplitMost = 256;    // most ranges the keys of a row are split into
 
-// Rows of a work-group.  Up to 64: its wavefronts have tiles of their own; more: each has a quarter of the rows.
+// Rows of a work-group.  Up to 64: its wavefronts have tiles of their own; more: each has a part of the rows.
 inline int block_rows(long long rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
 constexpr int kBlockFewRows = 64;
+constexpr int block_waves(int group_rows) { return group_rows == 16 || group_rows == 256 ? 8 : 4; }
 // Work-groups of that form that the chip holds at once.
-inline int block_round(int rows) { return rows == 64 || rows == 256 ? 256 : 512; }
+constexpr int block_round(int group_rows) { return group_rows == 32 || group_rows == 128 ? 512 : 256; }
 
 struct BlockSizes {
   long long heads, rows, row_blocks;    // sequence-heads of the cache; rows of one; work-groups that they take
@@ -40,18 +40,15 @@ inline BlockSizes block_sizes(const innerq_block_config_t& c, long long t_new) {
   s.split_most = (int)(most < 1 ? 1 : most);
   return s;
 }
-// Splits of the keys (tokens: the most a row attends to).  Few rows: not shorter than two tiles a wavefront.  Many: the least rounds x (units a
-// split + what a work-group costs besides).
+// Splits of the keys (tokens: the most a row attends to).  Few rows: the least tiles a wavefront, a second launch for the splits counted as ten of
+// them.  Many: the least rounds x (units a split + what a work-group costs besides).
 inline int block_splits(const BlockSizes& s, long long tokens) {
-  if (s.group_rows <= kBlockFewRows) {
-    const long long most = ceil_div(tokens, 2LL * kBlockTile * kBlockWaves);
-    return (int)(most < s.split_most ? most < 1 ? 1 : most : s.split_most);
-  }
   const long long units = ceil_div(tokens, kBlockTile);
   long long best = 1, best_cost = -1;
   for (long long n = 1; n <= s.split_most && n <= units; ++n) {
     const long long rounds = ceil_div(s.heads * s.row_blocks * n, block_round(s.group_rows));
-    const long long cost = rounds * (ceil_div(units, n) + 8) + (n > 1 ? 6 : 0);
+    const long long cost = s.group_rows <= kBlockFewRows ? ceil_div(units, n * block_waves(s.group_rows)) + (n > 1 ? 10 : 0)
+                                                         : rounds * (ceil_div(units, n) + 8) + (n > 1 ? 6 : 0);
     if (best_cost < 0 || cost < best_cost) { best = n; best_cost = cost; }
   }
   return (int)best;
@@ -60,20 +57,25 @@ inline int block_splits(const BlockSizes& s, long long tokens) {
 inline size_t block_slot_bytes(int group_rows) { return (size_t)group_rows * (kHeadDim + 2) * sizeof(float); }
 
 // A ragged batch of up to kBlockListMost sequences: work-groups find their work in a list made from the counts, one launch for the sequences of few
-// rows and one for those of more.  kBlockListItems: work-groups that such a launch aims at, one round.
+// rows and one for those of more.  A launch aims at one round of work-groups.  (Sequences of few rows alone that fill half a round as they are
+// have no list: it costs 4 us in front of the first load, and a launch behind.)
 constexpr int kBlockListMost = 256;
-constexpr int kBlockListItems = 512;
 constexpr int kBlockListRows = 128;     // rows of a work-group of the second launch
 constexpr int kBlockTableBytes = 2 * kBlockListMost * (int)sizeof(int);   // first slot and splits of every sequence, at the workspace's start
 struct BlockList {
+  bool use;
   int few_rows;                         // rows of a work-group of the first launch
   long long few, many;                  // most work-groups of either (none: 0)
 };
 inline BlockList block_list(const innerq_block_config_t& c, long long t_new) {
   const long long rows = t_new * (c.n_q_heads / c.n_kv_heads), heads = (long long)c.batch * c.n_kv_heads;
   const long long blocks = heads * ceil_div(rows, kBlockListRows);
-  return {rows > kBlockFewRows ? kBlockFewRows : block_rows(rows), heads > kBlockListItems ? heads : kBlockListItems,
-          rows <= kBlockFewRows ? 0 : blocks > kBlockListItems ? blocks : kBlockListItems};
+  BlockList l;
+  l.few_rows = rows > kBlockFewRows ? kBlockFewRows : block_rows(rows);
+  l.few = heads > block_round(l.few_rows) ? heads : block_round(l.few_rows);
+  l.many = rows <= kBlockFewRows ? 0 : blocks > block_round(kBlockListRows) ? blocks : block_round(kBlockListRows);
+  l.use = c.batch <= kBlockListMost && (l.many || 2 * heads <= block_round(l.few_rows));
+  return l;
 }
 // What every work-group of such a launch works out for itself (constexpr: device code, too).  A sequence's share of a launch: units, each a kv head
 // and a block of `block` rows, and tiles of its keys (one, if there are none: zeros are written); none if its rows are not above `from` and up to `to`.
@@ -85,15 +87,20 @@ constexpr BlockShare block_share(int cached, int fresh, bool causal, int heads_p
   return {n_kv_heads * ((rows + block - 1) / block), tiles < 1 ? 1 : tiles};
 }
 // The keys of a unit are cut into ranges of `length` tiles, the same for all sequences: the first of these lengths with which the ranges are no
-// more than kBlockListItems, or that of the longest sequence, which cuts none.  work: tiles of all units.
+// more than `items`, or that of the longest sequence, which cuts none.  work: tiles of all units; ranges: with `length`.  (Ranges are work / length
+// and a part of one a unit; the next length is what would fit if those parts stayed the same, or a sixteenth more.)
 constexpr int kBlockListLeast = 8;      // (a range shorter than that is mostly set-up)
-constexpr int block_first_length(float work) {
-  const float even = work * (1.0f / kBlockListItems);
+constexpr int block_first_length(float work, int items) {
+  const float even = work / (float)items;
   return even < kBlockListLeast ? kBlockListLeast : even > 0x1p20f ? 1 << 20 : (int)even;
 }
-constexpr int block_next_length(int length) { return length + 1 + length / 16; }
+constexpr int block_next_length(int length, int ranges, int items) {
+  const float fits = (float)length * (float)ranges / (float)items;
+  const int least = length + 1 + length / 16;
+  return fits < (float)least || !(fits < 0x1p20f) ? least : (int)fits;
+}
 constexpr int block_ranges(int tiles, int length) { return (tiles + length - 1) / length; }
-constexpr bool block_length_fits(int length, int longest, int ranges) { return length >= longest || ranges <= kBlockListItems; }
+constexpr bool block_length_fits(int length, int longest, int ranges, int items) { return length >= longest || ranges <= items; }
 // Range number `at` of a sequence: row blocks of the same range, which read the same keys, are neighbours.
 struct BlockPlace { int h, row_block, split; };
 constexpr BlockPlace block_place(int at, int units, int n_kv_heads, int splits) {
@@ -104,10 +111,10 @@ constexpr BlockPlace block_place(int at, int units, int n_kv_heads, int splits) 
 inline size_t block_workspace_bytes(const innerq_block_config_t& c, long long t_new) {
   const BlockSizes s = block_sizes(c, t_new);
   size_t bytes = s.split_most == 1 ? 0 : (size_t)(s.heads * s.row_blocks * s.split_most) * block_slot_bytes(s.group_rows);
-  if (c.batch <= kBlockListMost) {
-    // (work-groups beyond the items that were aimed at have no partial results: their sequences are not split)
-    const BlockList l = block_list(c, t_new);
-    const size_t list = (size_t)kBlockListItems * (block_slot_bytes(l.few_rows) + (l.many ? block_slot_bytes(kBlockListRows) : 0));
+  const BlockList l = block_list(c, t_new);
+  if (l.use) {
+    // (work-groups beyond the round that was aimed at have no partial results: their sequences are not split)
+    const size_t list = block_round(l.few_rows) * block_slot_bytes(l.few_rows) + (l.many ? block_round(kBlockListRows) * block_slot_bytes(kBlockListRows) : 0);
     bytes = list > bytes ? list : bytes;
   }
   return kBlockTableBytes + bytes;
