@@ -315,20 +315,25 @@ block_rows_kernel(BlockAttnArgs a) {
     const long long open_at = bh * a.s.block * D;
     const __half *ko = a.s.k.open + open_at, *vo = a.s.v.open + open_at;
     const __half *kf = a.k.p + b * a.k.batch + h * a.k.head, *vf = a.v.p + b * a.v.batch + h * a.v.head;
+    // (selections, no branches: the lanes of a wavefront may differ)
+    auto row_at = [&](const __half* o, const __half* f, long long pitch, int i) {
+      const bool waits = i < open;
+      const unsigned long long step = waits ? (unsigned long long)D : (unsigned long long)pitch;
+      const unsigned at = (unsigned)(waits ? i : i - open);
+      return (waits ? o : f) + at * step;
+    };
     auto fetch = [&](int u, Staged& x, Scales& sc) {
       sc = Scales{scale, 0.f, 1.f, 1.f};
       const int i0 = u * kBlockTile;
       auto token = [&](int i) { return i0 + i < plain ? i0 + i : plain - 1; };   // (behind the last one: that one again, masked)
       constexpr int N = 8 / WAVES, PER = 16 / N, PAIRS = 64 / N;                 // (as put_plain)
-      const int i = token(tid / PER);
-      const __half* k = (i < open ? ko + i * D : kf + (i - open) * a.k.token) + tid % PER * 8 * N;
+      const __half* k = row_at(ko, kf, a.k.token, token(tid / PER)) + tid % PER * 8 * N;
       x.a = *reinterpret_cast<const u32x4*>(k);
       if (N == 2) x.b = *reinterpret_cast<const u32x4*>(k + 8);
       u32x2 w[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int j = token(4 * (tid / PAIRS) + e);
-        const __half* v = (j < open ? vo + j * D : vf + (j - open) * a.v.token) + tid % PAIRS * 2 * N;
+        const __half* v = row_at(vo, vf, a.v.token, token(4 * (tid / PAIRS) + e)) + tid % PAIRS * 2 * N;
         if (N == 2) w[e] = *reinterpret_cast<const u32x2*>(v);
         else w[e] = u32x2{*reinterpret_cast<const uint32_t*>(v), 0u};
       }

@@ -68,8 +68,7 @@ template <int ROWS>
 __device__ __forceinline__ bool find_work(const BlockAttnArgs& a, BlockWork& w) {
   constexpr int N = kBlockListMost / 64;
   constexpr int ITEMS = block_round(ROWS);
-  const int lane = (int)threadIdx.x & 63, per = a.list_groups / 8;
-  const int item = (int)blockIdx.x < 8 * per ? (int)blockIdx.x % 8 * per + (int)blockIdx.x / 8 : (int)blockIdx.x;
+  const int lane = (int)threadIdx.x & 63;
   int units[N], tiles[N];                                // of the lane's sequences
   int most = 1;
   float work = 0.f;
@@ -94,16 +93,18 @@ __device__ __forceinline__ bool find_work(const BlockAttnArgs& a, BlockWork& w) 
   }
   most = __builtin_amdgcn_readfirstlane(most);
   int length = __builtin_amdgcn_readfirstlane(block_first_length(work, ITEMS));
-  int mine;
+  int mine, ranges;
   while (true) {
     mine = 0;
 #pragma unroll
     for (int j = 0; j < N; ++j) mine += units[j] * block_ranges(tiles[j], length);
-    const int ranges = __builtin_amdgcn_readfirstlane(wave_sum(mine));
+    ranges = __builtin_amdgcn_readfirstlane(wave_sum(mine));
     if (block_length_fits(length, most, ranges, ITEMS)) break;
     length = __builtin_amdgcn_readfirstlane(block_next_length(length, ranges, ITEMS));
   }
-  // the sequence whose items hold this one
+  // this work-group's item (the launch has a multiple of eight work-groups), and the sequence whose items hold it
+  const int per = (ranges + 7) / 8, item = (int)blockIdx.x % 8 * per + (int)blockIdx.x / 8;
+  if ((int)blockIdx.x / 8 >= per) return false;          // (uniform)
   int before = mine;
 #pragma unroll
   for (int i = 1; i < 64; i *= 2) {

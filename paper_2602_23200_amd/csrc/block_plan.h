@@ -40,14 +40,14 @@ inline BlockSizes block_sizes(const innerq_block_config_t& c, long long t_new) {
   s.split_most = (int)(most < 1 ? 1 : most);
   return s;
 }
-// Splits of the keys (tokens: the most a row attends to).  Few rows: the least tiles a wavefront, a second launch for the splits counted as ten of
+// Splits of the keys (tokens: the most a row attends to).  Few rows: the least tiles a wavefront, a second launch for the splits counted as four of
 // them.  Many: the least rounds x (units a split + what a work-group costs besides).
 inline int block_splits(const BlockSizes& s, long long tokens) {
   const long long units = ceil_div(tokens, kBlockTile);
   long long best = 1, best_cost = -1;
   for (long long n = 1; n <= s.split_most && n <= units; ++n) {
     const long long rounds = ceil_div(s.heads * s.row_blocks * n, block_round(s.group_rows));
-    const long long cost = s.group_rows <= kBlockFewRows ? ceil_div(units, n * block_waves(s.group_rows)) + (n > 1 ? 10 : 0)
+    const long long cost = s.group_rows <= kBlockFewRows ? ceil_div(units, n * block_waves(s.group_rows)) + (n > 1 ? 4 : 0)
                                                          : rounds * (ceil_div(units, n) + 8) + (n > 1 ? 6 : 0);
     if (best_cost < 0 || cost < best_cost) { best = n; best_cost = cost; }
   }
@@ -65,15 +65,15 @@ constexpr int kBlockTableBytes = 2 * kBlockListMost * (int)sizeof(int);   // fir
 struct BlockList {
   bool use;
   int few_rows;                         // rows of a work-group of the first launch
-  long long few, many;                  // most work-groups of either (none: 0)
+  long long few, many;                  // most work-groups of either (none: 0), a multiple of eight
 };
 inline BlockList block_list(const innerq_block_config_t& c, long long t_new) {
   const long long rows = t_new * (c.n_q_heads / c.n_kv_heads), heads = (long long)c.batch * c.n_kv_heads;
   const long long blocks = heads * ceil_div(rows, kBlockListRows);
   BlockList l;
   l.few_rows = rows > kBlockFewRows ? kBlockFewRows : block_rows(rows);
-  l.few = heads > block_round(l.few_rows) ? heads : block_round(l.few_rows);
-  l.many = rows <= kBlockFewRows ? 0 : blocks > block_round(kBlockListRows) ? blocks : block_round(kBlockListRows);
+  l.few = (heads > block_round(l.few_rows) ? heads : block_round(l.few_rows)) + 7 & ~7LL;
+  l.many = rows <= kBlockFewRows ? 0 : (blocks > block_round(kBlockListRows) ? blocks : block_round(kBlockListRows)) + 7 & ~7LL;
   l.use = c.batch <= kBlockListMost && (l.many || 2 * heads <= block_round(l.few_rows));
   return l;
 }
