@@ -136,13 +136,13 @@ int attention(const innerq_block_config_t& c, const innerq_block_cache_t& k, con
     a.table = static_cast<int*>(workspace);
     a.few_slots = a.slots = block_round(list.few_rows);
     a.few_rows = list.few_rows;
-    a.few_most = a.rows_to = kBlockFewRows;
+    a.few_most = a.rows_to = kBlockListFew;
     a.list_groups = (int)list.few;
     hipError_t e = launch(list.few_rows);
     if (e == hipSuccess && list.many) {
       a.ws = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ws) + (size_t)a.few_slots * block_slot_bytes(list.few_rows));
       a.slots = block_round(kBlockListRows);
-      a.rows_from = kBlockFewRows; a.rows_to = 0x7fffffff;
+      a.rows_from = kBlockListFew; a.rows_to = 0x7fffffff;
       a.list_groups = (int)list.many;
       e = launch(kBlockListRows);
     }

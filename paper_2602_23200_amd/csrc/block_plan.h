@@ -60,6 +60,7 @@ inline size_t block_slot_bytes(int group_rows) { return (size_t)group_rows * (kH
 // rows and one for those of more.  A launch aims at one round of work-groups.  (Sequences of few rows alone that fill half a round as they are
 // have no list: it costs 4 us in front of the first load, and a launch behind.)
 constexpr int kBlockListMost = 256;
+constexpr int kBlockListFew = 32;       // most rows of a sequence of the first launch
 constexpr int kBlockListRows = 128;     // rows of a work-group of the second launch
 constexpr int kBlockTableBytes = 2 * kBlockListMost * (int)sizeof(int);   // first slot and splits of every sequence, at the workspace's start
 struct BlockList {
@@ -71,9 +72,9 @@ inline BlockList block_list(const innerq_block_config_t& c, long long t_new) {
   const long long rows = t_new * (c.n_q_heads / c.n_kv_heads), heads = (long long)c.batch * c.n_kv_heads;
   const long long blocks = heads * ceil_div(rows, kBlockListRows);
   BlockList l;
-  l.few_rows = rows > kBlockFewRows ? kBlockFewRows : block_rows(rows);
+  l.few_rows = rows > kBlockListFew ? kBlockListFew : block_rows(rows);
   l.few = (heads > block_round(l.few_rows) ? heads : block_round(l.few_rows)) + 7 & ~7LL;
-  l.many = rows <= kBlockFewRows ? 0 : (blocks > block_round(kBlockListRows) ? blocks : block_round(kBlockListRows)) + 7 & ~7LL;
+  l.many = rows <= kBlockListFew ? 0 : (blocks > block_round(kBlockListRows) ? blocks : block_round(kBlockListRows)) + 7 & ~7LL;
   l.use = c.batch <= kBlockListMost && (l.many || 2 * heads <= block_round(l.few_rows));
   return l;
 }
