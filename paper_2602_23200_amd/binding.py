@@ -633,30 +633,45 @@ def _checked(st: int, where: str) -> None:
         raise InnerQError(st, where)
 
 
+_byref = C.byref
+
+
+def _block_rows(t, batch: int, heads: int, tokens: int, dim: int, dtype=None):
+    """_rows for the calls below (a third of the host's time in a call on short sequences went into it)."""
+    if dtype is None:
+        import torch
+        dtype = torch.float16
+    b, h, n, one = t.stride()
+    assert t.is_cuda and t.dtype is dtype and t.shape == (batch, heads, tokens, dim) and one == 1
+    return t.data_ptr(), _byref(innerq_strides_t(b if batch > 1 else 0, h if heads > 1 else 0, n if tokens > 1 else 0))
+
+
 def innerq_block_append(cache: BlockCache, k_new, v_new, stream=None) -> None:
     """k_new, v_new: fp16 rows [B, Hk, T, d] wherever they lie; a block is packed when its last token arrives."""
-    cfg, T = cache.cfg, k_new.shape[2]
-    _checked(lib().innerq_block_append(C.byref(cfg), C.byref(cache.c), *_rows(k_new, cfg, cfg.n_kv_heads, T),
-                                       *_rows(v_new, cfg, cfg.n_kv_heads, T), T, _stream(stream)), "innerq_block_append")
+    cfg = cache.cfg
+    B, H, T, d = cfg.batch, cfg.n_kv_heads, k_new.shape[2], cfg.head_dim
+    _checked(lib().innerq_block_append(_byref(cfg), _byref(cache.c), *_block_rows(k_new, B, H, T, d), *_block_rows(v_new, B, H, T, d), T,
+                                       _stream(stream)), "innerq_block_append")
 
 
 def innerq_block_append_ragged(cache: BlockCache, n_tokens_dev, t_new_dev, k_new, v_new, stream=None) -> None:
     """innerq_block_append with the counts of every sequence in device memory (int32 CUDA tensors [B]): n_tokens_dev cached,
     advanced by the call, t_new_dev new ones, at most T (None: T each)."""
-    cfg, T = cache.cfg, k_new.shape[2]
-    _checked(lib().innerq_block_append_ragged(C.byref(cfg), C.byref(cache.c), _counts(n_tokens_dev, cfg), _counts(t_new_dev, cfg),
-                                              *_rows(k_new, cfg, cfg.n_kv_heads, T), *_rows(v_new, cfg, cfg.n_kv_heads, T), T,
-                                              _stream(stream)), "innerq_block_append_ragged")
+    cfg = cache.cfg
+    B, H, T, d = cfg.batch, cfg.n_kv_heads, k_new.shape[2], cfg.head_dim
+    _checked(lib().innerq_block_append_ragged(_byref(cfg), _byref(cache.c), _counts(n_tokens_dev, cfg), _counts(t_new_dev, cfg),
+                                              *_block_rows(k_new, B, H, T, d), *_block_rows(v_new, B, H, T, d), T, _stream(stream)),
+             "innerq_block_append_ragged")
 
 
 def _wanted_rows(t, cfg, count):
-    return (None, None) if t is None else _rows(t, cfg, cfg.n_kv_heads, count)
+    return (None, None) if t is None else _block_rows(t, cfg.batch, cfg.n_kv_heads, count, cfg.head_dim)
 
 
 def innerq_block_read(cache: BlockCache, first: int, k_out=None, v_out=None, stream=None):
     """Tokens first .. of every sequence into the fp16 rows k_out, v_out [B, Hk, T, d] (either may be None)."""
     cfg, T = cache.cfg, (v_out if k_out is None else k_out).shape[2]
-    _checked(lib().innerq_block_read(C.byref(cfg), C.byref(cache.c), first, T, *_wanted_rows(k_out, cfg, T), *_wanted_rows(v_out, cfg, T),
+    _checked(lib().innerq_block_read(_byref(cfg), _byref(cache.c), first, T, *_wanted_rows(k_out, cfg, T), *_wanted_rows(v_out, cfg, T),
                                      _stream(stream)), "innerq_block_read")
     return k_out, v_out
 
@@ -665,27 +680,27 @@ def innerq_block_read_ragged(cache: BlockCache, n_tokens_dev, first_dev, k_out=N
     """innerq_block_read with counts and first tokens (None: 0) of every sequence in device memory; rows of tokens that are not there are
     left as they were."""
     cfg, T = cache.cfg, (v_out if k_out is None else k_out).shape[2]
-    _checked(lib().innerq_block_read_ragged(C.byref(cfg), C.byref(cache.c), _counts(n_tokens_dev, cfg), _counts(first_dev, cfg), T,
+    _checked(lib().innerq_block_read_ragged(_byref(cfg), _byref(cache.c), _counts(n_tokens_dev, cfg), _counts(first_dev, cfg), T,
                                             *_wanted_rows(k_out, cfg, T), *_wanted_rows(v_out, cfg, T), _stream(stream)),
              "innerq_block_read_ragged")
     return k_out, v_out
 
 
-def _block_result(cache: BlockCache, q, out, workspace, stream):
+def _block_result(out, q, B: int, H: int, T: int, d: int, workspace, stream):
     """The arguments from the queries on, and the output."""
-    cfg, T = cache.cfg, q.shape[2]
     out = _chunk_out(out, q)
-    return out, (*_rows(q, cfg, cfg.n_q_heads, T), T, *_rows(out, cfg, cfg.n_q_heads, T, out.dtype), int(out.element_size() == 4),
-                 workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream))
+    return out, (*_block_rows(q, B, H, T, d), T, *_block_rows(out, B, H, T, d, out.dtype), int(out.element_size() == 4),
+                 workspace.data_ptr(), workspace.nbytes, _stream(stream))
 
 
 def innerq_block_attention(cache: BlockCache, k_new, v_new, q, workspace, out=None, stream=None):
     """q [B, Hq, T, d] attends to the cache and causally to the new rows k_new, v_new [B, Hk, T, d] (not appended by this call)
     -> out [B, Hq, T, d] (fp32 unless an fp16 `out` is passed)."""
-    cfg, T = cache.cfg, q.shape[2]
-    out, rest = _block_result(cache, q, out, workspace, stream)
-    _checked(lib().innerq_block_attention(C.byref(cfg), C.byref(cache.c), *_rows(k_new, cfg, cfg.n_kv_heads, T),
-                                          *_rows(v_new, cfg, cfg.n_kv_heads, T), *rest), "innerq_block_attention")
+    cfg = cache.cfg
+    B, H, T, d = cfg.batch, cfg.n_kv_heads, q.shape[2], cfg.head_dim
+    out, rest = _block_result(out, q, B, cfg.n_q_heads, T, d, workspace, stream)
+    _checked(lib().innerq_block_attention(_byref(cfg), _byref(cache.c), *_block_rows(k_new, B, H, T, d), *_block_rows(v_new, B, H, T, d),
+                                          *rest), "innerq_block_attention")
     return out
 
 
@@ -693,26 +708,28 @@ def innerq_block_attention_ragged(cache: BlockCache, n_tokens_dev, t_new_dev, ma
                                   stream=None):
     """innerq_block_attention with the counts of every sequence in device memory (int32 CUDA tensors [B]): n_tokens_dev cached, t_new_dev
     new ones, at most T (None: T each); max_tokens bounds their sum."""
-    cfg, T = cache.cfg, q.shape[2]
-    out, rest = _block_result(cache, q, out, workspace, stream)
-    _checked(lib().innerq_block_attention_ragged(C.byref(cfg), C.byref(cache.c), _counts(n_tokens_dev, cfg), _counts(t_new_dev, cfg),
-                                                 max_tokens, *_rows(k_new, cfg, cfg.n_kv_heads, T),
-                                                 *_rows(v_new, cfg, cfg.n_kv_heads, T), *rest), "innerq_block_attention_ragged")
+    cfg = cache.cfg
+    B, H, T, d = cfg.batch, cfg.n_kv_heads, q.shape[2], cfg.head_dim
+    out, rest = _block_result(out, q, B, cfg.n_q_heads, T, d, workspace, stream)
+    _checked(lib().innerq_block_attention_ragged(_byref(cfg), _byref(cache.c), _counts(n_tokens_dev, cfg), _counts(t_new_dev, cfg),
+                                                 max_tokens, *_block_rows(k_new, B, H, T, d), *_block_rows(v_new, B, H, T, d), *rest),
+             "innerq_block_attention_ragged")
     return out
 
 
 def innerq_block_cross_attention(cache: BlockCache, q, workspace, out=None, stream=None):
     """q [B, Hq, T, d] attends to all cached tokens -> out [B, Hq, T, d] (fp32 unless an fp16 `out` is passed)."""
-    out, rest = _block_result(cache, q, out, workspace, stream)
-    _checked(lib().innerq_block_cross_attention(C.byref(cache.cfg), C.byref(cache.c), *rest), "innerq_block_cross_attention")
+    cfg = cache.cfg
+    out, rest = _block_result(out, q, cfg.batch, cfg.n_q_heads, q.shape[2], cfg.head_dim, workspace, stream)
+    _checked(lib().innerq_block_cross_attention(_byref(cfg), _byref(cache.c), *rest), "innerq_block_cross_attention")
     return out
 
 
 def innerq_block_cross_attention_ragged(cache: BlockCache, n_tokens_dev, t_new_dev, max_tokens: int, q, workspace, out=None, stream=None):
     """innerq_block_cross_attention with the counts of every sequence in device memory; a sequence without a token has rows of zeros."""
     cfg = cache.cfg
-    out, rest = _block_result(cache, q, out, workspace, stream)
-    _checked(lib().innerq_block_cross_attention_ragged(C.byref(cfg), C.byref(cache.c), _counts(n_tokens_dev, cfg), _counts(t_new_dev, cfg),
+    out, rest = _block_result(out, q, cfg.batch, cfg.n_q_heads, q.shape[2], cfg.head_dim, workspace, stream)
+    _checked(lib().innerq_block_cross_attention_ragged(_byref(cfg), _byref(cache.c), _counts(n_tokens_dev, cfg), _counts(t_new_dev, cfg),
                                                        max_tokens, *rest), "innerq_block_cross_attention_ragged")
     return out
 

@@ -130,27 +130,27 @@ int attention(const innerq_block_config_t& c, const innerq_block_cache_t& k, con
   a.few_slots = a.few_rows = a.few_most = 0;
   const bool e4m3 = c.type == INNERQ_E4M3;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  auto launch = [&](int group_rows) { return group_rows <= kBlockFewRows ? launch_block_attention(a, e4m3, group_rows, stream) : launch_block_rows(a, e4m3, group_rows, stream); };
+  auto launch = [&](const BlockForm& form) { return form.rows <= kBlockFewRows ? launch_block_attention(a, e4m3, form, stream) : launch_block_rows(a, e4m3, form, stream); };
   const BlockList list = block_list(c, t_new);
   if (n_dev && list.use) {
     a.table = static_cast<int*>(workspace);
-    a.few_slots = a.slots = block_round(list.few_rows);
-    a.few_rows = list.few_rows;
+    a.few_slots = a.slots = block_round(list.form);
+    a.few_rows = list.form.rows;
     a.few_most = a.rows_to = kBlockListFew;
     a.list_groups = (int)list.few;
-    hipError_t e = launch(list.few_rows);
+    hipError_t e = launch(list.form);
     if (e == hipSuccess && list.many) {
-      a.ws = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ws) + (size_t)a.few_slots * block_slot_bytes(list.few_rows));
-      a.slots = block_round(kBlockListRows);
+      a.ws = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ws) + (size_t)a.few_slots * block_slot_bytes(list.form.rows));
+      a.slots = block_round(kBlockListMany);
       a.rows_from = kBlockListFew; a.rows_to = 0x7fffffff;
       a.list_groups = (int)list.many;
-      e = launch(kBlockListRows);
+      e = launch(kBlockListMany);
     }
-    if (e == hipSuccess) e = launch_block_merge(a, kBlockListRows, stream);
+    if (e == hipSuccess) e = launch_block_merge(a, kBlockListMany, stream);
     return e == hipSuccess ? INNERQ_OK : INNERQ_E_HIP;
   }
-  hipError_t e = launch(sizes.group_rows);
-  if (e == hipSuccess && a.n_splits > 1) e = launch_block_merge(a, sizes.group_rows, stream);
+  hipError_t e = launch(sizes.form);
+  if (e == hipSuccess && a.n_splits > 1) e = launch_block_merge(a, sizes.form, stream);
   return e == hipSuccess ? INNERQ_OK : INNERQ_E_HIP;
 }
 

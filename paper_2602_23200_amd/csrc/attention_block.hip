@@ -145,15 +145,14 @@ struct Plain {
   __device__ __forceinline__ const __half* value(int i) const { return i < open ? vo + i * D : vf + (i - open) * vp; }
 };
 
-template <bool E4M3, int NR>
-__global__ void __launch_bounds__(64 * block_waves(16 * NR)) __attribute__((amdgpu_waves_per_eu(NR == 4 ? 1 : 2))) block_attention_kernel(BlockAttnArgs a) {
+template <bool E4M3, int NR, int W>
+__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(NR == 4 ? 1 : 2))) block_attention_kernel(BlockAttnArgs a) {
   using K = Kernel<E4M3, NR>;
-  constexpr int W = block_waves(16 * NR);
   __shared__ float lds[W * NR * (32 + 2) * 64];
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
   BlockWork work;
   if (a.table) {
-    if (!find_work<16 * NR>(a, work)) return;            // (uniform)
+    if (!find_work<16 * NR, W>(a, work)) return;            // (uniform)
   } else {
     const unsigned per = (unsigned)a.row_blocks * (unsigned)a.n_splits, bh = blockIdx.x / per, rest = blockIdx.x % per;
     work = {(int)(bh / (unsigned)a.s.n_kv_heads), (int)(bh % (unsigned)a.s.n_kv_heads), (int)(rest / (unsigned)a.n_splits),
@@ -402,29 +401,33 @@ __global__ void __launch_bounds__(256) block_merge_kernel(BlockAttnArgs a, int b
   store_four(a, at, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
 }
 
-template <bool E4M3>
-hipError_t launch_rows(const BlockAttnArgs& a, int group_rows, hipStream_t stream) {
+template <bool E4M3, int NR, int W>
+hipError_t launch_form(const BlockAttnArgs& a, hipStream_t stream) {
   const long long groups = a.table ? a.list_groups : (long long)a.s.batch * a.s.n_kv_heads * a.row_blocks * a.n_splits;
   if (groups >= (1LL << 31)) return hipErrorInvalidValue;
-  switch (group_rows) {
-    case 16: block_attention_kernel<E4M3, 1><<<(unsigned)groups, 64 * block_waves(group_rows), 0, stream>>>(a); break;
-    case 32: block_attention_kernel<E4M3, 2><<<(unsigned)groups, 64 * block_waves(group_rows), 0, stream>>>(a); break;
-    case 64: block_attention_kernel<E4M3, 4><<<(unsigned)groups, 64 * block_waves(group_rows), 0, stream>>>(a); break;
+  block_attention_kernel<E4M3, NR, W><<<(unsigned)groups, 64 * W, 0, stream>>>(a);
+  return hipGetLastError();
+}
+template <bool E4M3>
+hipError_t launch_rows(const BlockAttnArgs& a, const BlockForm& form, hipStream_t stream) {
+  switch (form.rows) {
+    case 16: return form.waves == 4 ? launch_form<E4M3, 1, 4>(a, stream) : launch_form<E4M3, 1, 8>(a, stream);
+    case 32: return launch_form<E4M3, 2, 4>(a, stream);
+    case 64: return launch_form<E4M3, 4, 4>(a, stream);
     default: return hipErrorInvalidValue;
   }
-  return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_block_attention(const BlockAttnArgs& a, bool e4m3, int group_rows, hipStream_t stream) {
-  return e4m3 ? launch_rows<true>(a, group_rows, stream) : launch_rows<false>(a, group_rows, stream);
+hipError_t launch_block_attention(const BlockAttnArgs& a, bool e4m3, const BlockForm& form, hipStream_t stream) {
+  return e4m3 ? launch_rows<true>(a, form, stream) : launch_rows<false>(a, form, stream);
 }
 
-hipError_t launch_block_merge(const BlockAttnArgs& a, int group_rows, hipStream_t stream) {
+hipError_t launch_block_merge(const BlockAttnArgs& a, const BlockForm& form, hipStream_t stream) {
   const long long blocks = ceil_div((long long)a.s.t_new * a.heads_per_kv, kMergeRows), all = (long long)a.s.batch * a.s.n_kv_heads * blocks;
   if (all >= (1LL << 31)) return hipErrorInvalidValue;
-  block_merge_kernel<<<(unsigned)all, 256, 0, stream>>>(a, (int)blocks, group_rows);
+  block_merge_kernel<<<(unsigned)all, 256, 0, stream>>>(a, (int)blocks, form.rows);
   return hipGetLastError();
 }
 

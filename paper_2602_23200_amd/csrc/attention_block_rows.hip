@@ -218,7 +218,7 @@ block_rows_kernel(BlockAttnArgs a) {
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   BlockWork w;
   if (a.table) {
-    if (!find_work<ROWS>(a, w)) return;                  // (uniform)
+    if (!find_work<ROWS, WAVES>(a, w)) return;                  // (uniform)
   } else {
     // Sequence-heads that can be shared out evenly stay on one XCD (its L2 then brings every unit from memory once); the last rows, which have
     // the most keys, go first.
@@ -398,13 +398,13 @@ block_rows_kernel(BlockAttnArgs a) {
 
 }  // namespace
 
-hipError_t launch_block_rows(const BlockAttnArgs& a, bool e4m3, int group_rows, hipStream_t stream) {
+hipError_t launch_block_rows(const BlockAttnArgs& a, bool e4m3, const BlockForm& form, hipStream_t stream) {
   const long long groups = a.table ? a.list_groups : (long long)a.s.batch * a.s.n_kv_heads * a.row_blocks * a.n_splits;
   if (groups >= (1LL << 31)) return hipErrorInvalidValue;
-  if (group_rows == 128) {
+  if (form.rows == 128) {
     if (e4m3) block_rows_kernel<true, 4><<<(unsigned)groups, 256, 0, stream>>>(a);
     else block_rows_kernel<false, 4><<<(unsigned)groups, 256, 0, stream>>>(a);
-  } else if (group_rows == 256) {
+  } else if (form.rows == 256) {
     if (e4m3) block_rows_kernel<true, 8><<<(unsigned)groups, 512, 0, stream>>>(a);
     else block_rows_kernel<false, 8><<<(unsigned)groups, 512, 0, stream>>>(a);
   } else {

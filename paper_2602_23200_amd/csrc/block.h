@@ -68,8 +68,8 @@ struct BlockAttnArgs {
   long long few_slots;
   int few_rows, few_most;              // rows of such a slot; most rows of a sequence that has them
 };
-hipError_t launch_block_attention(const BlockAttnArgs& a, bool e4m3, int group_rows, hipStream_t stream);
-hipError_t launch_block_rows(const BlockAttnArgs& a, bool e4m3, int group_rows, hipStream_t stream);
-hipError_t launch_block_merge(const BlockAttnArgs& a, int group_rows, hipStream_t stream);
+hipError_t launch_block_attention(const BlockAttnArgs& a, bool e4m3, const BlockForm& form, hipStream_t stream);
+hipError_t launch_block_rows(const BlockAttnArgs& a, bool e4m3, const BlockForm& form, hipStream_t stream);
+hipError_t launch_block_merge(const BlockAttnArgs& a, const BlockForm& form, hipStream_t stream);
 
 }  // namespace innerq

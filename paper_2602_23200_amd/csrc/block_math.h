@@ -64,10 +64,10 @@ __device__ __forceinline__ int wave_sum(int x) {
 }
 // A ragged batch: work-groups find their work from the counts of all sequences (four a lane; the arithmetic is the plan's), every wavefront
 // the same.  Neighbours in the list, which share keys, go to one XCD.
-template <int ROWS>
+template <int ROWS, int WAVES>
 __device__ __forceinline__ bool find_work(const BlockAttnArgs& a, BlockWork& w) {
   constexpr int N = kBlockListMost / 64;
-  constexpr int ITEMS = block_round(ROWS);
+  constexpr int ITEMS = block_round(BlockForm{ROWS, WAVES});
   const int lane = (int)threadIdx.x & 63;
   int units[N], tiles[N];                                // of the lane's sequences
   int most = 1;

@@ -17,25 +17,30 @@ constexpr long long block_packed(long long n, int block) { return n - n % block;
 
 constexpr int kBlockSplitMost = 256;    // most ranges the keys of a row are split into
 
-// Rows of a work-group.  Up to 64: its wavefronts have tiles of their own; more: each has a part of the rows.
-inline int block_rows(long long rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
+// A work-group: its rows, and wavefronts.  Up to 64 rows: the wavefronts have tiles of their own; more: each has a part of the rows.
+struct BlockForm { int rows, waves; };
 constexpr int kBlockFewRows = 64;
-constexpr int block_waves(int group_rows) { return group_rows == 16 || group_rows == 256 ? 8 : 4; }
+// 16 rows: eight wavefronts leave fewer partial results where sequence-heads are few, four share the chip better where they are many (us, four and
+// eight: one token of 8 heads x 32k 25.7, 20.0; 32 x 8k 19.7, 17.9; 256 x 8k 84.8, 81.3; 512 x 1437 33.3, 35.7; 512 x 90 to 1437 17.5, 21.4).
+constexpr BlockForm block_form(long long rows, long long heads) {
+  if (rows <= 16) return {16, heads > 256 ? 4 : 8};
+  return rows <= 32 ? BlockForm{32, 4} : rows <= 64 ? BlockForm{64, 4} : rows <= 128 ? BlockForm{128, 4} : BlockForm{256, 8};
+}
 // Work-groups of that form that the chip holds at once.
-constexpr int block_round(int group_rows) { return group_rows == 32 || group_rows == 128 ? 512 : 256; }
+constexpr int block_round(const BlockForm& f) { return f.rows == 16 ? (f.waves == 4 ? 768 : 256) : f.rows == 32 || f.rows == 128 ? 512 : 256; }
 
 struct BlockSizes {
   long long heads, rows, row_blocks;    // sequence-heads of the cache; rows of one; work-groups that they take
-  int group_rows;                       // rows of a work-group
+  BlockForm form;
   int split_most;                       // most splits
 };
 inline BlockSizes block_sizes(const innerq_block_config_t& c, long long t_new) {
   BlockSizes s;
   s.heads = (long long)c.batch * c.n_kv_heads;
   s.rows = t_new * (c.n_q_heads / c.n_kv_heads);
-  s.group_rows = block_rows(s.rows);
-  s.row_blocks = ceil_div(s.rows, s.group_rows);
-  long long most = (s.group_rows > kBlockFewRows ? 2 : 1) * block_round(s.group_rows) / (s.heads * s.row_blocks);
+  s.form = block_form(s.rows, s.heads);
+  s.row_blocks = ceil_div(s.rows, s.form.rows);
+  long long most = (s.form.rows > kBlockFewRows ? 2 : 1) * block_round(s.form) / (s.heads * s.row_blocks);
   most = most > kBlockSplitMost ? kBlockSplitMost : most;
   s.split_most = (int)(most < 1 ? 1 : most);
   return s;
@@ -46,8 +51,8 @@ inline int block_splits(const BlockSizes& s, long long tokens) {
   const long long units = ceil_div(tokens, kBlockTile);
   long long best = 1, best_cost = -1;
   for (long long n = 1; n <= s.split_most && n <= units; ++n) {
-    const long long rounds = ceil_div(s.heads * s.row_blocks * n, block_round(s.group_rows));
-    const long long cost = s.group_rows <= kBlockFewRows ? ceil_div(units, n * block_waves(s.group_rows)) + (n > 1 ? 4 : 0)
+    const long long rounds = ceil_div(s.heads * s.row_blocks * n, block_round(s.form));
+    const long long cost = s.form.rows <= kBlockFewRows ? ceil_div(units, n * s.form.waves) + (n > 1 ? 4 : 0)
                                                          : rounds * (ceil_div(units, n) + 8) + (n > 1 ? 6 : 0);
     if (best_cost < 0 || cost < best_cost) { best = n; best_cost = cost; }
   }
@@ -61,21 +66,22 @@ inline size_t block_slot_bytes(int group_rows) { return (size_t)group_rows * (kH
 // have no list: it costs 4 us in front of the first load, and a launch behind.)
 constexpr int kBlockListMost = 256;
 constexpr int kBlockListFew = 32;       // most rows of a sequence of the first launch
-constexpr int kBlockListRows = 128;     // rows of a work-group of the second launch
+constexpr BlockForm kBlockListMany = {128, 4};           // work-groups of the second launch
 constexpr int kBlockTableBytes = 2 * kBlockListMost * (int)sizeof(int);   // first slot and splits of every sequence, at the workspace's start
 struct BlockList {
   bool use;
-  int few_rows;                         // rows of a work-group of the first launch
+  BlockForm form;                       // of the first launch
   long long few, many;                  // most work-groups of either (none: 0), a multiple of eight
 };
+constexpr BlockForm block_list_form(long long rows) { return rows <= 16 ? BlockForm{16, 4} : BlockForm{32, 4}; }
 inline BlockList block_list(const innerq_block_config_t& c, long long t_new) {
   const long long rows = t_new * (c.n_q_heads / c.n_kv_heads), heads = (long long)c.batch * c.n_kv_heads;
-  const long long blocks = heads * ceil_div(rows, kBlockListRows);
+  const long long blocks = heads * ceil_div(rows, kBlockListMany.rows);
   BlockList l;
-  l.few_rows = rows > kBlockListFew ? kBlockListFew : block_rows(rows);
-  l.few = (heads > block_round(l.few_rows) ? heads : block_round(l.few_rows)) + 7 & ~7LL;
-  l.many = rows <= kBlockListFew ? 0 : (blocks > block_round(kBlockListRows) ? blocks : block_round(kBlockListRows)) + 7 & ~7LL;
-  l.use = c.batch <= kBlockListMost && (l.many || 2 * heads <= block_round(l.few_rows));
+  l.form = block_list_form(rows);
+  l.few = (heads > block_round(l.form) ? heads : block_round(l.form)) + 7 & ~7LL;
+  l.many = rows <= kBlockListFew ? 0 : (blocks > block_round(kBlockListMany) ? blocks : block_round(kBlockListMany)) + 7 & ~7LL;
+  l.use = c.batch <= kBlockListMost && (l.many || 2 * heads <= block_round(l.form));
   return l;
 }
 // What every work-group of such a launch works out for itself (constexpr: device code, too).  A sequence's share of a launch: units, each a kv head
@@ -111,11 +117,11 @@ constexpr BlockPlace block_place(int at, int units, int n_kv_heads, int splits) 
 
 inline size_t block_workspace_bytes(const innerq_block_config_t& c, long long t_new) {
   const BlockSizes s = block_sizes(c, t_new);
-  size_t bytes = s.split_most == 1 ? 0 : (size_t)(s.heads * s.row_blocks * s.split_most) * block_slot_bytes(s.group_rows);
+  size_t bytes = s.split_most == 1 ? 0 : (size_t)(s.heads * s.row_blocks * s.split_most) * block_slot_bytes(s.form.rows);
   const BlockList l = block_list(c, t_new);
   if (l.use) {
     // (work-groups beyond the round that was aimed at have no partial results: their sequences are not split)
-    const size_t list = block_round(l.few_rows) * block_slot_bytes(l.few_rows) + (l.many ? block_round(kBlockListRows) * block_slot_bytes(kBlockListRows) : 0);
+    const size_t list = block_round(l.form) * block_slot_bytes(l.form.rows) + (l.many ? block_round(kBlockListMany) * block_slot_bytes(kBlockListMany.rows) : 0);
     bytes = list > bytes ? list : bytes;
   }
   return kBlockTableBytes + bytes;

@@ -152,8 +152,8 @@ int main() {
       const long long splits = block_splits(s, n), slots = s.heads * s.row_blocks * splits;
       const char* why = nullptr;
       if (splits < 1 || splits > s.split_most) why = "splits";
-      if (splits > 1 && slots * (long long)block_slot_bytes(s.group_rows) > room) why = "workspace";
-      if (s.row_blocks * s.group_rows < s.rows) why = "rows left out";
+      if (splits > 1 && slots * (long long)block_slot_bytes(s.form.rows) > room) why = "workspace";
+      if (s.row_blocks * s.form.rows < s.rows) why = "rows left out";
       ++plans;
       split += splits > 1;
       if (why && ++bad <= 10) printf("%s: batch %d heads %d r %d chunk %lld capacity %lld cached %lld\n", why, b, h, r, t, cap, n);
