@@ -75,6 +75,7 @@ __device__ __forceinline__ void pack_block(const BlockStore& s, const BlockTenso
   const __half* open = x.open + ((long long)b * s.n_kv_heads + h) * (32 * SUB) * D;
   const __half* rows = fresh.p + b * fresh.batch + h * fresh.head;
   auto row = [&](int i) { return g0 + i < n ? open + i * D : rows + (g0 + i - n) * fresh.token; };
+  const long long tile = block_tile(s, b, h, g0 / kBlockTile);
   uint32_t w[SUB][32];
   uint32_t most = 0u;
   if (keys) {
@@ -104,7 +105,6 @@ __device__ __forceinline__ void pack_block(const BlockStore& s, const BlockTenso
   const float largest = (float)__builtin_bit_cast(_Float16, (unsigned short)top);
   const float scale = largest / (E4M3 ? 448.f : 127.f);
   const Divisor by = {scale, scale == 0.f ? 0.f : 1.0f / scale};      // (a block of zeros: zeros)
-  const long long tile = block_tile(s, b, h, g0 / kBlockTile);
   if (lane == 0) x.scales[block_scale(s, tile)] = scale;
 #pragma unroll
   for (int u = 0; u < SUB; ++u) {
@@ -165,13 +165,13 @@ __device__ __forceinline__ void append_unit(const BlockAppendArgs& a, bool keys,
 
 // A wavefront a unit; heads of one token next to each other, as a projection leaves them.
 template <bool E4M3>
-__global__ void __launch_bounds__(256) block_append_kernel(BlockAppendArgs a, long long units) {
-  const long long unit = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+__global__ void __launch_bounds__(256) block_append_kernel(BlockAppendArgs a, unsigned units) {
+  const unsigned unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   if (unit >= units) return;
-  const int H = a.s.n_kv_heads, h = (int)(unit % H), lane = (int)threadIdx.x & 63;
-  const long long rest = unit / H;
+  const unsigned H = (unsigned)a.s.n_kv_heads, rest = unit / H;
+  const int h = (int)(unit - rest * H), lane = (int)threadIdx.x & 63;
   const bool keys = (rest & 1) == 0;
-  const int j = (int)((rest >> 1) % a.units), b = (int)((rest >> 1) / a.units);
+  const int b = (int)((rest >> 1) / (unsigned)a.units), j = (int)(rest >> 1) - b * a.units;
   append_unit<E4M3>(a, keys, b, h, j, take_of(a.s, b), lane);
 }
 
@@ -221,14 +221,14 @@ __device__ __forceinline__ void decode(uint32_t w, float scale, uint32_t (&out)[
 
 // A wavefront takes the tokens of one 32-token tile of a head that are asked for.
 template <bool E4M3>
-__global__ void __launch_bounds__(256) block_read_kernel(BlockReadArgs a, int tiles, long long units) {
-  const long long unit = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+__global__ void __launch_bounds__(256) block_read_kernel(BlockReadArgs a, unsigned tiles, unsigned units) {
+  const unsigned unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   if (unit >= units) return;
   const BlockStore& s = a.s;
-  const int H = s.n_kv_heads, h = (int)(unit % H), lane = (int)threadIdx.x & 63;
-  const long long rest = unit / H;
+  const unsigned H = (unsigned)s.n_kv_heads, rest = unit / H;
+  const int h = (int)(unit - rest * H), lane = (int)threadIdx.x & 63;
   const bool keys = (rest & 1) == 0;
-  const int j = (int)((rest >> 1) % tiles), b = (int)((rest >> 1) / tiles);
+  const int b = (int)((rest >> 1) / tiles), j = (int)((rest >> 1) - b * tiles);
   __half* out = keys ? a.k : a.v;
   if (!out) return;
   int n = s.n_tokens;
@@ -306,9 +306,9 @@ hipError_t launch_block_append(const BlockAppendArgs& a, int* counts, bool e4m3,
     return hipGetLastError();
   }
   const long long units = (long long)a.s.batch * a.s.n_kv_heads * 2 * a.units, groups = ceil_div(units, 4);
-  if (groups >= (1LL << 31)) return hipErrorInvalidValue;
-  if (e4m3) block_append_kernel<true><<<(unsigned)groups, 256, 0, stream>>>(a, units);
-  else block_append_kernel<false><<<(unsigned)groups, 256, 0, stream>>>(a, units);
+  if (units >= (1LL << 31)) return hipErrorInvalidValue;       // (4 KB of the store each: more than the card has)
+  if (e4m3) block_append_kernel<true><<<(unsigned)groups, 256, 0, stream>>>(a, (unsigned)units);
+  else block_append_kernel<false><<<(unsigned)groups, 256, 0, stream>>>(a, (unsigned)units);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && counts) {
     block_counts_kernel<<<(unsigned)ceil_div(a.s.batch, 256), 256, 0, stream>>>(a.s, counts);
@@ -321,9 +321,9 @@ hipError_t launch_block_read(const BlockReadArgs& a, bool e4m3, hipStream_t stre
   // (a range that begins inside a tile reaches into one more)
   const int tiles = (int)((a.s.n_dev ? kBlockTile - 1 : a.first % kBlockTile) + a.s.t_new - 1) / kBlockTile + 1;
   const long long units = (long long)a.s.batch * a.s.n_kv_heads * 2 * tiles, groups = ceil_div(units, 4);
-  if (groups >= (1LL << 31)) return hipErrorInvalidValue;
-  if (e4m3) block_read_kernel<true><<<(unsigned)groups, 256, 0, stream>>>(a, tiles, units);
-  else block_read_kernel<false><<<(unsigned)groups, 256, 0, stream>>>(a, tiles, units);
+  if (units >= (1LL << 31)) return hipErrorInvalidValue;       // (8 KB of rows each: more than the card has)
+  if (e4m3) block_read_kernel<true><<<(unsigned)groups, 256, 0, stream>>>(a, (unsigned)tiles, (unsigned)units);
+  else block_read_kernel<false><<<(unsigned)groups, 256, 0, stream>>>(a, (unsigned)tiles, (unsigned)units);
   return hipGetLastError();
 }
 
