@@ -8,9 +8,9 @@
 // is what the second product wants of it as an operand.  Nothing passes through LDS but the wavefronts' results.
 //
 // Codes become fp16 exactly (8-bit integers: put under the exponent that gives the last bit weight one, the bias subtracted; E4M3: the
-// conversion instruction).  The scale of a block of keys is applied to finished scores, that of a block of values to finished
-// sums of a tile, both in fp32, and weights enter the second product as two fp16 pieces (22 bits), so the result is that of fp32 arithmetic
-// on the values the cache stands for.  The additional instructions are free: the kernel waits for memory.
+// conversion instruction); scales are taken as block_math.h says.  Up to 32 rows weights enter the second product as two fp16 pieces (22 bits), so
+// the result is that of fp32 arithmetic on the values the cache stands for, and the kernel still waits for memory; for 64 rows that would cost
+// (8 sequences of 32k tokens, 48 rows: 133 us, with one piece 110), and weights are rounded to fp16 as they are for more rows.
 //
 // The softmax reference level is put 2^9 below the score that raises it and raised again only when a score passes it by 2^15, so outputs
 // are scaled rarely; the statistics of a row are shared by its four lanes only then.
@@ -50,9 +50,15 @@ struct Rows {
   float m[NR], l[NR];
 };
 
-// Weights of the scores of a tile (level and sum move on), in two pieces.  s[r][a][i]: token 16 a + 4 (lane / 16) + i.  by: factor of the scores.
 template <int NR>
-__device__ __forceinline__ void weights(Rows<NR>& r, float4_t (&s)[NR][2], float by, half8_t (&hi)[NR], half8_t (&lo)[NR]) {
+constexpr int kPieces = NR == 4 ? 1 : 2;                 // fp16 pieces of a weight
+
+__device__ __forceinline__ float largest_of(const float4_t (&s)[2]) {
+  return fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+}
+// Weights of the scores of a tile (level and sum move on).  s[r][a][i]: token 16 a + 4 (lane / 16) + i.
+template <int NR>
+__device__ __forceinline__ void weights(Rows<NR>& r, float4_t (&s)[NR][2], const Scales& u, half8_t (&p)[NR][kPieces<NR>]) {
   bool raise = false;
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
@@ -60,18 +66,16 @@ __device__ __forceinline__ void weights(Rows<NR>& r, float4_t (&s)[NR][2], float
     for (int a = 0; a < 2; ++a)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        s[n][a][i] *= by;
+        s[n][a][i] = __builtin_fmaf(s[n][a][i], u.by, u.add);
         asm("" : "+v"(s[n][a][i]));                      // (rounded before the level is taken from it: far levels need that)
       }
-    const float top = fmaxf(fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3])), fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3])));
-    raise |= top > __builtin_fmaf(-kFarShare, __builtin_fabsf(r.m[n]), r.m[n]) + kRaise || (r.m[n] == -INFINITY && top > -INFINITY);
+    raise |= largest_of(s[n]) > threshold(r.m[n]);
   }
   if (__builtin_amdgcn_ballot_w64(raise)) {
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
-      float top = fmaxf(fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3])), fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3])));
-      top = row_most(top);
-      const bool up = top > __builtin_fmaf(-kFarShare, __builtin_fabsf(r.m[n]), r.m[n]) + kRaise || (r.m[n] == -INFINITY && top > -INFINITY);
+      const float top = row_most(largest_of(s[n]));
+      const bool up = top > threshold(r.m[n]);
       const float level = up ? fmaxf(r.m[n], __builtin_fabsf(top) > kFar ? top : top - kTop) : r.m[n];
       const float f = up ? __builtin_amdgcn_exp2f(r.m[n] - level) : 1.f;         // (0 from the empty state)
       r.l[n] *= f;
@@ -88,53 +92,51 @@ __device__ __forceinline__ void weights(Rows<NR>& r, float4_t (&s)[NR][2], float
     for (int a = 0; a < 2; ++a)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float p = __builtin_amdgcn_exp2f(s[n][a][i] - level);
-        hi[n][4 * a + i] = (_Float16)p;
-        lo[n][4 * a + i] = (_Float16)(p - (float)hi[n][4 * a + i]);
-        sum += p;
+        const float w = __builtin_amdgcn_exp2f(s[n][a][i] - level);
+        p[n][0][4 * a + i] = (_Float16)w;
+        if constexpr (kPieces<NR> == 2) p[n][1][4 * a + i] = (_Float16)(w - (float)p[n][0][4 * a + i]);
+        sum += kPieces<NR> == 2 ? w : (float)p[n][0][4 * a + i];
       }
-    r.l[n] += sum;
+    r.l[n] = __builtin_fmaf(sum, u.inv, r.l[n]);
   }
 }
 
-// One tile's codes as they are loaded, and where they are.
+// One tile's codes as they are loaded, and its scales.
 struct Tile {
   u32x4 k[4], v[4];
-  float ks, vs;
+  Scales scales;
 };
 
+template <int NR>
+__device__ __forceinline__ void add_values(Rows<NR>& r, int x, const half8_t& v, const half8_t (&p)[NR][kPieces<NR>]) {
+#pragma unroll
+  for (int n = 0; n < NR; ++n)
+#pragma unroll
+    for (int i = 0; i < kPieces<NR>; ++i) r.o[n][x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[n][i], r.o[n][x], 0, 0, 0);
+}
 template <bool E4M3, int NR>
-struct Kernel {
-  static __device__ __forceinline__ void scores(const Rows<NR>& r, const Tile& t, float4_t (&s)[NR][2]) {
+__device__ __forceinline__ void use_tile(Rows<NR>& r, const Tile& t) {
+  float4_t s[NR][2];
 #pragma unroll
-    for (int a = 0; a < 2; ++a) {
+  for (int a = 0; a < 2; ++a) {
 #pragma unroll
-      for (int n = 0; n < NR; ++n) s[n][a] = float4_t{};
+    for (int n = 0; n < NR; ++n) s[n][a] = float4_t{};
 #pragma unroll
-      for (int st = 0; st < 4; ++st) {
-        const u32x4 w = t.k[2 * a + st / 2];
-        const half8_t k = st & 1 ? expand<E4M3>(w.z, w.w) : expand<E4M3>(w.x, w.y);
+    for (int st = 0; st < 4; ++st) {
+      const u32x4 w = t.k[2 * a + st / 2];
+      const half8_t k = st & 1 ? expand<E4M3>(w.z, w.w) : expand<E4M3>(w.x, w.y);
 #pragma unroll
-        for (int n = 0; n < NR; ++n) s[n][a] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, r.q[n][st], s[n][a], 0, 0, 0);
-      }
+      for (int n = 0; n < NR; ++n) s[n][a] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, r.q[n][st], s[n][a], 0, 0, 0);
     }
   }
-  static __device__ __forceinline__ void values(Rows<NR>& r, const Tile& t, const half8_t (&hi)[NR], const half8_t (&lo)[NR]) {
+  half8_t p[NR][kPieces<NR>];
+  weights<NR>(r, s, t.scales, p);
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+  for (int q = 0; q < 4; ++q)
 #pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        const half8_t v = m ? expand<E4M3>(t.v[q].z, t.v[q].w) : expand<E4M3>(t.v[q].x, t.v[q].y);
-#pragma unroll
-        for (int n = 0; n < NR; ++n) {
-          float4_t c = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, hi[n], float4_t{}, 0, 0, 0);
-          c = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, lo[n], c, 0, 0, 0);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) r.o[n][2 * q + m][i] = __builtin_fmaf(t.vs, c[i], r.o[n][2 * q + m][i]);
-        }
-      }
-  }
-};
+    for (int m = 0; m < 2; ++m)
+      add_values<NR>(r, 2 * q + m, m ? expand_by<E4M3>(t.v[q].z, t.v[q].w, t.scales.shrink) : expand_by<E4M3>(t.v[q].x, t.v[q].y, t.scales.shrink), p);
+}
 
 // A sequence's fp16 tokens behind the packed ones, in order: the open ones, then the new ones.
 struct Plain {
@@ -147,7 +149,6 @@ struct Plain {
 
 template <bool E4M3, int NR, int W>
 __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(NR == 4 ? 1 : 2))) block_attention_kernel(BlockAttnArgs a) {
-  using K = Kernel<E4M3, NR>;
   __shared__ float lds[W * NR * (32 + 2) * 64];
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
   BlockWork work;
@@ -175,7 +176,6 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(NR 
     r.m[n] = -INFINITY;
     r.l[n] = 0.f;
   }
-  const float scale = 0.08838834764831845f * 1.4426950408889634f;
 
   // this wavefront's share of the tiles: packed ones, then those of fp16 tokens
   const bool causal = a.k.p != nullptr;
@@ -187,47 +187,28 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(NR 
 
   const int u1 = t1 < tiles1 ? t1 : tiles1;
   if (t0 < u1) {
-    // Where 64 tiles lie, and their scales: a tile a lane.  Tiles are loaded two ahead (behind the last one: that one again).
-    long long at = 0;
-    float ks = 0.f, vs = 0.f;
-    int base = -64;
+    // (tiles are loaded two ahead; behind the last one: that one again)
+    BlockUnits units;
     auto load = [&](int u, Tile& t) {
       u = u < u1 ? u : u1 - 1;
-      if (u >= base + 64 || base < 0) {
-        base = u;
-        const int mine = u + lane < u1 ? u + lane : u1 - 1;
-        at = block_tile(a.s, b, h, mine);
-        const long long sc = block_scale(a.s, at);
-        ks = a.s.k.scales[sc];
-        vs = a.s.v.scales[sc];
-      }
-      const int i = u - base;
-      const long long tile = (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(at >> 32), i) << 32) |
-                                         (unsigned)__builtin_amdgcn_readlane((int)at, i));
-      const u32x4* kp = reinterpret_cast<const u32x4*>(a.s.k.codes + tile * kBlockTileBytes);
-      const u32x4* vp = reinterpret_cast<const u32x4*>(a.s.v.codes + tile * kBlockTileBytes);
+      units.look(a.s, b, h, u, u1, lane);
+      const long long tile = units.tile(u) * kBlockTileBytes;
+      const u32x4* kp = reinterpret_cast<const u32x4*>(a.s.k.codes + tile);
+      const u32x4* vp = reinterpret_cast<const u32x4*>(a.s.v.codes + tile);
 #pragma unroll
       for (int x = 0; x < 4; ++x) t.k[x] = __builtin_nontemporal_load(kp + 64 * x + lane);
 #pragma unroll
       for (int x = 0; x < 4; ++x) t.v[x] = __builtin_nontemporal_load(vp + 64 * x + lane);
-      t.ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks), i));
-      t.vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs), i));
-    };
-    auto use = [&](const Tile& t) {
-      float4_t sc[NR][2];
-      half8_t hi[NR], lo[NR];
-      K::scores(r, t, sc);
-      weights<NR>(r, sc, t.ks * scale, hi, lo);
-      K::values(r, t, hi, lo);
+      t.scales = units.scales(u);
     };
     Tile x, y;
     load(t0, x);
     load(t0 + 1, y);
     for (int u = t0;;) {
-      use(x);
+      use_tile<E4M3, NR>(r, x);
       if (++u == u1) break;
       load(u + 1, x);
-      use(y);
+      use_tile<E4M3, NR>(r, y);
       if (++u == u1) break;
       load(u + 1, y);
     }
@@ -267,29 +248,23 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(NR 
           for (int i = 0; i < 4; ++i)
             if (i0 + 16 * x + 4 * g + i > limit) sc[n][x][i] = -INFINITY;
       }
-      half8_t hi[NR], lo[NR];
-      weights<NR>(r, sc, scale, hi, lo);
+      half8_t w[NR][kPieces<NR>];
+      weights<NR>(r, sc, Scales{kScoreScale, 0.f, 1.f, 1.f}, w);
       const __half* vsrc[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) vsrc[j] = p.value(token(16 * (j >> 2) + 4 * g + (j & 3))) + 2 * c;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        uint32_t w[8], e[4], o[4];
+        uint32_t x[8], e[4], o[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = *reinterpret_cast<const uint32_t*>(vsrc[j] + 32 * q);
+        for (int j = 0; j < 8; ++j) x[j] = *reinterpret_cast<const uint32_t*>(vsrc[j] + 32 * q);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          e[j] = __builtin_amdgcn_perm(w[2 * j + 1], w[2 * j], 0x05040100u);
-          o[j] = __builtin_amdgcn_perm(w[2 * j + 1], w[2 * j], 0x07060302u);
+          e[j] = __builtin_amdgcn_perm(x[2 * j + 1], x[2 * j], 0x05040100u);
+          o[j] = __builtin_amdgcn_perm(x[2 * j + 1], x[2 * j], 0x07060302u);
         }
-        const half8_t v[2] = {__builtin_bit_cast(half8_t, u32x4{e[0], e[1], e[2], e[3]}), __builtin_bit_cast(half8_t, u32x4{o[0], o[1], o[2], o[3]})};
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-          for (int n = 0; n < NR; ++n) {
-            r.o[n][2 * q + m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[m], hi[n], r.o[n][2 * q + m], 0, 0, 0);
-            r.o[n][2 * q + m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[m], lo[n], r.o[n][2 * q + m], 0, 0, 0);
-          }
+        add_values<NR>(r, 2 * q, __builtin_bit_cast(half8_t, u32x4{e[0], e[1], e[2], e[3]}), w);
+        add_values<NR>(r, 2 * q + 1, __builtin_bit_cast(half8_t, u32x4{o[0], o[1], o[2], o[3]}), w);
       }
     }
   }

@@ -11,10 +11,7 @@
 // is left of the vector work, the next unit's level and the decoding of the one after, stands between the matrix instructions of the
 // second product, with the keys of the unit after the next on their way to registers.
 //
-// Codes are exact in fp16.  The scale of a block of keys is a factor of its scores, that of a block of values a summand of the exponent,
-// so a weight carries it: w = 2^(s + log2 S_v - level), O = sum w code, and the normaliser is l = sum w / S_v of the same rounded weights.  A block
-// of far smaller values than the largest ones so far would have weights that fp16 does not hold; below 1/16 of their scale it counts as one of
-// 2^k S_v and its codes are multiplied by 2^-k in LDS.
+// Codes are exact in fp16 and scales are taken as block_math.h says.
 #include "block.h"
 #include "block_math.h"
 
@@ -32,9 +29,6 @@ __device__ __forceinline__ float other_half(float x) {   // lane ^ 32
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float((threadIdx.x & 32u) ? r[0] : r[1]);
 }
-
-// What is uniform over a unit: factor of the scores, summand of the exponent, 1 / S_v, 2^-k.
-struct Scales { float by, add, inv, shrink; };
 
 struct State {
   half8_t q[8];
@@ -90,7 +84,6 @@ __device__ __forceinline__ void put_plain(char* buf, int tid, const Staged& x) {
 
 // ---- the two products and what is between them
 
-__device__ __forceinline__ float threshold(float m) { return __builtin_fmaf(-kFarShare, __builtin_fabsf(m), m) + kRaise; }
 // Largest of a lane's scores, as an exponent.
 __device__ __forceinline__ float unit_top(const float16_t& s, const Scales& u) {
   float t = s[0];
@@ -251,7 +244,6 @@ block_rows_kernel(BlockAttnArgs a) {
   r.m = r.raise = -INFINITY;
   r.l = r.zero = 0.f;
   r.far = false;
-  const float scale = 0.08838834764831845f * 1.4426950408889634f;
 
   const bool causal = a.k.p != nullptr;
   const int last_row = (row0 + ROWS < rows ? row0 + ROWS : rows) - 1;
@@ -262,48 +254,18 @@ block_rows_kernel(BlockAttnArgs a) {
 
   const int u1 = t1 < tiles1 ? t1 : tiles1;
   if (t0 < u1) {
-    // Where 64 units lie, and their scales: a unit a lane, two such sets (loads run four units ahead of the arithmetic).
-    long long at = 0;
-    float by = 0.f, add = 0.f, inv = 0.f, shrink = 1.f, largest = 0.f;
-    int base = -64;
-    auto look = [&](int u) {
-      if (u < base + 64 && base >= 0) return;
-      base = u;
-      const int mine = u + lane < u1 ? u + lane : u1 - 1;
-      at = block_tile(a.s, b, h, mine);
-      const long long sc = block_scale(a.s, at);
-      by = a.s.k.scales[sc] * scale;
-      const float vs = a.s.v.scales[sc];
-      float most = vs;
-#pragma unroll
-      for (int i = 32; i > 0; i /= 2) most = fmaxf(most, __shfl_xor(most, i));
-      largest = fmaxf(largest, most);
-      // S = 2^k vs, at least a sixteenth of the largest (no values but zeros: any)
-      const float least = largest > 0.f ? largest * 0.0625f : 1.f;
-      float eff = vs;
-      shrink = 1.f;
-      if (vs < least) {
-        const int k = vs > 0.f ? ilogbf(least) - ilogbf(vs) + 1 : 0;
-        eff = vs > 0.f ? ldexpf(vs, k) : least;
-        shrink = vs > 0.f ? ldexpf(1.f, -k) : 1.f;
-      }
-      add = __builtin_amdgcn_logf(eff);
-      inv = 1.0f / eff;
-    };
-    auto lane_of = [&](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
+    BlockUnits units;
     // (eight wavefronts: half of them bring keys, half values)
     const bool keys = WAVES == 4 || wave < 4;
     const uint32_t mine_at = (uint32_t)(64 * (wave & 3) + lane) * 16;
     const int to = put_at(keys, wave & 3, lane), apart = keys ? 512 : 256;
     const uint8_t* codes = keys ? a.s.k.codes : a.s.v.codes;
     auto fetch = [&](int u, Staged& x, Scales& sc) {
-      look(u);
-      const int i = u - base;
-      const long long tile = (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(at >> 32), i) << 32) |
-                                         (unsigned)__builtin_amdgcn_readlane((int)at, i)) * kBlockTileBytes;
+      units.look(a.s, b, h, u, u1, lane);
+      const long long tile = units.tile(u) * kBlockTileBytes;
       x.a = *reinterpret_cast<const u32x4*>(codes + tile + mine_at);
       if (WAVES == 4) x.b = *reinterpret_cast<const u32x4*>(a.s.v.codes + tile + mine_at);
-      sc = Scales{lane_of(by, i), lane_of(add, i), lane_of(inv, i), lane_of(shrink, i)};
+      sc = units.scales(u);
     };
     auto put = [&](char* buf, const Staged& x, const Scales& sc) {
       put_codes<E4M3>(buf + to, apart, x.a, keys ? 1.f : sc.shrink);
@@ -323,7 +285,7 @@ block_rows_kernel(BlockAttnArgs a) {
       return (waits ? o : f) + at * step;
     };
     auto fetch = [&](int u, Staged& x, Scales& sc) {
-      sc = Scales{scale, 0.f, 1.f, 1.f};
+      sc = Scales{kScoreScale, 0.f, 1.f, 1.f};
       const int i0 = u * kBlockTile;
       auto token = [&](int i) { return i0 + i < plain ? i0 + i : plain - 1; };   // (behind the last one: that one again, masked)
       constexpr int N = 8 / WAVES, PER = 16 / N, PAIRS = 64 / N;                 // (as put_plain)

@@ -54,6 +54,49 @@ __device__ __forceinline__ BlockSeq block_seq(const BlockAttnArgs& a, int b) {
   return s;
 }
 
+__device__ __forceinline__ float lane_of(float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); }
+// The magnitude that raises a level: beyond kFar the sooner, so that a weight stays in fp16 whatever the rounding of the sum.
+__device__ __forceinline__ float threshold(float m) { return __builtin_fmaf(-kFarShare, __builtin_fabsf(m), m) + kRaise; }
+
+// Scales.  That of a block of keys is a factor of its scores.  That of a block of values is a summand of the exponent, so that a weight carries it:
+//   w = 2^(s + log2 S - level),  O = sum w code,  l = sum w / S  (of the same rounded weights).
+// A block of far smaller values than the largest ones so far would have weights that fp16 does not hold, though they count in full in l; below 1/16
+// of that scale it is taken as S = 2^k S_v with codes times 2^-k (exact in fp16 down to 2^-24).
+struct Scales { float by, add, inv, shrink; };           // factor of the scores, log2 S, 1 / S, 2^-k
+
+constexpr float kScoreScale = 0.08838834764831845f * 1.4426950408889634f;        // log2(e) / sqrt(d)
+
+// Where 64 tiles of a sequence's kv head lie, and their scales: a tile a lane.
+struct BlockUnits {
+  long long at = 0;
+  float by = 0.f, add = 0.f, inv = 0.f, shrink = 1.f, largest = 0.f;
+  int base = -1;
+  // Tile u (not below an earlier one) is among them from now on; tiles end before u1.
+  __device__ __forceinline__ void look(const BlockStore& s, int b, int h, int u, int u1, int lane) {
+    if (base >= 0 && u < base + 64) return;              // (uniform)
+    base = u;
+    at = block_tile(s, b, h, u + lane < u1 ? u + lane : u1 - 1);
+    const long long sc = block_scale(s, at);
+    by = s.k.scales[sc] * kScoreScale;
+    const float vs = s.v.scales[sc];
+    float most = vs;
+#pragma unroll
+    for (int i = 32; i > 0; i /= 2) most = fmaxf(most, __shfl_xor(most, i));
+    largest = fmaxf(largest, most);
+    const float least = largest > 0.f ? largest * 0.0625f : 1.f;
+    const int k = vs < least && vs > 0.f ? __builtin_amdgcn_frexp_expf(least) - __builtin_amdgcn_frexp_expf(vs) + 1 : 0;
+    const float size = vs > 0.f ? __builtin_amdgcn_ldexpf(vs, k) : least;        // (no values but zeros: any)
+    shrink = __builtin_amdgcn_ldexpf(1.f, -k);
+    add = __builtin_amdgcn_logf(size);
+    inv = 1.0f / size;
+  }
+  __device__ __forceinline__ long long tile(int u) const {
+    return (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(at >> 32), u - base) << 32) |
+                       (unsigned)__builtin_amdgcn_readlane((int)at, u - base));
+  }
+  __device__ __forceinline__ Scales scales(int u) const { return {lane_of(by, u - base), lane_of(add, u - base), lane_of(inv, u - base), lane_of(shrink, u - base)}; }
+};
+
 // What a work-group does.
 struct BlockWork { int b, h, row_block, split, n_splits; long long slot; };
 

@@ -4,8 +4,9 @@ be from it (shared by the tests of those calls).
 What is left between a right result and attention in 64 bits over the values that the cache stands for, with p the softmax weights, e =
 2^-24, u = 2^-11, everything to first order (second orders are below 2^-10 of it, in the factor 1.01):
 * a score is a sum of 128 products, exact in fp32 (11 bits of a query, 8 of a code; new and open rows 11), each of whose additions is off by 2 e (a matrix
-  core may cut instead of rounding) of at most a = sum |q_c k_c| / sqrt(d); its factor, the factor's product and the level's subtraction round magnitudes up
-  to the largest |score| a few times, the exponential adds 2 e.  A weight moved by a share s moves the output by p s (v - out);
+  core may cut instead of rounding) of at most a = sum |q_c k_c| / sqrt(d); its factor, the sum with the logarithm of the values' scale (below 40) and the
+  level's subtraction round magnitudes up to the largest |score| and that logarithm a few times, the exponential, the logarithm and the scale's reciprocal
+  add 2 e each.  A weight moved by a share s moves the output by p s (v - out);
 * a weight enters the second product as two fp16 pieces, the second one rounded by u of what the first one left, which is u of the weight: u^2.  Below
   fp16's normal range the pieces' smallest step counts, 2^-25 at a level 2^9 below the largest weight: 2^-34 of that one;
 * many rows (form "many"): one piece, u of the weight (the normaliser sums the same rounded weights), and values rounded to fp16, u of each;
@@ -84,7 +85,7 @@ def attend(q, K, V, half, many=False, hidden=None):
         p = np.exp(s - s.max(-1, keepdims=True))
         p /= p.sum(-1, keepdims=True)
         out[g] = p @ v
-        share = p * ((u if many else u * u) + e * (256 * a + 8 * most + 8)) + 2.0 ** -34 * p.max(-1, keepdims=True) * ~hidden
+        share = p * ((u if many else u * u) + e * (256 * a + 8 * most + 50)) + 2.0 ** -34 * p.max(-1, keepdims=True) * ~hidden
         for i in range(t):                                  # (differences to the output: a row at a time)
             bound[g, i] = 1.01 * share[i] @ np.abs(v - out[g, i])
         bound[g] += (2 * (N + 600) * e + (1.01 * u if many else 0.0)) * (p @ np.abs(v)) + (2.0 ** -25 if many else 0.0)

@@ -8,7 +8,7 @@ from tests.chunk_reference import check
 
 pytestmark = pytest.mark.gpu
 D = 128
-MANY = 64                                                  # rows of a kv head up to which weights and values are not rounded to fp16
+MANY = 32                                                  # rows of a kv head up to which weights keep 22 bits
 
 
 @pytest.fixture(scope="module")
