@@ -9,7 +9,9 @@ What is left between a right result and attention in 64 bits over the values tha
   add 2 e each.  A weight moved by a share s moves the output by p s (v - out);
 * a weight enters the second product as two fp16 pieces, the second one rounded by u of what the first one left, which is u of the weight: u^2.  Below
   fp16's normal range the pieces' smallest step counts, 2^-25 at a level 2^9 below the largest weight: 2^-34 of that one;
-* many rows (form "many"): one piece, u of the weight (the normaliser sums the same rounded weights), and values rounded to fp16, u of each;
+* many rows: one piece, u of the weight (the normaliser sums the same rounded weights);
+* the codes of a block of values whose scale is below 1/16 of the largest enter times 2^-k, multiples of 2^-24: exact down to 2^-28 of that scale, below it off
+  by 2^-25 at a scale of at most 1/8 of the largest, which is 2^-35 of the largest value;
 * sums over tokens in fp32: 2 e of sum p |v| for every token and for every wavefront and range that a row is spread over;
 * an fp16 output is rounded by u of itself (2^-25 where it is a denormal)."""
 import numpy as np
@@ -88,7 +90,7 @@ def attend(q, K, V, half, many=False, hidden=None):
         share = p * ((u if many else u * u) + e * (256 * a + 8 * most + 50)) + 2.0 ** -34 * p.max(-1, keepdims=True) * ~hidden
         for i in range(t):                                  # (differences to the output: a row at a time)
             bound[g, i] = 1.01 * share[i] @ np.abs(v - out[g, i])
-        bound[g] += (2 * (N + 600) * e + (1.01 * u if many else 0.0)) * (p @ np.abs(v)) + (2.0 ** -25 if many else 0.0)
+        bound[g] += 2 * (N + 600) * e * (p @ np.abs(v)) + 2.0 ** -35 * np.abs(v).max()
     if half:
         bound += u * np.abs(out) + 2.0 ** -25
     return out, bound
