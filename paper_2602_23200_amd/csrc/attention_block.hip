@@ -317,16 +317,21 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(NR 
   }
 }
 
-// The splits of a row joined: half a wavefront a row, a lane four channels, eight splits under way.
-constexpr int kMergeRows = 8;                            // of a work-group
+// The splits of a row joined: half a wavefront a row, a lane four channels, eight splits under way (where there are fewer the last one is read again:
+// a form with four under way was as fast where rows are many and 1 us slower at the smallest calls).  The launch is bounded, and its
+// work-groups walk over the rows: of a padded batch most rows are not there, and starting work-groups for them cost more than the joining (16
+// sequences of 1 to 256 new tokens 183 us with a work-group for every eight rows, 177 with 4096 at most, 174 with 2048).
+constexpr int kMergeRows = 8;                            // of a work-group at once
+constexpr int kMergeGroups = 2048;                       // of a launch where rows are many
 __global__ void __launch_bounds__(256) block_merge_kernel(BlockAttnArgs a, int blocks, int group_rows) {
-  const int bh = (int)(blockIdx.x / (unsigned)blocks), row = (int)(blockIdx.x % (unsigned)blocks) * kMergeRows + ((int)threadIdx.x >> 5);
+  const int bh = (int)(blockIdx.x / (unsigned)blocks), first = (int)(blockIdx.x % (unsigned)blocks) * kMergeRows;
   const int b = bh / a.s.n_kv_heads, h = bh % a.s.n_kv_heads, channel = 4 * ((int)threadIdx.x & 31);
   const int own = block_seq(a, b).t * a.heads_per_kv;
-  if (row >= own) return;
-  int n_splits = a.n_splits, step_rows = group_rows;     // rows from one split to the next
+  if (first >= own) return;
+  int n_splits = a.n_splits, step = 1;                   // slots from one split to the next
   const float* ws = a.ws;
-  long long slots = a.slots, slot_row;
+  long long slots = a.slots, slot;                       // the first one's of the first rows
+  int row_step;                                          // .. and from one block of rows to the next
   if (a.table) {
     n_splits = a.table[2 * b + 1];
     if (n_splits == 1) return;                           // (written already)
@@ -335,45 +340,48 @@ __global__ void __launch_bounds__(256) block_merge_kernel(BlockAttnArgs a, int b
       ws = a.ws_few;
       slots = a.few_slots;
     }
-    const int blocks_of = (own + group_rows - 1) / group_rows;
-    slot_row = ((long long)a.table[2 * b] + (long long)h * blocks_of * n_splits + row / group_rows) * group_rows + row % group_rows;
-    step_rows = blocks_of * group_rows;
+    step = (own + group_rows - 1) / group_rows;
+    slot = a.table[2 * b] + (long long)h * step * n_splits;
+    row_step = 1;
   } else {
-    slot_row = ((long long)bh * a.row_blocks + row / group_rows) * n_splits * group_rows + row % group_rows;
+    slot = (long long)bh * a.row_blocks * n_splits;
+    row_step = n_splits;
   }
-  const float* ml = ws + slot_row * 2;
-  const float* po = ws + slots * (group_rows * 2) + slot_row * D + channel;
-  const long long step_ml = step_rows * 2, step_o = (long long)step_rows * D;
-  float level = -INFINITY, den = 0.f;
-  float4_t o = {};
-  for (int p0 = 0; p0 < n_splits; p0 += 8) {
-    float2 st[8];
-    float4_t v[8];
+  for (int row = first + ((int)threadIdx.x >> 5); row < own; row += blocks * kMergeRows) {
+    const long long at = (slot + (long long)(row / group_rows) * row_step) * group_rows + row % group_rows;
+    const float *ml = ws + at * 2, *po = ws + slots * (group_rows * 2) + at * D + channel;
+    const long long step_ml = (long long)step * group_rows * 2, step_o = (long long)step * group_rows * D;
+    float level = -INFINITY, den = 0.f;
+    float4_t o = {};
+    for (int p0 = 0; p0 < n_splits; p0 += 8) {
+      float2 st[8];
+      float4_t v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int p = p0 + e < n_splits ? p0 + e : n_splits - 1;
-      st[e] = *reinterpret_cast<const float2*>(ml + p * step_ml);
-      v[e] = *reinterpret_cast<const float4_t*>(po + p * step_o);
+      for (int e = 0; e < 8; ++e) {
+        const int p = p0 + e < n_splits ? p0 + e : n_splits - 1;
+        st[e] = *reinterpret_cast<const float2*>(ml + p * step_ml);
+        v[e] = *reinterpret_cast<const float4_t*>(po + p * step_o);
+      }
+      float top = level;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, st[e].x);
+      const float old = level == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(level - top);
+      den *= old;
+      o *= old;
+      level = top;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float f = p0 + e >= n_splits || st[e].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[e].x - top);
+        den = __builtin_fmaf(f, st[e].y, den);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(f, v[e][i], o[i]);
+      }
     }
-    float top = level;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) top = fmaxf(top, st[e].x);
-    const float old = level == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(level - top);
-    den *= old;
-    o *= old;
-    level = top;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float f = p0 + e >= n_splits || st[e].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[e].x - top);
-      den = __builtin_fmaf(f, st[e].y, den);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(f, v[e][i], o[i]);
-    }
+    const float inv = den > 0.f ? 1.0f / den : 0.f;
+    const int i = row / a.heads_per_kv;
+    const long long out = b * a.out_batch + (h * a.heads_per_kv + row - i * a.heads_per_kv) * a.out_head + i * a.out_token + channel;
+    store_four(a, out, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
   }
-  const float inv = den > 0.f ? 1.0f / den : 0.f;
-  const int i = row / a.heads_per_kv;
-  const long long at = b * a.out_batch + (h * a.heads_per_kv + row - i * a.heads_per_kv) * a.out_head + i * a.out_token + channel;
-  store_four(a, at, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
 }
 
 template <bool E4M3, int NR, int W>
@@ -400,7 +408,8 @@ hipError_t launch_block_attention(const BlockAttnArgs& a, bool e4m3, const Block
 }
 
 hipError_t launch_block_merge(const BlockAttnArgs& a, const BlockForm& form, hipStream_t stream) {
-  const long long blocks = ceil_div((long long)a.s.t_new * a.heads_per_kv, kMergeRows), all = (long long)a.s.batch * a.s.n_kv_heads * blocks;
+  const long long heads = (long long)a.s.batch * a.s.n_kv_heads, most = ceil_div((long long)a.s.t_new * a.heads_per_kv, kMergeRows);
+  const long long even = ceil_div(kMergeGroups, heads), blocks = most < even ? most : even, all = heads * blocks;
   if (all >= (1LL << 31)) return hipErrorInvalidValue;
   block_merge_kernel<<<(unsigned)all, 256, 0, stream>>>(a, (int)blocks, form.rows);
   return hipGetLastError();
