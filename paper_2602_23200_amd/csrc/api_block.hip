@@ -123,8 +123,7 @@ int attention(const innerq_block_config_t& c, const innerq_block_cache_t& k, con
   a.row_blocks = (int)sizes.row_blocks;
   a.n_splits = block_splits(sizes, tokens);
   a.table = nullptr;
-  a.list_groups = 0;
-  a.rows_from = 0; a.rows_to = 0x7fffffff;
+  a.list_few = a.list_many = 0;
   a.ws = a.ws_few = reinterpret_cast<float*>(static_cast<char*>(workspace) + kBlockTableBytes);
   a.slots = sizes.heads * sizes.row_blocks * a.n_splits;
   a.few_slots = a.few_rows = a.few_most = 0;
@@ -136,16 +135,14 @@ int attention(const innerq_block_config_t& c, const innerq_block_cache_t& k, con
     a.table = static_cast<int*>(workspace);
     a.few_slots = a.slots = block_round(list.form);
     a.few_rows = list.form.rows;
-    a.few_most = a.rows_to = kBlockListFew;
-    a.list_groups = (int)list.few;
-    hipError_t e = launch(list.form);
-    if (e == hipSuccess && list.many) {
+    a.few_most = kBlockListFew;
+    a.list_few = (int)list.few;
+    a.list_many = (int)list.many;
+    if (list.many) {
       a.ws = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ws) + (size_t)a.few_slots * block_slot_bytes(list.form.rows));
       a.slots = block_round(kBlockListMany);
-      a.rows_from = kBlockListFew; a.rows_to = 0x7fffffff;
-      a.list_groups = (int)list.many;
-      e = launch(kBlockListMany);
     }
+    hipError_t e = list.many ? launch_block_list(a, e4m3, stream) : launch(list.form);
     if (e == hipSuccess) e = launch_block_merge(a, kBlockListMany, stream);
     return e == hipSuccess ? INNERQ_OK : INNERQ_E_HIP;
   }

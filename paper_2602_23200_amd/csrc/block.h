@@ -60,16 +60,16 @@ struct BlockAttnArgs {
   int heads_per_kv;
   int row_blocks, n_splits;
   int* table;                          // a list: first slot and splits of every sequence are left here for the merge; else null
-  int list_groups;                     // work-groups of the launch
-  int rows_from, rows_to;              // sequences of this launch: with that many rows (from excluded, to included)
+  int list_few, list_many;             // work-groups of either kind
   float* ws;                           // slots: (level in the log2 domain, sum) of every row, then 128 sums of every row
   long long slots;                     // that ws holds
-  float* ws_few;                       // merge of a list: the slots of the sequences of few rows (ws: of the others)
+  float* ws_few;                       // a list with both kinds: the slots of the sequences of few rows (ws: of the others)
   long long few_slots;
   int few_rows, few_most;              // rows of such a slot; most rows of a sequence that has them
 };
 hipError_t launch_block_attention(const BlockAttnArgs& a, bool e4m3, const BlockForm& form, hipStream_t stream);
 hipError_t launch_block_rows(const BlockAttnArgs& a, bool e4m3, const BlockForm& form, hipStream_t stream);
+hipError_t launch_block_list(const BlockAttnArgs& a, bool e4m3, hipStream_t stream);     // both kinds
 hipError_t launch_block_merge(const BlockAttnArgs& a, const BlockForm& form, hipStream_t stream);
 
 }  // namespace innerq

@@ -106,9 +106,10 @@ __device__ __forceinline__ int wave_sum(int x) {
   return x;
 }
 // A ragged batch: work-groups find their work from the counts of all sequences (four a lane; the arithmetic is the plan's), every wavefront
-// the same.  Neighbours in the list, which share keys, go to one XCD.
+// the same: of the sequences with rows above `from` and up to `to`, those of work-group `group`.  Neighbours in the list, which share keys, go to one
+// XCD.
 template <int ROWS, int WAVES>
-__device__ __forceinline__ bool find_work(const BlockAttnArgs& a, BlockWork& w) {
+__device__ __forceinline__ bool find_work(const BlockAttnArgs& a, int from, int to, int group, BlockWork& w) {
   constexpr int N = kBlockListMost / 64;
   constexpr int ITEMS = block_round(BlockForm{ROWS, WAVES});
   const int lane = (int)threadIdx.x & 63;
@@ -121,7 +122,7 @@ __device__ __forceinline__ bool find_work(const BlockAttnArgs& a, BlockWork& w) 
     units[j] = tiles[j] = 0;
     if (b < a.s.batch) {
       const BlockSeq s = block_seq(a, b);
-      const BlockShare share = block_share(s.n, s.t, a.k.p != nullptr, a.heads_per_kv, a.s.n_kv_heads, a.rows_from, a.rows_to, ROWS);
+      const BlockShare share = block_share(s.n, s.t, a.k.p != nullptr, a.heads_per_kv, a.s.n_kv_heads, from, to, ROWS);
       units[j] = share.units;
       tiles[j] = share.tiles;
     }
@@ -146,8 +147,8 @@ __device__ __forceinline__ bool find_work(const BlockAttnArgs& a, BlockWork& w) 
     length = __builtin_amdgcn_readfirstlane(block_next_length(length, ranges, ITEMS));
   }
   // this work-group's item (the launch has a multiple of eight work-groups), and the sequence whose items hold it
-  const int per = (ranges + 7) / 8, item = (int)blockIdx.x % 8 * per + (int)blockIdx.x / 8;
-  if ((int)blockIdx.x / 8 >= per) return false;          // (uniform)
+  const int per = (ranges + 7) / 8, item = group % 8 * per + group / 8;
+  if (group / 8 >= per) return false;          // (uniform)
   int before = mine;
 #pragma unroll
   for (int i = 1; i < 64; i *= 2) {

@@ -61,16 +61,19 @@ inline int block_splits(const BlockSizes& s, long long tokens) {
 // A partial result of a work-group (a slot): level, sum and 128 sums of every row.
 inline size_t block_slot_bytes(int group_rows) { return (size_t)group_rows * (kHeadDim + 2) * sizeof(float); }
 
-// A ragged batch of up to kBlockListMost sequences: work-groups find their work in a list made from the counts, one launch for the sequences of few
-// rows and one for those of more.  A launch aims at one round of work-groups.  (Sequences of few rows alone that fill half a round as they are
-// have no list: it costs 4 us in front of the first load, and a launch behind.)
+// A ragged batch of up to kBlockListMost sequences: work-groups find their work in two lists made from the counts, of the sequences of few rows and of
+// those of more, each aimed at one round of work-groups.  With both they are one launch, the work-groups of many rows first: those of few rows find room
+// beside them and wait for memory while they compute (two launches and this one: 16 sequences of 1 to 256 new tokens over 1 to 16k 182 us, 167; 8 of 1 to
+// 40 over 1 to 4000 41.4, 32.2; 64 of 1 to 512 566, 551).  Sequences of few rows alone that fill half a round as they are have no list: it costs 4 us
+// in front of the first load, and a launch behind.  The second list's work-groups have 128 rows, not 256, and the first one's up to 32, not 64 (the
+// first of these cases, in two launches: 199 and 215 us; 187 and 199).
 constexpr int kBlockListMost = 256;
-constexpr int kBlockListFew = 32;       // most rows of a sequence of the first launch
-constexpr BlockForm kBlockListMany = {128, 4};           // work-groups of the second launch
+constexpr int kBlockListFew = 32;       // most rows of a sequence of the first list
+constexpr BlockForm kBlockListMany = {128, 4};           // work-groups of the second list
 constexpr int kBlockTableBytes = 2 * kBlockListMost * (int)sizeof(int);   // first slot and splits of every sequence, at the workspace's start
 struct BlockList {
   bool use;
-  BlockForm form;                       // of the first launch
+  BlockForm form;                       // of the first list
   long long few, many;                  // most work-groups of either (none: 0), a multiple of eight
 };
 constexpr BlockForm block_list_form(long long rows) { return rows <= 16 ? BlockForm{16, 4} : BlockForm{32, 4}; }
@@ -84,7 +87,7 @@ inline BlockList block_list(const innerq_block_config_t& c, long long t_new) {
   l.use = c.batch <= kBlockListMost && (l.many || 2 * heads <= block_round(l.form));
   return l;
 }
-// What every work-group of such a launch works out for itself (constexpr: device code, too).  A sequence's share of a launch: units, each a kv head
+// What every work-group works out for itself (constexpr: device code, too).  A sequence's share of a list: units, each a kv head
 // and a block of `block` rows, and tiles of its keys (one, if there are none: zeros are written); none if its rows are not above `from` and up to `to`.
 struct BlockShare { int units, tiles; };
 constexpr BlockShare block_share(int cached, int fresh, bool causal, int heads_per_kv, int n_kv_heads, int from, int to, int block) {

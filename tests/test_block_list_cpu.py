@@ -1,5 +1,5 @@
 """The launch plan of attention over the 8-bit cache (csrc/block_plan.h, whose arithmetic the kernels call), walked on the CPU over random
-calls.  Ragged batches: every (sequence, head, block of rows, range) is some work-group's exactly once, no item lies beyond the launch, and none that
+calls.  Ragged batches: every (sequence, head, block of rows, range) is some work-group's exactly once, no item lies beyond its list, and none that
 leaves a partial result beyond the workspace.  Calls of the same counts: as many ranges as the workspace holds, at any length."""
 import os
 import shutil
@@ -23,7 +23,7 @@ static void fail(const char* why, int batch, int heads, int r, int t) {
   if (++bad <= 10) printf("%s: batch %d heads %d r %d new %d\n", why, batch, heads, r, t);
 }
 
-// One launch: rows above `from` and up to `to`.
+// One list: rows above `from` and up to `to`.
 static void walk(const std::vector<int>& n, const std::vector<int>& t, bool causal, int heads, int r, int most_new, int from, int to, const BlockForm& f, long long groups,
                  float nudge) {
   const int batch = (int)n.size(), round = block_round(f);
@@ -36,7 +36,7 @@ static void walk(const std::vector<int>& n, const std::vector<int>& t, bool caus
     longest = std::max(longest, share[b].tiles);
     work += (float)share[b].units * (float)share[b].tiles;
     const int rows = t[b] * r;
-    if ((rows > from && rows <= to) != (share[b].units > 0)) fail("rows of the other launch", batch, heads, r, most_new);
+    if ((rows > from && rows <= to) != (share[b].units > 0)) fail("rows of the other list", batch, heads, r, most_new);
     if (share[b].units && (long long)share[b].units / heads * f.rows < rows) fail("rows left out", batch, heads, r, most_new);
     if (share[b].units && (long long)share[b].tiles * kBlockTile < n[b] + (causal ? t[b] : 0)) fail("tokens left out", batch, heads, r, most_new);
   }
@@ -123,7 +123,7 @@ int main() {
       n[b] = rng() % 4 == 0 ? 0 : draw(1, most_cached + 1);
       t[b] = rng() % 5 == 0 ? 0 : std::min(most_new, draw(1, most_new + 1));
     }
-    for (int x : t) if (x * r > (list.many ? kBlockListFew : list.form.rows) && !list.many) fail("no launch for these rows", batch, heads, r, most_new);
+    for (int x : t) if (x * r > (list.many ? kBlockListFew : list.form.rows) && !list.many) fail("no list for these rows", batch, heads, r, most_new);
     for (const float nudge : {1.0f, 0.999f, 1.001f}) {     // (the sum's order is the wavefront's own)
       walk(n, t, causal, heads, r, most_new, 0, kBlockListFew, list.form, list.few, nudge);
       if (list.many) walk(n, t, causal, heads, r, most_new, kBlockListFew, 0x7fffffff, kBlockListMany, list.many, nudge);
