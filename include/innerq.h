@@ -518,7 +518,8 @@ int innerq_block_append_ragged(const innerq_block_config_t *cfg, const innerq_bl
                                const void *v_new, const innerq_strides_t *v_strides, int64_t t_new, void *hip_stream);
 
 /* Tokens first .. first + count - 1 of every sequence as fp16 rows: fp16(fl(S * code)) of packed tokens, open ones as they came.
- *   k_out, v_out  device, fp16 rows (row i: token first + i); either may be NULL (with its strides) if it is not wanted
+ *   k_out, v_out  device, fp16 rows (row i: token first + i), not overlapping each other; either may be NULL (with its strides) if
+ *                 it is not wanted
  * INNERQ_E_ARG unless 0 <= first, 0 <= count and first + count <= n_tokens. */
 int innerq_block_read(const innerq_block_config_t *cfg, const innerq_block_cache_t *cache, int64_t first, int64_t count,
                       void *k_out, const innerq_strides_t *k_strides, void *v_out, const innerq_strides_t *v_strides,

@@ -109,7 +109,7 @@ def test_a_step_in_a_graph(env):
 
 
 def test_chunks_in_a_graph_and_other_streams(env):
-    """A long ragged chunk (two launches and a merge) in a graph on a side stream, two calls on two streams at once, and a given stream."""
+    """A long ragged chunk (sequences of few rows and of many, and a merge) in a graph on a side stream, two calls on two streams at once, and a given stream."""
     torch, iq = env
     rng = np.random.default_rng(4)
     lengths, T, Hk, r = [900, 64, 2000], 90, 2, 4
@@ -164,6 +164,84 @@ def test_batches_without_a_list(env, B, Hk, r, t):
         check(out[b, :, :m], *ref.attend(q[b, :, :m], *full, False, many, ref.causal(n, m)), b)
         check(cross[b, :, :m], *ref.attend(q[b, :, :m], *held, False, many), b)
         assert (out[b, :, m:] == 4.0).all() and (cross[b, :, m:] == 4.0).all()
+
+
+@pytest.mark.parametrize("B,Hk,r,t", [(256, 2, 4, 40), (100, 8, 1, 90), (64, 4, 8, 4)])
+def test_lists_of_many_sequences(env, B, Hk, r, t):
+    """Few and many rows, splits and none, empty sequences side by side; work-groups of the merge take rows one after the other.  Twice over one workspace, the
+    second time with other counts."""
+    torch, iq = env
+    rng = np.random.default_rng(B)
+    lengths = [int(n) for n in rng.integers(0, 100, B)]
+    for b, n in zip((0, 7, B // 2, B - 1), (3000, 0, 1500, 2211)):
+        lengths[b] = n
+    cache, _, counts, k, v = bc.filled(torch, iq, rng, lengths, Hk * r, Hk, True, 32, capacity=3136)
+    q, kn, vn = (rng.standard_normal((B, H, t, D)).astype(np.float16) for H in (Hk * r, Hk, Hk))
+    ws = iq.allocate_block_workspace(cache.cfg, t)
+    for turn in range(2):
+        new = [int(x) for x in (rng.integers(0, 3, B) if turn else rng.integers(0, t + 1, B))]
+        new[0], new[1], new[B - 1] = (1, t, 2) if turn else (t, 1, t)
+        out = torch.full((B, Hk * r, t, D), 4.0, device="cuda")
+        iq.innerq_block_attention_ragged(cache, counts, dev(torch, new), 3136, *(torch.from_numpy(x).cuda() for x in (kn, vn, q)), ws, out=out)
+        out = out.cpu().numpy()
+        for b in [0, 1, 2, 7, B // 2, B - 1]:
+            n, m = lengths[b], new[b]
+            full = [np.concatenate([ref.held(x[b, :, :n], 32, True), y[b, :, :m].astype(np.float64)], 1) for x, y in ((k, kn), (v, vn))]
+            check(out[b, :, :m], *ref.attend(q[b, :, :m], *full, False, t * r > 32, ref.causal(n, m)), (turn, b))
+            assert (out[b, :, m:] == 4.0).all()
+
+
+@pytest.mark.parametrize("t", [1, 100])
+def test_rows_of_all_heads_and_sequences_the_same(env, t):
+    """New keys and values broadcast over sequences and heads, queries over sequences (strides of zero); and more rows than the merge has work-groups for."""
+    torch, iq = env
+    rng = np.random.default_rng(t)
+    B, Hk, r, n = 8, 8, 4, 2000
+    cache, _, counts, k, v = bc.filled(torch, iq, rng, [n] * B, Hk * r, Hk, False, 64, capacity=2112)
+    q, kn, vn = (rng.standard_normal((1, H, t, D)).astype(np.float16) for H in (Hk * r, 1, 1))
+    rows = [torch.from_numpy(x).cuda().expand(B, H, t, D) for x, H in ((kn, Hk), (vn, Hk), (q, Hk * r))]
+    ws = iq.allocate_block_workspace(cache.cfg, t)
+    out = torch.empty(B, Hk * r, t, D, device="cuda")
+    iq.innerq_block_attention(cache, *rows, ws, out=out)
+    for b in (0, B - 1):
+        for h in (0, Hk - 1):
+            full = [np.concatenate([ref.held(x[b, h:h + 1], 64, False), y[0].astype(np.float64)], 1) for x, y in ((k, kn), (v, vn))]
+            at = slice(h * r, h * r + r)
+            check(out[b, at].cpu().numpy(), *ref.attend(q[0, at], *full, False, t * r > 32, ref.causal(n, t)), (b, h))
+    iq.innerq_block_append(cache, rows[0], rows[1])
+    for b in (0, B - 1):
+        bc.check_contents(iq, cache, None, b, *(np.concatenate([x[b], np.broadcast_to(y[0], (Hk, t, D))], 1) for x, y in ((k, kn), (v, vn))), False)
+
+
+def test_a_prefix_of_shared_pages(env):
+    """Two sequences whose tables name the same pages for their first 128 tokens and pages of their own behind: read and attended to by both, and left as they are
+    by what either appends."""
+    torch, iq = env
+    rng = np.random.default_rng(12)
+    Hk, r, cap, n = 2, 4, 320, 128
+    table = torch.tensor([[4, 2, 0, 1, 3], [4, 2, 7, 6, 5]], dtype=torch.int32, device="cuda")
+    cfg = iq.make_block_config(2, Hk * r, Hk, type=iq.E4M3, block=32, capacity_tokens=cap, page_pool_pages=8)
+    cache = iq.allocate_block_cache(cfg, page_table=table)
+    k, v = bc.keys_and_values(rng, [n + 90], Hk)
+    own_k, own_v = bc.keys_and_values(rng, [90], Hk)
+    K, V = ([x[0], np.concatenate([x[0, :, :n], y[0]], 1)] for x, y in ((k, own_k), (v, own_v)))
+    counts = dev(torch, [0, 0])
+    prefix = [torch.from_numpy(x[:, :, :n]).cuda().expand(2, Hk, n, D) for x in (k, v)]
+    iq.innerq_block_append_ragged(cache, counts, dev(torch, [n, 0]), *prefix)               # (by the first one)
+    counts[1] = n
+    before = {name: cache.buffers[name].cpu().numpy() for name in iq.BLOCK_BUFFER_NAMES if "open" not in name}
+    own = [torch.from_numpy(np.stack([x[b][:, n:] for b in range(2)])).cuda() for x in (K, V)]
+    iq.innerq_block_append_ragged(cache, counts, dev(torch, [90, 67]), *own)
+    lengths = [n + 90, n + 67]
+    for name, was in before.items():
+        pages = was.reshape(8, -1)
+        assert np.array_equal(cache.buffers[name].cpu().numpy().reshape(8, -1)[[2, 4]], pages[[2, 4]]), name
+    for b, m in enumerate(lengths):
+        bc.check_contents(iq, cache, table.cpu().numpy(), b, K[b][:, :m], V[b][:, :m], True)
+    q = rng.standard_normal((2, Hk * r, 3, D)).astype(np.float16)
+    out = iq.innerq_block_cross_attention_ragged(cache, counts, None, cap, torch.from_numpy(q).cuda(), iq.allocate_block_workspace(cfg, 3)).cpu().numpy()
+    for b, m in enumerate(lengths):
+        check(out[b], *ref.attend(q[b], *(ref.held(x[b][:, :m], 32, True) for x in (K, V)), True), b)
 
 
 def test_beams_share_a_sequence(env):
