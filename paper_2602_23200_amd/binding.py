@@ -646,12 +646,23 @@ def _block_rows(t, batch: int, heads: int, tokens: int, dim: int, dtype=None):
     return t.data_ptr(), _byref(innerq_strides_t(b if batch > 1 else 0, h if heads > 1 else 0, n if tokens > 1 else 0))
 
 
+def _block_stream(stream, t) -> Optional[int]:
+    """_stream for rows t, which lie on the current device: calls launch there."""
+    import torch
+    try:
+        device = torch._C._cuda_getDevice()
+    except AttributeError:                                # (a private name, as in _stream)
+        device = torch.cuda.current_device()
+    assert t.get_device() == device
+    return _stream(stream)
+
+
 def innerq_block_append(cache: BlockCache, k_new, v_new, stream=None) -> None:
     """k_new, v_new: fp16 rows [B, Hk, T, d] wherever they lie; a block is packed when its last token arrives."""
     cfg = cache.cfg
     B, H, T, d = cfg.batch, cfg.n_kv_heads, k_new.shape[2], cfg.head_dim
     _checked(lib().innerq_block_append(_byref(cfg), _byref(cache.c), *_block_rows(k_new, B, H, T, d), *_block_rows(v_new, B, H, T, d), T,
-                                       _stream(stream)), "innerq_block_append")
+                                       _block_stream(stream, k_new)), "innerq_block_append")
 
 
 def innerq_block_append_ragged(cache: BlockCache, n_tokens_dev, t_new_dev, k_new, v_new, stream=None) -> None:
@@ -660,7 +671,8 @@ def innerq_block_append_ragged(cache: BlockCache, n_tokens_dev, t_new_dev, k_new
     cfg = cache.cfg
     B, H, T, d = cfg.batch, cfg.n_kv_heads, k_new.shape[2], cfg.head_dim
     _checked(lib().innerq_block_append_ragged(_byref(cfg), _byref(cache.c), _counts(n_tokens_dev, cfg), _counts(t_new_dev, cfg),
-                                              *_block_rows(k_new, B, H, T, d), *_block_rows(v_new, B, H, T, d), T, _stream(stream)),
+                                              *_block_rows(k_new, B, H, T, d), *_block_rows(v_new, B, H, T, d), T,
+                                              _block_stream(stream, k_new)),
              "innerq_block_append_ragged")
 
 
@@ -670,18 +682,20 @@ def _wanted_rows(t, cfg, count):
 
 def innerq_block_read(cache: BlockCache, first: int, k_out=None, v_out=None, stream=None):
     """Tokens first .. of every sequence into the fp16 rows k_out, v_out [B, Hk, T, d] (either may be None)."""
-    cfg, T = cache.cfg, (v_out if k_out is None else k_out).shape[2]
+    cfg, some = cache.cfg, v_out if k_out is None else k_out
+    T = some.shape[2]
     _checked(lib().innerq_block_read(_byref(cfg), _byref(cache.c), first, T, *_wanted_rows(k_out, cfg, T), *_wanted_rows(v_out, cfg, T),
-                                     _stream(stream)), "innerq_block_read")
+                                     _block_stream(stream, some)), "innerq_block_read")
     return k_out, v_out
 
 
 def innerq_block_read_ragged(cache: BlockCache, n_tokens_dev, first_dev, k_out=None, v_out=None, stream=None):
     """innerq_block_read with counts and first tokens (None: 0) of every sequence in device memory; rows of tokens that are not there are
     left as they were."""
-    cfg, T = cache.cfg, (v_out if k_out is None else k_out).shape[2]
+    cfg, some = cache.cfg, v_out if k_out is None else k_out
+    T = some.shape[2]
     _checked(lib().innerq_block_read_ragged(_byref(cfg), _byref(cache.c), _counts(n_tokens_dev, cfg), _counts(first_dev, cfg), T,
-                                            *_wanted_rows(k_out, cfg, T), *_wanted_rows(v_out, cfg, T), _stream(stream)),
+                                            *_wanted_rows(k_out, cfg, T), *_wanted_rows(v_out, cfg, T), _block_stream(stream, some)),
              "innerq_block_read_ragged")
     return k_out, v_out
 
@@ -689,8 +703,9 @@ def innerq_block_read_ragged(cache: BlockCache, n_tokens_dev, first_dev, k_out=N
 def _block_result(out, q, B: int, H: int, T: int, d: int, workspace, stream):
     """The arguments from the queries on, and the output."""
     out = _chunk_out(out, q)
+    assert workspace.is_cuda and workspace.is_contiguous()
     return out, (*_block_rows(q, B, H, T, d), T, *_block_rows(out, B, H, T, d, out.dtype), int(out.element_size() == 4),
-                 workspace.data_ptr(), workspace.nbytes, _stream(stream))
+                 workspace.data_ptr(), workspace.nbytes, _block_stream(stream, q))
 
 
 def innerq_block_attention(cache: BlockCache, k_new, v_new, q, workspace, out=None, stream=None):

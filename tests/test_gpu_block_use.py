@@ -331,3 +331,23 @@ def test_a_sequence_of_the_largest_length(env):
         want = (2.0 + 0.5 * n * low) / (1.0 + n * low)
         # (63 tokens of the marked block differ by 0.004 in key and value: 2^-20 of all; sums of equal addends: 2^-23 each)
         assert (out - want).abs().max().item() <= want * 2.0 ** -23 * (n / 512 / 16 + 3000) + 1e-3, t
+
+
+def test_rows_of_another_device_are_refused(env, monkeypatch):
+    """Calls launch on the current device: with rows of another one nothing is launched."""
+    torch, iq = env
+    cache, _ = bc.empty(torch, iq, 1, 4, 1, 64, False, 32)
+    q, k, v = (torch.zeros(1, H, 2, D, dtype=torch.float16, device="cuda") for H in (4, 1, 1))
+    ws, counts = iq.allocate_block_workspace(cache.cfg, 2), dev(torch, [0])
+    monkeypatch.delattr(torch._C, "_cuda_getDevice", raising=False)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for call in (lambda: iq.innerq_block_append(cache, k, v), lambda: iq.innerq_block_append_ragged(cache, counts, None, k, v),
+                 lambda: iq.innerq_block_read(cache, 0, k, v), lambda: iq.innerq_block_read_ragged(cache, counts, None, None, v),
+                 lambda: iq.innerq_block_attention(cache, k, v, q, ws), lambda: iq.innerq_block_attention_ragged(cache, counts, None, 64, k, v, q, ws),
+                 lambda: iq.innerq_block_cross_attention(cache, q, ws), lambda: iq.innerq_block_cross_attention_ragged(cache, counts, None, 64, q, ws)):
+        with pytest.raises(AssertionError):
+            call()
+    monkeypatch.undo()
+    with pytest.raises(AssertionError):
+        iq.innerq_block_cross_attention(cache, q, ws.cpu())
+    assert cache.c.n_tokens == 0 and counts.tolist() == [0]
