@@ -110,7 +110,7 @@ int attention(const innerq_block_config_t& c, const innerq_block_cache_t& k, con
   if (!workspace) return INNERQ_E_NULL;
   if (misaligned(workspace)) return INNERQ_E_ALIGN;
   if (workspace_bytes < block_workspace_bytes(c, t_new)) return INNERQ_E_WORKSPACE;
-  const BlockSizes sizes = block_sizes(c, t_new);
+  const long long heads = (long long)c.batch * c.n_kv_heads;
   BlockAttnArgs a;
   a.s = store_of(c, k, n_dev, t_dev, t_new);
   a.k = causal ? rows_of(k_new, *k_strides) : RowView{nullptr, 0, 0, 0};
@@ -120,34 +120,37 @@ int attention(const innerq_block_config_t& c, const innerq_block_cache_t& k, con
   a.out_batch = out_strides->batch; a.out_head = out_strides->head; a.out_token = out_strides->token;
   a.out_is_fp32 = out_is_fp32;
   a.heads_per_kv = c.n_q_heads / c.n_kv_heads;
-  a.row_blocks = (int)sizes.row_blocks;
-  a.n_splits = block_splits(sizes, tokens);
   a.table = nullptr;
   a.list_few = a.list_many = 0;
   a.ws = a.ws_few = reinterpret_cast<float*>(static_cast<char*>(workspace) + kBlockTableBytes);
-  a.slots = sizes.heads * sizes.row_blocks * a.n_splits;
+  a.slots = a.row_blocks = a.n_splits = 0;
   a.few_slots = a.few_rows = a.few_most = 0;
   const bool e4m3 = c.type == INNERQ_E4M3;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   auto launch = [&](const BlockForm& form) { return form.rows <= kBlockFewRows ? launch_block_attention(a, e4m3, form, stream) : launch_block_rows(a, e4m3, form, stream); };
-  const BlockList list = block_list(c, t_new);
-  if (n_dev && list.use) {
+  const BlockList list = n_dev ? block_list(c, t_new, tokens) : BlockList{};
+  if (list.use) {
     a.table = static_cast<int*>(workspace);
     a.few_slots = a.slots = block_round(list.form);
     a.few_rows = list.form.rows;
-    a.few_most = kBlockListFew;
+    a.few_most = list.few_most;
     a.list_few = (int)list.few;
     a.list_many = (int)list.many;
     if (list.many) {
       a.ws = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ws) + (size_t)a.few_slots * block_slot_bytes(list.form.rows));
-      a.slots = block_round(kBlockListMany);
+      a.slots = block_round(kBlockMany.form);
     }
     hipError_t e = list.many ? launch_block_list(a, e4m3, stream) : launch(list.form);
-    if (e == hipSuccess) e = launch_block_merge(a, kBlockListMany, stream);
+    if (e == hipSuccess) e = launch_block_merge(a, kBlockMany.form, stream);
     return e == hipSuccess ? INNERQ_OK : INNERQ_E_HIP;
   }
-  hipError_t e = launch(sizes.form);
-  if (e == hipSuccess && a.n_splits > 1) e = launch_block_merge(a, sizes.form, stream);
+  // (ragged: how many tokens the sequences have is not known here)
+  const BlockPlan plan = block_plan(c, t_new, tokens, causal && !n_dev ? 0.5f * (float)t_new : 0.f);
+  a.row_blocks = (int)plan.row_blocks;
+  a.n_splits = plan.n_splits;
+  a.slots = heads * plan.row_blocks * plan.n_splits;
+  hipError_t e = launch(plan.form);
+  if (e == hipSuccess && a.n_splits > 1) e = launch_block_merge(a, plan.form, stream);
   return e == hipSuccess ? INNERQ_OK : INNERQ_E_HIP;
 }
 

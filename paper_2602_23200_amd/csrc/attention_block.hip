@@ -21,18 +21,16 @@ namespace {
 
 using namespace block_few;
 
-template <bool E4M3, int NR, int W>
+template <bool E4M3, int NR>
 __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(NR == 4 ? 1 : 2))) block_attention_kernel(BlockAttnArgs a) {
-  __shared__ float lds[kFloats<NR, W>];
+  __shared__ float lds[kFloats<NR>];
   BlockWork work;
   if (a.table) {
     if (!find_work<16 * NR, W>(a, 0, a.few_most, (int)blockIdx.x, work)) return;      // (uniform)
   } else {
-    const unsigned per = (unsigned)a.row_blocks * (unsigned)a.n_splits, bh = blockIdx.x / per, rest = blockIdx.x % per;
-    work = {(int)(bh / (unsigned)a.s.n_kv_heads), (int)(bh % (unsigned)a.s.n_kv_heads), (int)(rest / (unsigned)a.n_splits),
-            (int)(rest % (unsigned)a.n_splits), a.n_splits, (long long)blockIdx.x};
+    work = uniform_work(a);
   }
-  attend<E4M3, NR, W>(a, work, lds, a.ws, a.slots);
+  attend<E4M3, NR>(a, work, lds, a.ws, a.slots);
 }
 
 // The splits of a row joined: half a wavefront a row, a lane four channels, eight splits under way (where there are fewer the last one is read again:
@@ -102,19 +100,19 @@ __global__ void __launch_bounds__(256) block_merge_kernel(BlockAttnArgs a, int b
   }
 }
 
-template <bool E4M3, int NR, int W>
+template <bool E4M3, int NR>
 hipError_t launch_form(const BlockAttnArgs& a, hipStream_t stream) {
   const long long groups = a.table ? a.list_few : (long long)a.s.batch * a.s.n_kv_heads * a.row_blocks * a.n_splits;
   if (groups >= (1LL << 31)) return hipErrorInvalidValue;
-  block_attention_kernel<E4M3, NR, W><<<(unsigned)groups, 64 * W, 0, stream>>>(a);
+  block_attention_kernel<E4M3, NR><<<(unsigned)groups, 64 * W, 0, stream>>>(a);
   return hipGetLastError();
 }
 template <bool E4M3>
 hipError_t launch_rows(const BlockAttnArgs& a, const BlockForm& form, hipStream_t stream) {
   switch (form.rows) {
-    case 16: return form.waves == 4 ? launch_form<E4M3, 1, 4>(a, stream) : launch_form<E4M3, 1, 8>(a, stream);
-    case 32: return launch_form<E4M3, 2, 4>(a, stream);
-    case 64: return launch_form<E4M3, 4, 4>(a, stream);
+    case 16: return launch_form<E4M3, 1>(a, stream);
+    case 32: return launch_form<E4M3, 2>(a, stream);
+    case 64: return launch_form<E4M3, 4>(a, stream);
     default: return hipErrorInvalidValue;
   }
 }

@@ -342,35 +342,21 @@ __device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& 
 template <bool E4M3, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) block_rows_kernel(BlockAttnArgs a) {
   __shared__ __align__(16) char lds[kUnits * kUnitBytes];
-  // Sequence-heads that can be shared out evenly stay on one XCD (its L2 then brings every unit from memory once); the last rows, which have the
-  // most keys, go first.
-  const unsigned heads = (unsigned)(a.s.batch * a.s.n_kv_heads);
-  const bool pinned = heads % 8u == 0u;
-  const unsigned slot = pinned ? blockIdx.x / 8u : blockIdx.x, mine_heads = pinned ? heads / 8u : heads;
-  const unsigned rank = slot / (mine_heads * (unsigned)a.n_splits), rest = slot % (mine_heads * (unsigned)a.n_splits);
-  const unsigned bh = rest / (unsigned)a.n_splits + (pinned ? blockIdx.x % 8u * mine_heads : 0u);
-  BlockWork w;
-  w.split = (int)(rest % (unsigned)a.n_splits);
-  w.n_splits = a.n_splits;
-  w.row_block = a.row_blocks - 1 - (int)rank;
-  w.b = (int)(bh / (unsigned)a.s.n_kv_heads);
-  w.h = (int)(bh % (unsigned)a.s.n_kv_heads);
-  w.slot = ((long long)bh * a.row_blocks + w.row_block) * a.n_splits + w.split;
-  attend<E4M3, WAVES>(a, w, lds);
+  attend<E4M3, WAVES>(a, uniform_work(a), lds);
 }
 
 // A ragged batch with sequences of many rows and of few: the first work-groups have the former, those behind them the latter, which wait for memory
 // while others compute.
 template <bool E4M3>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) block_list_kernel(BlockAttnArgs a) {
-  constexpr int kFew = (int)sizeof(float) * block_few::kFloats<2, 4>, kMany = kUnits * kUnitBytes;
+  constexpr int kFew = (int)sizeof(float) * block_few::kFloats<2>, kMany = kUnits * kUnitBytes;
   __shared__ __align__(16) char lds[kFew > kMany ? kFew : kMany];
   BlockWork w;
   if ((int)blockIdx.x < a.list_many) {
     if (find_work<128, 4>(a, a.few_most, 0x7fffffff, (int)blockIdx.x, w)) attend<E4M3, 4>(a, w, lds);
   } else {
     if (find_work<32, 4>(a, 0, a.few_most, (int)blockIdx.x - a.list_many, w))
-      block_few::attend<E4M3, 2, 4>(a, w, reinterpret_cast<float*>(lds), a.ws_few, a.few_slots);
+      block_few::attend<E4M3, 2>(a, w, reinterpret_cast<float*>(lds), a.ws_few, a.few_slots);
   }
 }
 

@@ -134,11 +134,12 @@ struct Plain {
   __device__ __forceinline__ const __half* value(int i) const { return i < open ? vo + i * D : vf + (i - open) * vp; }
 };
 
-template <int NR, int W>
+constexpr int W = 4;                                    // wavefronts of a work-group
+template <int NR>
 constexpr int kFloats = W * NR * (32 + 2) * 64;          // of LDS
 
 // ws, slots: where partial results go, and how many it holds.
-template <bool E4M3, int NR, int W>
+template <bool E4M3, int NR>
 __device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& work, float* lds, float* ws, long long slots) {
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
   const int b = work.b, h = work.h;

@@ -100,6 +100,23 @@ struct BlockUnits {
 // What a work-group does.
 struct BlockWork { int b, h, row_block, split, n_splits; long long slot; };
 
+// The same counts for all, or the same work-groups whatever the counts: sequence-heads that can be shared out evenly stay on one XCD (its L2 then brings
+// every tile from memory once), those of a sequence, which are as long, on different ones; the last rows, which have the most keys, go first.
+__device__ __forceinline__ BlockWork uniform_work(const BlockAttnArgs& a) {
+  const unsigned heads = (unsigned)(a.s.batch * a.s.n_kv_heads), n = (unsigned)a.n_splits;
+  const bool pinned = heads % 8u == 0u && a.row_blocks > 1;
+  const unsigned at = pinned ? blockIdx.x / 8u : blockIdx.x, mine = pinned ? heads / 8u : heads;
+  const unsigned rank = at / (mine * n), rest = at % (mine * n), bh = pinned ? rest / n * 8u + blockIdx.x % 8u : rest / n;
+  BlockWork w;
+  w.b = (int)(bh / (unsigned)a.s.n_kv_heads);
+  w.h = (int)(bh % (unsigned)a.s.n_kv_heads);
+  w.row_block = a.row_blocks - 1 - (int)rank;
+  w.split = (int)(rest % n);
+  w.n_splits = a.n_splits;
+  w.slot = ((long long)bh * a.row_blocks + w.row_block) * a.n_splits + w.split;
+  return w;
+}
+
 __device__ __forceinline__ int wave_sum(int x) {
 #pragma unroll
   for (int i = 1; i < 64; i *= 2) x += __shfl_xor(x, i);

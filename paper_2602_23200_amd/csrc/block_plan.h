@@ -2,6 +2,9 @@
 // (no HIP); what kernels work out from counts in device memory is constexpr.
 #pragma once
 
+#include <cmath>
+#include <initializer_list>
+
 #include "plan.h"
 
 namespace innerq {
@@ -14,50 +17,78 @@ constexpr long long kBlockMostCapacity = 1LL << 24;      // tokens and their pro
 constexpr long long block_packed(long long n, int block) { return n - n % block; }
 
 // ---- attention.  A row: one query head of one new token; the rows of a kv head share its keys.
-
 constexpr int kBlockSplitMost = 256;    // most ranges the keys of a row are split into
 
 // A work-group: its rows, and wavefronts.  Up to 64 rows: the wavefronts have tiles of their own; more: each has a part of the rows.
 struct BlockForm { int rows, waves; };
 constexpr int kBlockFewRows = 64;
-// 16 rows: eight wavefronts leave fewer partial results where sequence-heads are few, four share the chip better where they are many (us, four and
-// eight: one token of 8 heads x 32k 25.7, 20.0; 32 x 8k 19.7, 17.9; 256 x 8k 84.8, 81.3; 512 x 1437 33.3, 35.7; 512 x 90 to 1437 17.5, 21.4).
-constexpr BlockForm block_form(long long rows, long long heads) {
-  if (rows <= 16) return {16, heads > 256 ? 4 : 8};
-  return rows <= 32 ? BlockForm{32, 4} : rows <= 64 ? BlockForm{64, 4} : rows <= 128 ? BlockForm{128, 4} : BlockForm{256, 8};
-}
 // Work-groups of that form that the chip holds at once.
-constexpr int block_round(const BlockForm& f) { return f.rows == 16 ? (f.waves == 4 ? 768 : 256) : f.rows == 32 || f.rows == 128 ? 512 : 256; }
+constexpr int block_round(const BlockForm& f) { return 256 * (f.rows == 16 ? 3 : f.rows == 32 || f.rows == 128 ? 2 : 1); }
 
-struct BlockSizes {
-  long long heads, rows, row_blocks;    // sequence-heads of the cache; rows of one; work-groups that they take
-  BlockForm form;
-  int split_most;                       // most splits
-};
-inline BlockSizes block_sizes(const innerq_block_config_t& c, long long t_new) {
-  BlockSizes s;
-  s.heads = (long long)c.batch * c.n_kv_heads;
-  s.rows = t_new * (c.n_q_heads / c.n_kv_heads);
-  s.form = block_form(s.rows, s.heads);
-  s.row_blocks = ceil_div(s.rows, s.form.rows);
-  long long most = (s.form.rows > kBlockFewRows ? 2 : 1) * block_round(s.form) / (s.heads * s.row_blocks);
-  most = most > kBlockSplitMost ? kBlockSplitMost : most;
-  s.split_most = (int)(most < 1 ? 1 : most);
-  return s;
+// What a form costs, us: before the first tile, for every tile that a wavefront (many rows: the work-group) takes one after the other, with a CU of its own
+// and in more than 256 work-groups; where the keys are split, for the second launch and for so many rows of partial results.  The constants are fitted to
+// 16700 timings of calls with 4 to 2048 rows of each of 1 to 1024 sequence-heads over 0 to 32k tokens, every form and number of ranges; of these
+// the one that is chosen takes 1.1 % longer than the fastest one in the mean, 27 % at worst.  (By the number of rows alone, with as many ranges as fill
+// the chip, calls of 17 rows and more took 25 % longer in the mean, three times as long at worst: 300 rows of 8 heads over 300 tokens 26 us, now 12;
+// 128 over 1682 29, now 13.)
+struct BlockKind { BlockForm form; float setup, tile, crowded, join, partial; };
+constexpr BlockKind kBlockKinds[] = {{{16, 4}, 5.0f, 0.62f, 1.4f, 3.0f, 4200.f},
+                                     {{32, 4}, 6.4f, 0.86f, 1.8f, 3.0f, 4200.f},
+                                     {{64, 4}, 8.3f, 1.2f, 1.2f, 3.0f, 6300.f},
+                                     {{128, 4}, 9.2f, 0.69f, 1.0f, 3.5f, 8400.f},
+                                     {{256, 8}, 9.3f, 0.89f, 0.89f, 4.4f, 8400.f}};
+constexpr BlockKind kBlockFew = kBlockKinds[1], kBlockMany = kBlockKinds[3];     // of a list
+// Bytes of the cache a us.  (Up to 224 work-groups no CU has two while another has none.  8 sequences of 8 heads over 32k tokens, one token: in 3 ranges 84 us,
+// 4 93, 6 90, 8 93, 12 91; 5 tokens: 93, 96, 97, 98.)
+constexpr float block_rate(float groups) { return groups <= 224.f ? 6.5e6f : 6.0e6f; }
+// Forms that come into question (of 16 rows a work-group for 17 and more reads the keys too often, of 64 for 129; wider ones would be empty for the most part).
+constexpr bool block_suits(const BlockForm& f, long long rows) {
+  return f.rows == 16 ? rows <= 16 : f.rows == 32 ? rows > 16 : f.rows == 64 ? rows > 32 && rows <= 128 : rows > f.rows / 2;
 }
-// Splits of the keys (tokens: the most a row attends to).  Few rows: the least tiles a wavefront, a second launch for the splits counted as four of
-// them.  Many: the least rounds x (units a split + what a work-group costs besides).
-inline int block_splits(const BlockSizes& s, long long tokens) {
-  const long long units = ceil_div(tokens, kBlockTile);
-  long long best = 1, best_cost = -1;
-  for (long long n = 1; n <= s.split_most && n <= units; ++n) {
-    const long long rounds = ceil_div(s.heads * s.row_blocks * n, block_round(s.form));
-    const long long cost = s.form.rows <= kBlockFewRows ? ceil_div(units, n * s.form.waves) + (n > 1 ? 4 : 0)
-                                                         : rounds * (ceil_div(units, n) + 8) + (n > 1 ? 6 : 0);
-    if (best_cost < 0 || cost < best_cost) { best = n; best_cost = cost; }
+// units: tiles of the longest row block; average: of one in the mean.
+inline float block_cost(const BlockKind& k, long long heads, long long row_blocks, float units, float average, int n) {
+  const float groups = (float)(heads * row_blocks) * (float)n, ways = (float)(k.form.rows <= kBlockFewRows ? n * k.form.waves : n);
+  const float share = units / ways, tile = groups <= 256.f ? k.tile : k.crowded, rounds = groups / (float)block_round(k.form);
+  float us = k.setup + 0.5f * (std::ceil(share) + (share < 1.f ? 1.f : share)) * tile;
+  if (rounds > 1.f) {
+    const float mean = average / ways, all = (rounds <= 3.f ? std::ceil(rounds) : rounds + 0.5f) * (k.setup + (mean < 0.5f ? 0.5f : mean) * tile);
+    us = all > us ? all : us;
   }
-  return (int)best;
+  const float bytes = (float)heads * units * (2 * kBlockTileBytes) / block_rate(groups);
+  us = std::sqrt(std::sqrt(us * us * us * us + bytes * bytes * bytes * bytes));      // (the larger of the two, and more where they are alike)
+  return us + (n > 1 ? k.join + 0.85f * (float)((n + 7) / 8) + groups * (float)k.form.rows / k.partial : 0.f);
 }
+// Most ranges: partial results for one round of work-groups (many rows: two).
+inline int block_split_most(const BlockForm& f, long long heads, long long row_blocks) {
+  const long long most = (f.rows > kBlockFewRows ? 2 : 1) * block_round(f) / (heads * row_blocks);
+  return (int)(most < 1 ? 1 : most > kBlockSplitMost ? kBlockSplitMost : most);
+}
+struct BlockPlan { BlockForm form; long long row_blocks; int n_splits; float us; };
+inline BlockPlan block_plan_of(const BlockKind& k, long long heads, long long rows, float units, float average) {
+  BlockPlan best = {k.form, ceil_div(rows, k.form.rows), 1, 0.f};
+  if (best.row_blocks == 1) average = units;
+  const int most = block_split_most(k.form, heads, best.row_blocks);
+  best.us = block_cost(k, heads, best.row_blocks, units, average, 1);
+  // (steps of an eighth and less)
+  for (int n = 2; n <= most && (float)n <= units; n += n < 8 ? 1 : n < 16 ? 2 : n < 32 ? 4 : n < 64 ? 8 : n < 128 ? 16 : 32) {
+    const float us = block_cost(k, heads, best.row_blocks, units, average, n);
+    if (us < best.us) { best.us = us; best.n_splits = n; }
+  }
+  return best;
+}
+// tokens: the most that a row attends to; of them, for the row block in the mean, `fewer` not.
+inline BlockPlan block_plan(const innerq_block_config_t& c, long long t_new, long long tokens, float fewer) {
+  const long long heads = (long long)c.batch * c.n_kv_heads, rows = t_new * (c.n_q_heads / c.n_kv_heads);
+  const float units = (float)ceil_div(tokens, kBlockTile), average = units - fewer / kBlockTile;
+  BlockPlan best = {};
+  for (const BlockKind& k : kBlockKinds) {
+    if (!block_suits(k.form, rows)) continue;
+    const BlockPlan x = block_plan_of(k, heads, rows, units, average);
+    if (best.n_splits == 0 || x.us < best.us) best = x;
+  }
+  return best;
+}
+
 // A partial result of a work-group (a slot): level, sum and 128 sums of every row.
 inline size_t block_slot_bytes(int group_rows) { return (size_t)group_rows * (kHeadDim + 2) * sizeof(float); }
 
@@ -68,24 +99,30 @@ inline size_t block_slot_bytes(int group_rows) { return (size_t)group_rows * (kH
 // in front of the first load, and a launch behind.  The second list's work-groups have 128 rows, not 256, and the first one's up to 32, not 64 (the
 // first of these cases, in two launches: 199 and 215 us; 187 and 199).
 constexpr int kBlockListMost = 256;
-constexpr int kBlockListFew = 32;       // most rows of a sequence of the first list
-constexpr BlockForm kBlockListMany = {128, 4};           // work-groups of the second list
 constexpr int kBlockTableBytes = 2 * kBlockListMost * (int)sizeof(int);   // first slot and splits of every sequence, at the workspace's start
 struct BlockList {
   bool use;
   BlockForm form;                       // of the first list
+  int few_most;                         // most rows of a sequence of the first list
   long long few, many;                  // most work-groups of either (none: 0), a multiple of eight
 };
-constexpr BlockForm block_list_form(long long rows) { return rows <= 16 ? BlockForm{16, 4} : BlockForm{32, 4}; }
-inline BlockList block_list(const innerq_block_config_t& c, long long t_new) {
+inline BlockList block_list_of(const innerq_block_config_t& c, long long t_new, bool all_few) {
   const long long rows = t_new * (c.n_q_heads / c.n_kv_heads), heads = (long long)c.batch * c.n_kv_heads;
-  const long long blocks = heads * ceil_div(rows, kBlockListMany.rows);
   BlockList l;
-  l.form = block_list_form(rows);
-  l.few = (heads > block_round(l.form) ? heads : block_round(l.form)) + 7 & ~7LL;
-  l.many = rows <= kBlockListFew ? 0 : (blocks > block_round(kBlockListMany) ? blocks : block_round(kBlockListMany)) + 7 & ~7LL;
-  l.use = c.batch <= kBlockListMost && (l.many || 2 * heads <= block_round(l.form));
+  l.form = rows <= 16 ? kBlockKinds[0].form : kBlockFew.form;
+  l.few_most = (int)(all_few || rows <= l.form.rows ? rows : l.form.rows);
+  const long long few = heads * ceil_div(l.few_most, l.form.rows), many = heads * ceil_div(rows, kBlockMany.form.rows);
+  l.few = (few > block_round(l.form) ? few : block_round(l.form)) + 7 & ~7LL;
+  l.many = rows <= l.few_most ? 0 : (many > block_round(kBlockMany.form) ? many : block_round(kBlockMany.form)) + 7 & ~7LL;
+  l.use = c.batch <= kBlockListMost && (rows > l.form.rows || 2 * few <= block_round(l.form));
   return l;
+}
+// Every sequence in the first list where a batch of the longest ones would be faster so.
+inline BlockList block_list(const innerq_block_config_t& c, long long t_new, long long tokens) {
+  const long long rows = t_new * (c.n_q_heads / c.n_kv_heads), heads = (long long)c.batch * c.n_kv_heads;
+  const float units = (float)ceil_div(tokens, kBlockTile);
+  const bool all_few = rows <= kBlockFew.form.rows || block_plan_of(kBlockFew, heads, rows, units, units).us <= block_plan_of(kBlockMany, heads, rows, units, units).us;
+  return block_list_of(c, t_new, all_few);
 }
 // What every work-group works out for itself (constexpr: device code, too).  A sequence's share of a list: units, each a kv head
 // and a block of `block` rows, and tiles of its keys (one, if there are none: zeros are written); none if its rows are not above `from` and up to `to`.
@@ -118,13 +155,21 @@ constexpr BlockPlace block_place(int at, int units, int n_kv_heads, int splits) 
   return {h, rest % blocks, rest / blocks};
 }
 
+// (whatever the number of tokens)
 inline size_t block_workspace_bytes(const innerq_block_config_t& c, long long t_new) {
-  const BlockSizes s = block_sizes(c, t_new);
-  size_t bytes = s.split_most == 1 ? 0 : (size_t)(s.heads * s.row_blocks * s.split_most) * block_slot_bytes(s.form.rows);
-  const BlockList l = block_list(c, t_new);
-  if (l.use) {
+  const long long heads = (long long)c.batch * c.n_kv_heads, rows = t_new * (c.n_q_heads / c.n_kv_heads);
+  size_t bytes = 0;
+  for (const BlockKind& k : kBlockKinds) {
+    const long long row_blocks = ceil_div(rows, k.form.rows), most = block_split_most(k.form, heads, row_blocks);
+    if (!block_suits(k.form, rows) || most == 1) continue;
+    const size_t slots = (size_t)(heads * row_blocks * most) * block_slot_bytes(k.form.rows);
+    bytes = slots > bytes ? slots : bytes;
+  }
+  for (const bool all_few : {false, true}) {
+    const BlockList l = block_list_of(c, t_new, all_few);
+    if (!l.use) continue;
     // (work-groups beyond the round that was aimed at have no partial results: their sequences are not split)
-    const size_t list = block_round(l.form) * block_slot_bytes(l.form.rows) + (l.many ? block_round(kBlockListMany) * block_slot_bytes(kBlockListMany.rows) : 0);
+    const size_t list = block_round(l.form) * block_slot_bytes(l.form.rows) + (l.many ? block_round(kBlockMany.form) * block_slot_bytes(kBlockMany.form.rows) : 0);
     bytes = list > bytes ? list : bytes;
   }
   return kBlockTableBytes + bytes;

@@ -148,14 +148,15 @@ int main() {
     c.batch = b; c.n_kv_heads = h; c.n_q_heads = h * r; c.head_dim = 128; c.capacity_tokens = cap; c.block = 32;
     const long long room = (long long)block_workspace_bytes(c, t) - kBlockTableBytes;
     for (long long n = 0; n <= cap; n = n * 5 / 3 + 1) {
-      const BlockSizes s = block_sizes(c, t);
-      const long long splits = block_splits(s, n), slots = s.heads * s.row_blocks * splits;
+      const BlockPlan p = block_plan(c, t, n, n % 3 ? 0.f : 0.5f * t);
+      const long long rows = t * r, slots = (long long)b * h * p.row_blocks * p.n_splits;
       const char* why = nullptr;
-      if (splits < 1 || splits > s.split_most) why = "splits";
-      if (splits > 1 && slots * (long long)block_slot_bytes(s.form.rows) > room) why = "workspace";
-      if (s.row_blocks * s.form.rows < s.rows) why = "rows left out";
+      if (p.n_splits < 1 || p.n_splits > block_split_most(p.form, (long long)b * h, p.row_blocks) || !(p.us > 0.f)) why = "splits";
+      if (p.n_splits > 1 && (slots * (long long)block_slot_bytes(p.form.rows) > room || p.n_splits > (n + kBlockTile - 1) / kBlockTile)) why = "workspace";
+      if (p.row_blocks * p.form.rows < rows || (p.row_blocks - 1) * p.form.rows >= rows || !block_suits(p.form, rows)) why = "rows";
+      if ((p.form.rows > kBlockFewRows ? 32 * p.form.waves != p.form.rows : p.form.waves != 4)) why = "a form that there is no kernel of";
       ++plans;
-      split += splits > 1;
+      split += p.n_splits > 1;
       if (why && ++bad <= 10) printf("%s: batch %d heads %d r %d chunk %lld capacity %lld cached %lld\n", why, b, h, r, t, cap, n);
     }
   }
