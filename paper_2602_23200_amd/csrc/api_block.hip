@@ -131,14 +131,14 @@ int attention(const innerq_block_config_t& c, const innerq_block_cache_t& k, con
   const BlockList list = n_dev ? block_list(c, t_new, tokens) : BlockList{};
   if (list.use) {
     a.table = static_cast<int*>(workspace);
-    a.few_slots = a.slots = block_round(list.form);
+    a.few_slots = a.slots = block_list_items(list.form);
     a.few_rows = list.form.rows;
     a.few_most = list.few_most;
     a.list_few = (int)list.few;
     a.list_many = (int)list.many;
     if (list.many) {
       a.ws = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ws) + (size_t)a.few_slots * block_slot_bytes(list.form.rows));
-      a.slots = block_round(kBlockMany.form);
+      a.slots = block_list_items(kBlockMany.form);
     }
     hipError_t e = list.many ? launch_block_list(a, e4m3, stream) : launch(list.form);
     if (e == hipSuccess) e = launch_block_merge(a, kBlockMany.form, stream);

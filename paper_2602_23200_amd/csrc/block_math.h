@@ -128,7 +128,7 @@ __device__ __forceinline__ int wave_sum(int x) {
 template <int ROWS, int WAVES>
 __device__ __forceinline__ bool find_work(const BlockAttnArgs& a, int from, int to, int group, BlockWork& w) {
   constexpr int N = kBlockListMost / 64;
-  constexpr int ITEMS = block_round(BlockForm{ROWS, WAVES});
+  constexpr int ITEMS = block_list_items(BlockForm{ROWS, WAVES});
   const int lane = (int)threadIdx.x & 63;
   int units[N], tiles[N];                                // of the lane's sequences
   int most = 1;

@@ -93,12 +93,15 @@ inline BlockPlan block_plan(const innerq_block_config_t& c, long long t_new, lon
 inline size_t block_slot_bytes(int group_rows) { return (size_t)group_rows * (kHeadDim + 2) * sizeof(float); }
 
 // A ragged batch of up to kBlockListMost sequences: work-groups find their work in two lists made from the counts, of the sequences of few rows and of
-// those of more, each aimed at one round of work-groups.  With both they are one launch, the work-groups of many rows first: those of few rows find room
+// those of more, each aimed at a number of work-groups.  With both they are one launch, the work-groups of many rows first: those of few rows find room
 // beside them and wait for memory while they compute (two launches and this one: 16 sequences of 1 to 256 new tokens over 1 to 16k 182 us, 167; 8 of 1 to
 // 40 over 1 to 4000 41.4, 32.2; 64 of 1 to 512 566, 551).  Sequences of few rows alone that fill half a round as they are have no list: it costs 4 us
 // in front of the first load, and a launch behind.  The second list's work-groups have 128 rows, not 256, and the first one's up to 32, not 64 (the
 // first of these cases, in two launches: 199 and 215 us; 187 and 199).
 constexpr int kBlockListMost = 256;
+// Ranges that a list aims at.  (As many as the chip holds, 768, 512 and 512: 8 sequences of 1 to 32k tokens, one new one 46.8 us, with these 43.8; of 1 to
+// 8000 22.7 and 21.2, 1 to 5 new ones 24.0 and 21.4; cross attention of 16 x 16 heads over 1 to 1437 17.7 and 18.7.)
+constexpr int block_list_items(const BlockForm& f) { return f.rows == 32 ? 256 : 512; }
 constexpr int kBlockTableBytes = 2 * kBlockListMost * (int)sizeof(int);   // first slot and splits of every sequence, at the workspace's start
 struct BlockList {
   bool use;
@@ -112,8 +115,8 @@ inline BlockList block_list_of(const innerq_block_config_t& c, long long t_new, 
   l.form = rows <= 16 ? kBlockKinds[0].form : kBlockFew.form;
   l.few_most = (int)(all_few || rows <= l.form.rows ? rows : l.form.rows);
   const long long few = heads * ceil_div(l.few_most, l.form.rows), many = heads * ceil_div(rows, kBlockMany.form.rows);
-  l.few = (few > block_round(l.form) ? few : block_round(l.form)) + 7 & ~7LL;
-  l.many = rows <= l.few_most ? 0 : (many > block_round(kBlockMany.form) ? many : block_round(kBlockMany.form)) + 7 & ~7LL;
+  l.few = (few > block_list_items(l.form) ? few : block_list_items(l.form)) + 7 & ~7LL;
+  l.many = rows <= l.few_most ? 0 : (many > block_list_items(kBlockMany.form) ? many : block_list_items(kBlockMany.form)) + 7 & ~7LL;
   l.use = c.batch <= kBlockListMost && (rows > l.form.rows || 2 * few <= block_round(l.form));
   return l;
 }
@@ -168,8 +171,8 @@ inline size_t block_workspace_bytes(const innerq_block_config_t& c, long long t_
   for (const bool all_few : {false, true}) {
     const BlockList l = block_list_of(c, t_new, all_few);
     if (!l.use) continue;
-    // (work-groups beyond the round that was aimed at have no partial results: their sequences are not split)
-    const size_t list = block_round(l.form) * block_slot_bytes(l.form.rows) + (l.many ? block_round(kBlockMany.form) * block_slot_bytes(kBlockMany.form.rows) : 0);
+    // (work-groups beyond the number that was aimed at have no partial results: their sequences are not split)
+    const size_t list = block_list_items(l.form) * block_slot_bytes(l.form.rows) + (l.many ? block_list_items(kBlockMany.form) * block_slot_bytes(kBlockMany.form.rows) : 0);
     bytes = list > bytes ? list : bytes;
   }
   return kBlockTableBytes + bytes;

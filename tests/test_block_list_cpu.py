@@ -26,7 +26,7 @@ static void fail(const char* why, int batch, int heads, int r, int t) {
 // One list: rows above `from` and up to `to`.
 static void walk(const std::vector<int>& n, const std::vector<int>& t, bool causal, int heads, int r, int most_new, int from, int to, const BlockForm& f, long long groups,
                  float nudge) {
-  const int batch = (int)n.size(), round = block_round(f);
+  const int batch = (int)n.size(), round = block_list_items(f);
   if (groups % 8) fail("not a multiple of eight", batch, heads, r, most_new);
   std::vector<BlockShare> share(batch);
   int longest = 1;
@@ -107,8 +107,8 @@ int main() {
     const BlockList list = block_list(c, most_new, bound);
     if (!list.use) continue;
     ++used;
-    if (kBlockTableBytes + block_round(list.form) * block_slot_bytes(list.form.rows) +
-            (list.many ? block_round(kBlockMany.form) * block_slot_bytes(kBlockMany.form.rows) : 0) > bytes) fail("workspace of a list", batch, heads, r, most_new);
+    if (kBlockTableBytes + block_list_items(list.form) * block_slot_bytes(list.form.rows) +
+            (list.many ? block_list_items(kBlockMany.form) * block_slot_bytes(kBlockMany.form.rows) : 0) > bytes) fail("workspace of a list", batch, heads, r, most_new);
     std::vector<int> n(batch), t(batch);
     for (int b = 0; b < batch; ++b) {
       n[b] = rng() % 4 == 0 ? 0 : draw(1, most_cached + 1);
@@ -124,7 +124,7 @@ int main() {
   }
   // as much work as 31 bits of rows have over as many tokens as a call may name: lengths and ranges stay within 31 bits
   for (float work = 1.0f; work < 1e14f; work *= 1.7f)
-    for (const int round : {256, 512, 768}) {
+    for (const int round : {256, 512}) {
       const int length = block_first_length(work, round);
       if (length < kBlockListLeast || (length < work / round - 1 && length < 1 << 20)) fail("first length", 0, 0, 0, 0);
       for (const int tiles : {1, 1000, 1 << 19})
