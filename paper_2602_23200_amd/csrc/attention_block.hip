@@ -33,10 +33,11 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(NR 
   attend<E4M3, NR>(a, work, lds, a.ws, a.slots);
 }
 
-// The splits of a row joined: half a wavefront a row, a lane four channels, eight splits under way (where there are fewer the last one is read again:
-// a form with four under way was as fast where rows are many and 1 us slower at the smallest calls).  The launch is bounded, and its
-// work-groups walk over the rows: of a padded batch most rows are not there, and starting work-groups for them cost more than the joining (16
-// sequences of 1 to 256 new tokens 183 us with a work-group for every eight rows, 177 with 4096 at most, 174 with 2048).
+// The splits of a row joined: half a wavefront a row, a lane four channels, eight splits under way (only those that are there: with the last one read again in
+// place of the others, of a ragged batch with one to four, 15 us, now 11).  The launch is bounded, and its work-groups walk over the rows: of a padded
+// batch most rows are not there, and starting work-groups for them cost more than the joining (16 sequences of 1 to 256 new tokens 183 us with a
+// work-group for every eight rows, 177 with 4096 at most, 174 with 2048).  What bounds it is memory: three partial results of 9600 rows x 4 sequences
+// (60 MB) 15 us; of few rows the launch (4 us).
 constexpr int kMergeRows = 8;                            // of a work-group at once
 constexpr int kMergeGroups = 2048;                       // of a launch where rows are many
 __global__ void __launch_bounds__(256) block_merge_kernel(BlockAttnArgs a, int blocks, int group_rows) {
@@ -49,7 +50,7 @@ __global__ void __launch_bounds__(256) block_merge_kernel(BlockAttnArgs a, int b
   long long slots = a.slots, slot;                       // the first one's of the first rows
   int row_step;                                          // .. and from one block of rows to the next
   if (a.table) {
-    n_splits = a.table[2 * b + 1];
+    n_splits = __builtin_amdgcn_readfirstlane(a.table[2 * b + 1]);
     if (n_splits == 1) return;                           // (written already)
     if (own <= a.few_most) {
       group_rows = a.few_rows;
@@ -74,9 +75,12 @@ __global__ void __launch_bounds__(256) block_merge_kernel(BlockAttnArgs a, int b
       float4_t v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int p = p0 + e < n_splits ? p0 + e : n_splits - 1;
-        st[e] = *reinterpret_cast<const float2*>(ml + p * step_ml);
-        v[e] = *reinterpret_cast<const float4_t*>(po + p * step_o);
+        st[e] = float2{-INFINITY, 0.f};
+        v[e] = float4_t{};
+        if (p0 + e < n_splits) {                         // (uniform)
+          st[e] = *reinterpret_cast<const float2*>(ml + (p0 + e) * step_ml);
+          v[e] = *reinterpret_cast<const float4_t*>(po + (p0 + e) * step_o);
+        }
       }
       float top = level;
 #pragma unroll
@@ -87,7 +91,7 @@ __global__ void __launch_bounds__(256) block_merge_kernel(BlockAttnArgs a, int b
       level = top;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float f = p0 + e >= n_splits || st[e].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[e].x - top);
+        const float f = st[e].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[e].x - top);
         den = __builtin_fmaf(f, st[e].y, den);
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(f, v[e][i], o[i]);
