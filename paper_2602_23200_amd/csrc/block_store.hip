@@ -1,7 +1,10 @@
 // Writing the cache in 8 bits with block scales, and reading it back.
 //
 // Both are copies that change width: a value is read once and written once (2 + 1 bytes), and what bounds them is memory; for a single token it is
-// the launch.  A wavefront takes a block of one head by itself (32 x 128 values: 64 a lane, in registers), so the largest magnitude
+// the launch.  Writing 4 x 8 heads x 32k tokens, 806 MB: 143 us, 5.6 TB/s (a copy of as many bytes 163); reading them back 146, and 119 where the codes stay
+// in the last-level cache; ragged prompts of 16 x 8 heads, 46 MB, 17; a token of 32 x 8 heads 7.5, the newest 257 tokens of 8 x 8 heads 5.2.
+//
+// A wavefront takes a block of one head by itself (32 x 128 values: 64 a lane, in registers), so the largest magnitude
 // is a reduction over its lanes and no barrier stands in the way.  Keys: a lane has sixteen channels of a token, sixteen bytes of the
 // store.  Values: a lane has two channels of eight tokens, the sixteen bytes that a lane of the attention kernel takes as one operand of
 // either channel, so the transposition is made of whole registers.
