@@ -68,12 +68,26 @@ __device__ __forceinline__ void put_codes(char* dst, int apart, const u32x4& w, 
   *reinterpret_cast<half8_t*>(dst + apart) = expand_by<E4M3>(w.z, w.w, by);
 }
 
-// fp16 rows.  Keys: a thread has 32 / WAVES octets of a token ..; values: four tokens of 8 / WAVES pairs of channels.
+// fp16 rows.  Keys: a thread has 64 / WAVES channels of a token, pairs of lanes next to each other and 32 / WAVES tokens of a wavefront in turn (a token's
+// channels in a row of lanes would all go to the same banks); values: four tokens of 8 / WAVES pairs of channels, with eight wavefronts the same
+// four for a wavefront, so that where the rows are is worked out once for all lanes.  (First prompt of 16384 tokens of 32 heads: 2770 us with neither, 2540
+// with the first, 2440 with both.)
+template <int WAVES>
+struct PlainPart {
+  static constexpr int N = 8 / WAVES, T = 4 * N;         // octets of a thread, tokens of a wavefront
+  int token, octet;
+  __device__ __forceinline__ explicit PlainPart(int tid) {
+    const int l = tid & 63;
+    token = (tid >> 6) * T + l / 2 % T;
+    octet = ((l & 1) | l / (2 * T) << 1) * N;
+  }
+};
 template <int WAVES>
 __device__ __forceinline__ void put_plain(char* buf, int tid, const Staged& x) {
-  constexpr int N = 8 / WAVES, PER = 16 / N;             // octets of a thread, threads of a token
+  constexpr int N = PlainPart<WAVES>::N;
   {
-    char* dst = buf + tid % PER * N * 512 + row_of(tid / PER) * 16;
+    const PlainPart<WAVES> part(tid);
+    char* dst = buf + part.octet * 512 + row_of(part.token) * 16;
     *reinterpret_cast<u32x4*>(dst) = x.a;
     if (N == 2) *reinterpret_cast<u32x4*>(dst + 512) = x.b;
   }
@@ -122,7 +136,7 @@ __device__ __forceinline__ void two_weights(int e, const float16_t& s, float by,
 
 // Units u0 .. u1 of one kind.  fetch(u, regs, scales): a unit's bytes into registers, and its scales; put(buffer, regs, scales): into LDS; mask(u,
 // scores): scores of tokens that a row does not attend to are -infinity.
-template <bool MASKED, typename Fetch, typename Put, typename Mask>
+template <typename Fetch, typename Put, typename Mask>
 __device__ __forceinline__ void walk(int u0, int u1, char* lds, State& r, int lane, Fetch fetch, Put put, Mask mask) {
   if (u0 >= u1) return;
   auto at = [&](int u) { return lds + ((u - u0) % kUnits) * kUnitBytes; };
@@ -151,7 +165,7 @@ __device__ __forceinline__ void walk(int u0, int u1, char* lds, State& r, int la
 #pragma unroll
   for (int e = 0; e < 8; ++e) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[e], r.q[e], s, 0, 0, 0);
   keys(u0 + 1);
-  if (MASKED) mask(u0, s);
+  mask(u0, s);
   top = unit_top(s, now);
   // s: scores of unit u; k: keys of unit u + 1; x: unit u + 3
   auto step = [&](int u, float16_t& s, float16_t& t, Staged& x, Scales& sx) {
@@ -181,13 +195,14 @@ __device__ __forceinline__ void walk(int u0, int u1, char* lds, State& r, int la
       __builtin_amdgcn_sched_barrier(0);
     }
     r.l = __builtin_fmaf(sum, now.inv, r.l);
+    mask(bound(u + 1), t);
     // the second product; the keys after the next, a unit into LDS, the largest of the next scores
     keys(u + 2);
     put(at(u + 3), x, sx);
     now = next;
     next = third;
     third = sx;
-    if (!MASKED) top = unit_top(t, now);
+    top = unit_top(t, now);
 #pragma unroll
     for (int e = 0; e < 8; ++e) r.o[e % 4] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[e], p[e / 4], r.o[e % 4], 0, 0, 0);
 #pragma unroll
@@ -195,10 +210,6 @@ __device__ __forceinline__ void walk(int u0, int u1, char* lds, State& r, int la
       __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
       __builtin_amdgcn_sched_group_barrier(0x2, 12, 0);
-    }
-    if (MASKED) {
-      mask(bound(u + 1), t);
-      top = unit_top(t, now);
     }
     fetch(bound(u + 5), x, sx);
     __syncthreads();
@@ -259,7 +270,7 @@ __device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& 
       put_codes<E4M3>(buf + to, apart, x.a, keys ? 1.f : sc.shrink);
       if (WAVES == 4) put_codes<E4M3>(buf + put_at(false, wave, lane), 256, x.b, sc.shrink);
     };
-    walk<false>(t0, u1, lds, r, lane, fetch, put, [](int, float16_t&) {});
+    walk(t0, u1, lds, r, lane, fetch, put, [](int, float16_t&) {});
   }
   if (t1 > tiles1) {
     const long long open_at = bh * a.s.block * D;
@@ -276,14 +287,15 @@ __device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& 
       sc = Scales{kScoreScale, 0.f, 1.f, 1.f};
       const int i0 = u * kBlockTile;
       auto token = [&](int i) { return i0 + i < plain ? i0 + i : plain - 1; };   // (behind the last one: that one again, masked)
-      constexpr int N = 8 / WAVES, PER = 16 / N, PAIRS = 64 / N;                 // (as put_plain)
-      const __half* k = row_at(ko, kf, a.k.token, token(tid / PER)) + tid % PER * 8 * N;
+      constexpr int N = PlainPart<WAVES>::N, PAIRS = 64 / N;                     // (as put_plain)
+      const PlainPart<WAVES> part(tid);
+      const __half* k = row_at(ko, kf, a.k.token, token(part.token)) + part.octet * 8;
       x.a = *reinterpret_cast<const u32x4*>(k);
       if (N == 2) x.b = *reinterpret_cast<const u32x4*>(k + 8);
       u32x2 w[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const __half* v = row_at(vo, vf, a.v.token, token(4 * (tid / PAIRS) + e)) + tid % PAIRS * 2 * N;
+        const __half* v = row_at(vo, vf, a.v.token, token(4 * (WAVES == 8 ? wave : tid / PAIRS) + e)) + tid % PAIRS * 2 * N;
         if (N == 2) w[e] = *reinterpret_cast<const u32x2*>(v);
         else w[e] = u32x2{*reinterpret_cast<const uint32_t*>(v), 0u};
       }
@@ -299,7 +311,7 @@ __device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& 
       for (int i = 0; i < 16; ++i)
         if (token_of(i, half) > left) sc[i] = -INFINITY;
     };
-    walk<true>(t0 > tiles1 ? t0 - tiles1 : 0, t1 - tiles1, lds, r, lane, fetch, [&](char* buf, const Staged& x, const Scales&) { put_plain<WAVES>(buf, tid, x); },
+    walk(t0 > tiles1 ? t0 - tiles1 : 0, t1 - tiles1, lds, r, lane, fetch, [&](char* buf, const Staged& x, const Scales&) { put_plain<WAVES>(buf, tid, x); },
                mask);
   }
 
