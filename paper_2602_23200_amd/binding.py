@@ -8,6 +8,7 @@ not built, importing it here fails.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from dataclasses import dataclass
 from typing import Optional
@@ -636,6 +637,12 @@ def _checked(st: int, where: str) -> None:
 _byref = C.byref
 
 
+@functools.lru_cache(maxsize=256)
+def _strides(batch: int, head: int, token: int):
+    """A read-only innerq_strides_t of these values, by reference (making one takes longer than finding it)."""
+    return _byref(innerq_strides_t(batch, head, token))
+
+
 def _block_rows(t, batch: int, heads: int, tokens: int, dim: int, dtype=None):
     """_rows for the calls below (a third of the host's time in a call on short sequences went into it)."""
     if dtype is None:
@@ -643,7 +650,7 @@ def _block_rows(t, batch: int, heads: int, tokens: int, dim: int, dtype=None):
         dtype = torch.float16
     b, h, n, one = t.stride()
     assert t.is_cuda and t.dtype is dtype and t.shape == (batch, heads, tokens, dim) and one == 1
-    return t.data_ptr(), _byref(innerq_strides_t(b if batch > 1 else 0, h if heads > 1 else 0, n if tokens > 1 else 0))
+    return t.data_ptr(), _strides(b if batch > 1 else 0, h if heads > 1 else 0, n if tokens > 1 else 0)
 
 
 def _block_stream(stream, t) -> Optional[int]:
