@@ -25,18 +25,18 @@ constexpr int kBlockFewRows = 64;
 // Work-groups of that form that the chip holds at once.
 constexpr int block_round(const BlockForm& f) { return 256 * (f.rows == 16 ? 3 : f.rows == 32 || f.rows == 128 ? 2 : 1); }
 
-// What a form costs, us: before the first tile, for every tile that a wavefront (many rows: the work-group) takes one after the other, with a CU of its own
-// and in more than 256 work-groups; where the keys are split, for the second launch and for so many rows of partial results.  The constants are fitted to
-// 16700 timings of calls with 4 to 2048 rows of each of 1 to 1024 sequence-heads over 0 to 32k tokens, every form and number of ranges; of these
-// the one that is chosen takes 1.1 % longer than the fastest one in the mean, 27 % at worst.  (By the number of rows alone, with as many ranges as fill
-// the chip, calls of 17 rows and more took 25 % longer in the mean, three times as long at worst: 300 rows of 8 heads over 300 tokens 26 us, now 12;
-// 128 over 1682 29, now 13.)
-struct BlockKind { BlockForm form; float setup, tile, crowded, join, partial; };
-constexpr BlockKind kBlockKinds[] = {{{16, 4}, 5.0f, 0.62f, 1.4f, 3.0f, 4200.f},
-                                     {{32, 4}, 6.4f, 0.86f, 1.8f, 3.0f, 4200.f},
-                                     {{64, 4}, 8.3f, 1.2f, 1.2f, 3.0f, 6300.f},
-                                     {{128, 4}, 9.2f, 0.69f, 1.0f, 3.5f, 8400.f},
-                                     {{256, 8}, 9.3f, 0.89f, 0.89f, 4.4f, 8400.f}};
+// What a form costs, us: before the first tile of the first work-groups and of later ones; for every tile that a wavefront (many rows: the work-group) takes
+// one after the other, with a CU of its own and in more than 256 work-groups; where the keys are split, for the second launch and for so many rows of
+// partial results.  The constants are fitted to 16700 timings of calls with 4 to 2048 rows of each of 1 to 1024 sequence-heads over 0 to 32k tokens, every
+// form and number of ranges; of these the one that is chosen takes 0.9 % longer than the fastest one in the mean, 27 % at worst.  (By the number of rows
+// alone, with as many ranges as fill the chip, calls of 17 rows and more took 25 % longer in the mean, three times as long at worst: 300 rows of 8 heads
+// over 300 tokens 26 us, now 12; 128 over 1682 29, now 13.)
+struct BlockKind { BlockForm form; float setup, again, tile, crowded, join, partial; };
+constexpr BlockKind kBlockKinds[] = {{{16, 4}, 5.0f, 3.0f, 0.62f, 1.4f, 3.0f, 4200.f},
+                                     {{32, 4}, 6.4f, 5.0f, 0.86f, 1.8f, 3.0f, 4200.f},
+                                     {{64, 4}, 8.3f, 6.5f, 1.2f, 1.2f, 3.0f, 6300.f},
+                                     {{128, 4}, 9.2f, 3.0f, 0.69f, 1.0f, 3.5f, 8400.f},
+                                     {{256, 8}, 9.3f, 7.0f, 0.89f, 0.89f, 4.4f, 8400.f}};
 constexpr BlockKind kBlockFew = kBlockKinds[1], kBlockMany = kBlockKinds[3];     // of a list
 // Bytes of the cache a us.  (Up to 224 work-groups no CU has two while another has none.  8 sequences of 8 heads over 32k tokens, one token: in 3 ranges 84 us,
 // 4 93, 6 90, 8 93, 12 91; 5 tokens: 93, 96, 97, 98.)
@@ -51,7 +51,8 @@ inline float block_cost(const BlockKind& k, long long heads, long long row_block
   const float share = units / ways, tile = groups <= 256.f ? k.tile : k.crowded, rounds = groups / (float)block_round(k.form);
   float us = k.setup + 0.5f * (std::ceil(share) + (share < 1.f ? 1.f : share)) * tile;
   if (rounds > 1.f) {
-    const float mean = average / ways, all = (rounds <= 3.f ? std::ceil(rounds) : rounds + 0.5f) * (k.setup + (mean < 0.5f ? 0.5f : mean) * tile);
+    const float mean = average / ways, r = rounds <= 3.f ? std::ceil(rounds) : rounds + 0.5f;
+    const float all = k.setup + (r - 1.f) * k.again + r * (mean < 0.5f ? 0.5f : mean) * tile;
     us = all > us ? all : us;
   }
   const float bytes = (float)heads * units * (2 * kBlockTileBytes) / block_rate(groups);
