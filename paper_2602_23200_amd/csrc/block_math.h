@@ -123,8 +123,7 @@ __device__ __forceinline__ int wave_sum(int x) {
   return x;
 }
 // A ragged batch: work-groups find their work from the counts of all sequences (four a lane; the arithmetic is the plan's), every wavefront
-// the same: of the sequences with rows above `from` and up to `to`, those of work-group `group`.  Neighbours in the list, which share keys, go to one
-// XCD.
+// the same: of the sequences with rows above `from` and up to `to`, those of work-group `group`.
 template <int ROWS, int WAVES>
 __device__ __forceinline__ bool find_work(const BlockAttnArgs& a, int from, int to, int group, BlockWork& w) {
   constexpr int N = kBlockListMost / 64;
@@ -163,32 +162,35 @@ __device__ __forceinline__ bool find_work(const BlockAttnArgs& a, int from, int 
     if (block_length_fits(length, most, ranges, ITEMS)) break;
     length = __builtin_amdgcn_readfirstlane(block_next_length(length, ranges, ITEMS));
   }
-  // this work-group's item (the launch has a multiple of eight work-groups), and the sequence whose items hold it
-  const int per = (ranges + 7) / 8, item = group % 8 * per + group / 8;
-  if (group / 8 >= per) return false;          // (uniform)
+  // this work-group's place in the line, and the sequence that it belongs to
+  const bool by_head = block_by_head(a.s.n_kv_heads);
+  const int place = block_turn(group, ranges, by_head), scale = by_head ? 8 : 1;
+  if (place < 0) return false;                           // (uniform)
+  if (by_head) mine /= 8;
   int before = mine;
 #pragma unroll
   for (int i = 1; i < 64; i *= 2) {
     const int x = __shfl_up(before, i);
     if (lane >= i) before += x;
   }
-  const unsigned long long reach = __builtin_amdgcn_ballot_w64(before > item);
+  const unsigned long long reach = __builtin_amdgcn_ballot_w64(before > place);
   if (reach == 0) return false;                          // (uniform)
   const int owner = __builtin_ctzll(reach);
   int first = __builtin_amdgcn_readlane(before - mine, owner);
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    const int u = __builtin_amdgcn_readlane(units[j], owner), splits = block_ranges(__builtin_amdgcn_readlane(tiles[j], owner), length), all = u * splits;
-    if (item >= first && item < first + all) {
-      const BlockPlace at = block_place(item - first, u, a.s.n_kv_heads, splits);
+    const int u = __builtin_amdgcn_readlane(units[j], owner), splits = block_ranges(__builtin_amdgcn_readlane(tiles[j], owner), length), all = u * splits / scale;
+    if (place >= first && place < first + all) {
+      const int range = block_range(place - first, group, u, a.s.n_kv_heads, splits, by_head);
+      const BlockPlace at = block_place(range, u, a.s.n_kv_heads, splits);
       w.b = N * owner + j;
       w.h = at.h;
       w.row_block = at.row_block;
       w.split = at.split;
       w.n_splits = splits;
-      w.slot = item;
-      if (item == first && threadIdx.x == 0) {
-        a.table[2 * w.b] = item;
+      w.slot = first * scale + range;
+      if (range == 0 && threadIdx.x == 0) {
+        a.table[2 * w.b] = first * scale;
         a.table[2 * w.b + 1] = splits;
       }
       return true;

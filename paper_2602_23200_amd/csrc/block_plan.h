@@ -96,7 +96,7 @@ inline size_t block_slot_bytes(int group_rows) { return (size_t)group_rows * (kH
 // A ragged batch of up to kBlockListMost sequences: work-groups find their work in two lists made from the counts, of the sequences of few rows and of
 // those of more, each aimed at a number of work-groups.  With both they are one launch, the work-groups of many rows first: those of few rows find room
 // beside them and wait for memory while they compute (two launches and this one: 16 sequences of 1 to 256 new tokens over 1 to 16k 182 us, 167; 8 of 1 to
-// 40 over 1 to 4000 41.4, 32.2; 64 of 1 to 512 566, 551).  Sequences of few rows alone that fill half a round as they are have no list: it costs 4 us
+// 40 over 1 to 4000 41.4, 32.2).  Sequences of few rows alone that fill half a round as they are have no list: it costs 4 us
 // in front of the first load, and a launch behind.  The second list's work-groups have 128 rows, not 256, and the first one's up to 32, not 64 (the
 // first of these cases, in two launches: 199 and 215 us; 187 and 199).
 constexpr int kBlockListMost = 256;
@@ -152,6 +152,21 @@ constexpr int block_next_length(int length, int ranges, int items) {
 }
 constexpr int block_ranges(int tiles, int length) { return (tiles + length - 1) / length; }
 constexpr bool block_length_fits(int length, int longest, int ranges, int items) { return length >= longest || ranges <= items; }
+// Which range a work-group takes.  Work-groups go to the eight dies in turn.  Where heads are a multiple of eight a die has an eighth of the heads, of every
+// sequence: a head's keys are read by one die, and sequences of any lengths are shared out evenly.  Otherwise a die has an eighth of the line.  (An eighth
+// of the line for each die, and this: 8 prompts of 16 to 2000 tokens 152 us, 97; 64 sequences of 1 to 512 new tokens over 250 to 4000 555, 313; the 16
+// above 157, 153.)  The last rows, which have the most keys, go first.
+constexpr bool block_by_head(int n_kv_heads) { return n_kv_heads % 8 == 0; }
+// Its place in the line (by head: in its die's line, an eighth of every sequence's ranges; none: -1).
+constexpr int block_turn(int group, int ranges, bool by_head) {
+  const int per = (ranges + 7) / 8, turn = group / 8, place = by_head ? turn : group % 8 * per + turn;
+  return turn < per && (by_head || place < ranges) ? place : -1;
+}
+// The number of the range within its sequence, from its place there.
+constexpr int block_range(int place, int group, int units, int n_kv_heads, int splits, bool by_head) {
+  const int blocks = units / n_kv_heads, each = blocks * splits, h = by_head ? place / each * 8 + group % 8 : place / each, rest = place % each;
+  return h * each + rest / blocks * blocks + blocks - 1 - rest % blocks;
+}
 // Range number `at` of a sequence: row blocks of the same range, which read the same keys, are neighbours.
 struct BlockPlace { int h, row_block, split; };
 constexpr BlockPlace block_place(int at, int units, int n_kv_heads, int splits) {

@@ -54,16 +54,28 @@ static void walk(const std::vector<int>& n, const std::vector<int>& t, bool caus
   ++lists;
   lengthened += turns > 0;
   if (items > groups) fail("more items than work-groups", batch, heads, r, most_new);
-  // (the work-groups of eight dies have an eighth of the items each)
-  const long long per = (items + 7) / 8;
+  // every work-group's range, as it finds it
+  const bool by_head = block_by_head(heads);
+  const int scale = by_head ? 8 : 1;
   std::vector<char> taken(items, 0);
   for (long long x = 0; x < groups; ++x) {
-    const long long item = x % 8 * per + x / 8;
-    if (x / 8 >= per || item >= items) continue;
-    if (taken[item]) fail("an item twice", batch, heads, r, most_new);
-    taken[item] = 1;
+    const int place = block_turn((int)x, (int)items, by_head);
+    if (place < 0) continue;
+    long long first = 0;
+    for (int b = 0; b < batch; ++b) {
+      const int splits = block_ranges(share[b].tiles, length), all = share[b].units * splits / scale;
+      if (place >= first && place < first + all) {
+        const int range = block_range((int)(place - first), (int)x, share[b].units, heads, splits, by_head);
+        if (range < 0 || range >= share[b].units * splits) { fail("a range that is none", batch, heads, r, most_new); break; }
+        char& mark = taken[first * scale + range];
+        if (mark) fail("a range twice", batch, heads, r, most_new);
+        mark = 1;
+        break;
+      }
+      first += all;
+    }
   }
-  for (const char x : taken) if (!x) fail("an item of no work-group", batch, heads, r, most_new);
+  for (const char x : taken) if (!x) { fail("a range of no work-group", batch, heads, r, most_new); break; }
   bool cut = false, whole = false;
   long long first = 0;
   std::vector<char> seen;
@@ -96,7 +108,7 @@ int main() {
   auto draw = [&](double lo, double hi) { return (int)std::exp(std::uniform_real_distribution<double>(std::log(lo), std::log(hi))(rng)); };
   const int some_heads[] = {1, 2, 3, 8, 8, 16, 32, 64}, some_r[] = {1, 2, 4, 4, 7, 8, 16};
   long long used = 0, wide = 0;
-  for (int turn = 0; turn < 6000; ++turn) {
+  for (int turn = 0; turn < 2500; ++turn) {
     const int batch = draw(1, 300), heads = some_heads[rng() % 8], r = some_r[rng() % 7], most_new = draw(1, 5000), most_cached = draw(1, 1 << (10 + rng() % 15));
     const bool causal = rng() % 2;
     innerq_block_config_t c = {};
@@ -132,7 +144,7 @@ int main() {
     }
   printf("%lld calls with a list, %lld of them of blocks of few rows alone, %lld lists, %lld lengthened, %lld of more items than aimed at, %lld cut in part, %lld bad\n", used, wide, lists, lengthened,
          uncut, mixed, bad);
-  return bad || used < 2000 || wide < 200 || lengthened < 500 || uncut < 300 || mixed < 500;
+  return bad || used < 800 || wide < 80 || lengthened < 200 || uncut < 120 || mixed < 200;
 }
 """
 
