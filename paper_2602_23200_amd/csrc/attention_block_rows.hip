@@ -63,9 +63,9 @@ __device__ __forceinline__ int put_at(bool keys, int part, int lane) {
   return kUnitValues + part * 2048 + (g >> 1) * 1024 + (g & 1) * 512 + c * 16;
 }
 template <bool E4M3>
-__device__ __forceinline__ void put_codes(char* dst, int apart, const u32x4& w, float by) {
-  *reinterpret_cast<half8_t*>(dst) = expand_by<E4M3>(w.x, w.y, by);
-  *reinterpret_cast<half8_t*>(dst + apart) = expand_by<E4M3>(w.z, w.w, by);
+__device__ __forceinline__ void put_codes(char* dst, int apart, const u32x4& w, const Codes& by) {
+  *reinterpret_cast<half8_t*>(dst) = expand<E4M3>(w.x, w.y, by);
+  *reinterpret_cast<half8_t*>(dst + apart) = expand<E4M3>(w.z, w.w, by);
 }
 
 // fp16 rows.  Keys: a thread has 64 / WAVES channels of a token, pairs of lanes next to each other and 32 / WAVES tokens of a wavefront in turn (a token's
@@ -253,7 +253,7 @@ __device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& 
 
   const int u1 = t1 < tiles1 ? t1 : tiles1;
   if (t0 < u1) {
-    BlockUnits units;
+    BlockUnits<E4M3> units;
     // (eight wavefronts: half of them bring keys, half values)
     const bool keys = WAVES == 4 || wave < 4;
     const uint32_t mine_at = (uint32_t)(64 * (wave & 3) + lane) * 16;
@@ -267,8 +267,8 @@ __device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& 
       sc = units.scales(u);
     };
     auto put = [&](char* buf, const Staged& x, const Scales& sc) {
-      put_codes<E4M3>(buf + to, apart, x.a, keys ? 1.f : sc.shrink);
-      if (WAVES == 4) put_codes<E4M3>(buf + put_at(false, wave, lane), 256, x.b, sc.shrink);
+      put_codes<E4M3>(buf + to, apart, x.a, keys ? codes_times<E4M3>(0) : sc.values);
+      if (WAVES == 4) put_codes<E4M3>(buf + put_at(false, wave, lane), 256, x.b, sc.values);
     };
     walk(t0, u1, lds, r, lane, fetch, put, [](int, float16_t&) {});
   }
@@ -284,7 +284,7 @@ __device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& 
       return (waits ? o : f) + at * step;
     };
     auto fetch = [&](int u, Staged& x, Scales& sc) {
-      sc = Scales{kScoreScale, 0.f, 1.f, 1.f};
+      sc = Scales{kScoreScale, 0.f, 1.f, {}};
       const int i0 = u * kBlockTile;
       auto token = [&](int i) { return i0 + i < plain ? i0 + i : plain - 1; };   // (behind the last one: that one again, masked)
       constexpr int N = PlainPart<WAVES>::N, PAIRS = 64 / N;                     // (as put_plain)

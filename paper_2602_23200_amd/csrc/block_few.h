@@ -111,7 +111,7 @@ __device__ __forceinline__ void use_tile(Rows<NR>& r, const Tile& t) {
 #pragma unroll
     for (int st = 0; st < 4; ++st) {
       const u32x4 w = t.k[2 * a + st / 2];
-      const half8_t k = st & 1 ? expand<E4M3>(w.z, w.w) : expand<E4M3>(w.x, w.y);
+      const half8_t k = st & 1 ? expand<E4M3>(w.z, w.w, codes_times<E4M3>(0)) : expand<E4M3>(w.x, w.y, codes_times<E4M3>(0));
 #pragma unroll
       for (int n = 0; n < NR; ++n) s[n][a] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, r.q[n][st], s[n][a], 0, 0, 0);
     }
@@ -122,7 +122,7 @@ __device__ __forceinline__ void use_tile(Rows<NR>& r, const Tile& t) {
   for (int q = 0; q < 4; ++q)
 #pragma unroll
     for (int m = 0; m < 2; ++m)
-      add_values<NR>(r, 2 * q + m, m ? expand_by<E4M3>(t.v[q].z, t.v[q].w, t.scales.shrink) : expand_by<E4M3>(t.v[q].x, t.v[q].y, t.scales.shrink), p);
+      add_values<NR>(r, 2 * q + m, m ? expand<E4M3>(t.v[q].z, t.v[q].w, t.scales.values) : expand<E4M3>(t.v[q].x, t.v[q].y, t.scales.values), p);
 }
 
 // A sequence's fp16 tokens behind the packed ones, in order: the open ones, then the new ones.
@@ -171,7 +171,7 @@ __device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& 
   const int u1 = t1 < tiles1 ? t1 : tiles1;
   if (t0 < u1) {
     // (tiles are loaded two ahead; behind the last one: that one again)
-    BlockUnits units;
+    BlockUnits<E4M3> units;
     auto load = [&](int u, Tile& t) {
       u = u < u1 ? u : u1 - 1;
       units.look(a.s, b, h, u, u1, lane);
@@ -232,7 +232,7 @@ __device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& 
             if (i0 + 16 * x + 4 * g + i > limit) sc[n][x][i] = -INFINITY;
       }
       half8_t w[NR][kPieces<NR>];
-      weights<NR>(r, sc, Scales{kScoreScale, 0.f, 1.f, 1.f}, w);
+      weights<NR>(r, sc, Scales{kScoreScale, 0.f, 1.f, {}}, w);
       const __half* vsrc[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) vsrc[j] = p.value(token(16 * (j >> 2) + 4 * g + (j & 3))) + 2 * c;

@@ -16,29 +16,35 @@ constexpr float kTop = 9.0f, kRaise = 15.0f;
 constexpr float kFar = 0x1p19f;                          // levels beyond: neighbours in fp32 are 2^-4 apart and more
 constexpr float kFarShare = 0x1p-16f;                    // of its own size, by which a level is raised the sooner
 
-// Eight codes as fp16, times a power of two.
+// By which power of two a tensor's codes are multiplied.  E4M3: its bits in fp32; integers: see int_codes.
+struct Codes { uint32_t by, top; };
 template <bool E4M3>
-__device__ __forceinline__ half8_t expand_by(uint32_t a, uint32_t b, float by) {
+__device__ __forceinline__ constexpr Codes codes_times(int x) {
+  if (E4M3) return {(uint32_t)(x + 127) << 23, 0u};
+  const IntCodes c = int_codes(x);
+  return {c.factor_bias, c.top};
+}
+// Eight codes as fp16, times that: exact down to multiples of 2^-24 (integers to 2^-24, E4M3, whose codes reach 2^-9, to 2^-15), rounded to them below.
+template <bool E4M3>
+__device__ __forceinline__ half8_t expand(uint32_t a, uint32_t b, const Codes& c) {
   half2_t h[4];
   if constexpr (E4M3) {
+    const float by = __uint_as_float(c.by);
     h[0] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, by, false));
     h[1] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, by, true));
     h[2] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, by, false));
     h[3] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, by, true));
   } else {
-    // (1024 + 128 + code under the exponent of 1024; exact for every power of two up to 1)
-    const half2_t f = {(_Float16)by, (_Float16)by}, bias = f * (_Float16)-1152.f;
+    const half2_t both = __builtin_bit_cast(half2_t, c.by), f = {both.x, both.x}, bias = {both.y, both.y};
     a ^= 0x80808080u;
     b ^= 0x80808080u;
-    h[0] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, a, 0x04010400u)), f, bias);
-    h[1] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, a, 0x04030402u)), f, bias);
-    h[2] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, b, 0x04010400u)), f, bias);
-    h[3] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, b, 0x04030402u)), f, bias);
+    h[0] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(c.top, a, 0x04010400u)), f, bias);
+    h[1] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(c.top, a, 0x04030402u)), f, bias);
+    h[2] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(c.top, b, 0x04010400u)), f, bias);
+    h[3] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(c.top, b, 0x04030402u)), f, bias);
   }
   return half8_t{h[0].x, h[0].y, h[1].x, h[1].y, h[2].x, h[2].y, h[3].x, h[3].y};
 }
-template <bool E4M3>
-__device__ __forceinline__ half8_t expand(uint32_t a, uint32_t b) { return expand_by<E4M3>(a, b, 1.f); }
 
 struct BlockSeq { int n, t, packed; };
 __device__ __forceinline__ BlockSeq block_seq(const BlockAttnArgs& a, int b) {
@@ -55,21 +61,26 @@ __device__ __forceinline__ BlockSeq block_seq(const BlockAttnArgs& a, int b) {
 }
 
 __device__ __forceinline__ float lane_of(float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); }
+__device__ __forceinline__ uint32_t lane_of(uint32_t x, int i) { return (uint32_t)__builtin_amdgcn_readlane((int)x, i); }
 // The magnitude that raises a level: beyond kFar the sooner, so that a weight stays in fp16 whatever the rounding of the sum.
 __device__ __forceinline__ float threshold(float m) { return __builtin_fmaf(-kFarShare, __builtin_fabsf(m), m) + kRaise; }
 
 // Scales.  That of a block of keys is a factor of its scores.  That of a block of values is a summand of the exponent, so that a weight carries it:
 //   w = 2^(s + log2 S - level),  O = sum w code,  l = sum w / S  (of the same rounded weights).
 // A block of far smaller values than the largest ones so far would have weights that fp16 does not hold, though they count in full in l; below 1/16
-// of that scale it is taken as S = 2^k S_v with codes times 2^-k (exact in fp16 down to 2^-24).
-struct Scales { float by, add, inv, shrink; };           // factor of the scores, log2 S, 1 / S, 2^-k
+// of that scale it is taken as S = 2^k S_v with codes times 2^-k.  Of that product fp16 holds multiples of 2^-24, so that every scale is taken 2^-kLift times and
+// codes 2^kLift times as large: what is rounded is off by 2^-25 at 2^-8 of the largest scale and less, 2^-39 of the largest value.
+constexpr int kLift = 5;                                 // (1152 2^5, which integers have taken away, is an fp16 number)
+struct Scales { float by, add, inv; Codes values; };     // factor of the scores, log2 S, 1 / S, 2^-k
 
 constexpr float kScoreScale = 0.08838834764831845f * 1.4426950408889634f;        // log2(e) / sqrt(d)
 
 // Where 64 tiles of a sequence's kv head lie, and their scales: a tile a lane.
+template <bool E4M3>
 struct BlockUnits {
   long long at = 0;
-  float by = 0.f, add = 0.f, inv = 0.f, shrink = 1.f, largest = 0.f;
+  float by = 0.f, add = 0.f, inv = 0.f, largest = 0.f;
+  Codes values = {0u, 0u};
   int base = -1;
   // Tile u (not below an earlier one) is among them from now on; tiles end before u1.
   __device__ __forceinline__ void look(const BlockStore& s, int b, int h, int u, int u1, int lane) {
@@ -85,8 +96,8 @@ struct BlockUnits {
     largest = fmaxf(largest, most);
     const float least = largest > 0.f ? largest * 0.0625f : 1.f;
     const int k = vs < least && vs > 0.f ? __builtin_amdgcn_frexp_expf(least) - __builtin_amdgcn_frexp_expf(vs) + 1 : 0;
-    const float size = vs > 0.f ? __builtin_amdgcn_ldexpf(vs, k) : least;        // (no values but zeros: any)
-    shrink = __builtin_amdgcn_ldexpf(1.f, -k);
+    const float size = vs > 0.f ? __builtin_amdgcn_ldexpf(vs, k - kLift) : least;        // (no values but zeros: any)
+    values = codes_times<E4M3>(kLift - k);
     add = __builtin_amdgcn_logf(size);
     inv = 1.0f / size;
   }
@@ -94,7 +105,9 @@ struct BlockUnits {
     return (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(at >> 32), u - base) << 32) |
                        (unsigned)__builtin_amdgcn_readlane((int)at, u - base));
   }
-  __device__ __forceinline__ Scales scales(int u) const { return {lane_of(by, u - base), lane_of(add, u - base), lane_of(inv, u - base), lane_of(shrink, u - base)}; }
+  __device__ __forceinline__ Scales scales(int u) const {
+    return {lane_of(by, u - base), lane_of(add, u - base), lane_of(inv, u - base), {lane_of(values.by, u - base), lane_of(values.top, u - base)}};
+  }
 };
 
 // What a work-group does.
