@@ -63,7 +63,7 @@ __device__ __forceinline__ int put_at(bool keys, int part, int lane) {
   return kUnitValues + part * 2048 + (g >> 1) * 1024 + (g & 1) * 512 + c * 16;
 }
 template <bool E4M3>
-__device__ __forceinline__ void put_codes(char* dst, int apart, const u32x4& w, const Codes& by) {
+__device__ __forceinline__ void put_codes(char* dst, int apart, const u32x4& w, uint32_t by) {
   *reinterpret_cast<half8_t*>(dst) = expand<E4M3>(w.x, w.y, by);
   *reinterpret_cast<half8_t*>(dst + apart) = expand<E4M3>(w.z, w.w, by);
 }
@@ -83,7 +83,7 @@ struct PlainPart {
   }
 };
 template <int WAVES>
-__device__ __forceinline__ void put_plain(char* buf, int tid, const Staged& x) {
+__device__ __forceinline__ void put_plain(char* buf, int tid, const Staged& x, uint32_t by) {
   constexpr int N = PlainPart<WAVES>::N;
   {
     const PlainPart<WAVES> part(tid);
@@ -99,8 +99,8 @@ __device__ __forceinline__ void put_plain(char* buf, int tid, const Staged& x) {
   for (int p = 0; p < N; ++p) {                          // channels ch + 2 p, ch + 2 p + 1
     const u32x2 even = {__builtin_amdgcn_perm(w[1][p], w[0][p], 0x05040100u), __builtin_amdgcn_perm(w[3][p], w[2][p], 0x05040100u)};
     const u32x2 odd = {__builtin_amdgcn_perm(w[1][p], w[0][p], 0x07060302u), __builtin_amdgcn_perm(w[3][p], w[2][p], 0x07060302u)};
-    *reinterpret_cast<u32x2*>(dst + 16 * p) = even;
-    *reinterpret_cast<u32x2*>(dst + 16 * p + 256) = odd;
+    *reinterpret_cast<u32x2*>(dst + 16 * p) = u32x2{times(even.x, by), times(even.y, by)};
+    *reinterpret_cast<u32x2*>(dst + 16 * p + 256) = u32x2{times(odd.x, by), times(odd.y, by)};
   }
 }
 
@@ -125,6 +125,12 @@ __device__ __forceinline__ void raise_level(State& r, float mine) {
   r.zero = level == -INFINITY ? 0.f : level;
   r.raise = threshold(level);
   r.far = __builtin_amdgcn_ballot_w64(__builtin_fabsf(r.zero) > kFar) != 0;
+}
+__device__ __forceinline__ void shift_level(State& r, int e) {
+  r.m -= (float)e;
+  r.l = __builtin_amdgcn_ldexpf(r.l, e);
+  r.zero = r.m == -INFINITY ? 0.f : r.m;
+  r.raise = threshold(r.m);
 }
 // Weights of scores 2 e, 2 e + 1.
 __device__ __forceinline__ void two_weights(int e, const float16_t& s, float by, float bias, half8_t (&p)[2], float& sum) {
@@ -252,8 +258,8 @@ __device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& 
   const int t0 = w.split * share + (w.split < more ? w.split : more), t1 = t0 + share + (w.split < more ? 1 : 0);
 
   const int u1 = t1 < tiles1 ? t1 : tiles1;
+  BlockUnits<E4M3> units;
   if (t0 < u1) {
-    BlockUnits<E4M3> units;
     // (eight wavefronts: half of them bring keys, half values)
     const bool keys = WAVES == 4 || wave < 4;
     const uint32_t mine_at = (uint32_t)(64 * (wave & 3) + lane) * 16;
@@ -276,6 +282,9 @@ __device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& 
     const long long open_at = bh * a.s.block * D;
     const __half *ko = a.s.k.open + open_at, *vo = a.s.v.open + open_at;
     const __half *kf = a.k.p + b * a.k.batch + h * a.k.head, *vf = a.v.p + b * a.v.batch + h * a.v.head;
+    const int shift = plain_shift(units.largest);
+    const uint32_t by = half_power(-shift) * 0x10001u;
+    if (shift) shift_level(r, shift);                    // (uniform)
     // (selections, no branches: the lanes of a wavefront may differ)
     auto row_at = [&](const __half* o, const __half* f, long long pitch, int i) {
       const bool waits = i < open;
@@ -284,7 +293,7 @@ __device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& 
       return (waits ? o : f) + at * step;
     };
     auto fetch = [&](int u, Staged& x, Scales& sc) {
-      sc = Scales{kScoreScale, 0.f, 1.f, {}};
+      sc = kPlainScales;
       const int i0 = u * kBlockTile;
       auto token = [&](int i) { return i0 + i < plain ? i0 + i : plain - 1; };   // (behind the last one: that one again, masked)
       constexpr int N = PlainPart<WAVES>::N, PAIRS = 64 / N;                     // (as put_plain)
@@ -311,8 +320,9 @@ __device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& 
       for (int i = 0; i < 16; ++i)
         if (token_of(i, half) > left) sc[i] = -INFINITY;
     };
-    walk(t0 > tiles1 ? t0 - tiles1 : 0, t1 - tiles1, lds, r, lane, fetch, [&](char* buf, const Staged& x, const Scales&) { put_plain<WAVES>(buf, tid, x); },
-               mask);
+    walk(t0 > tiles1 ? t0 - tiles1 : 0, t1 - tiles1, lds, r, lane, fetch,
+         [&](char* buf, const Staged& x, const Scales&) { put_plain<WAVES>(buf, tid, x, by); }, mask);
+    if (shift) shift_level(r, -shift);
   }
 
   // results: a lane has channels 32 x + 16 y + 8 half + 2 i + m of its row, at o[x][4 y + 8 m + i]

@@ -169,9 +169,9 @@ __device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& 
   const int t0 = part * share + (part < more ? part : more), t1 = t0 + share + (part < more ? 1 : 0);
 
   const int u1 = t1 < tiles1 ? t1 : tiles1;
+  BlockUnits<E4M3> units;
   if (t0 < u1) {
     // (tiles are loaded two ahead; behind the last one: that one again)
-    BlockUnits<E4M3> units;
     auto load = [&](int u, Tile& t) {
       u = u < u1 ? u : u1 - 1;
       units.look(a.s, b, h, u, u1, lane);
@@ -206,6 +206,16 @@ __device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& 
     p.kp = a.k.token;
     p.vp = a.v.token;
     p.open = open;
+    const int shift = plain_shift(units.largest);
+    const uint32_t by = half_power(-shift) * 0x10001u;
+    auto shift_by = [&](int e) {
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        r.m[n] -= (float)e;
+        r.l[n] = __builtin_amdgcn_ldexpf(r.l[n], e);
+      }
+    };
+    if (shift) shift_by(shift);                          // (uniform)
     for (int u = t0 > tiles1 ? t0 : tiles1; u < t1; ++u) {
       const int i0 = (u - tiles1) * kBlockTile;
       auto token = [&](int i) { return i0 + i < plain ? i0 + i : plain - 1; };    // (behind the last one: that one again, masked)
@@ -232,7 +242,7 @@ __device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& 
             if (i0 + 16 * x + 4 * g + i > limit) sc[n][x][i] = -INFINITY;
       }
       half8_t w[NR][kPieces<NR>];
-      weights<NR>(r, sc, Scales{kScoreScale, 0.f, 1.f, {}}, w);
+      weights<NR>(r, sc, kPlainScales, w);
       const __half* vsrc[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) vsrc[j] = p.value(token(16 * (j >> 2) + 4 * g + (j & 3))) + 2 * c;
@@ -240,7 +250,7 @@ __device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& 
       for (int q = 0; q < 4; ++q) {
         uint32_t x[8], e[4], o[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = *reinterpret_cast<const uint32_t*>(vsrc[j] + 32 * q);
+        for (int j = 0; j < 8; ++j) x[j] = times(*reinterpret_cast<const uint32_t*>(vsrc[j] + 32 * q), by);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           e[j] = __builtin_amdgcn_perm(x[2 * j + 1], x[2 * j], 0x05040100u);
@@ -250,6 +260,7 @@ __device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& 
         add_values<NR>(r, 2 * q + 1, __builtin_bit_cast(half8_t, u32x4{o[0], o[1], o[2], o[3]}), w);
       }
     }
+    if (shift) shift_by(-shift);
   }
 
   // the wavefronts' results meet in LDS, each joins CH channels of a lane's eight in channels 32 q ..

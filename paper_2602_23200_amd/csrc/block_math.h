@@ -12,36 +12,32 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // log2 of the weight that the largest score has when it raises the level, and of the largest weight before the level is raised.
-constexpr float kTop = 9.0f, kRaise = 15.0f;
+constexpr float kTop = 10.0f, kRaise = 15.0f;
 constexpr float kFar = 0x1p19f;                          // levels beyond: neighbours in fp32 are 2^-4 apart and more
 constexpr float kFarShare = 0x1p-16f;                    // of its own size, by which a level is raised the sooner
 
 // By which power of two a tensor's codes are multiplied.  E4M3: its bits in fp32; integers: see int_codes.
-struct Codes { uint32_t by, top; };
 template <bool E4M3>
-__device__ __forceinline__ constexpr Codes codes_times(int x) {
-  if (E4M3) return {(uint32_t)(x + 127) << 23, 0u};
-  const IntCodes c = int_codes(x);
-  return {c.factor_bias, c.top};
-}
+__device__ __forceinline__ constexpr uint32_t codes_times(int x) { return E4M3 ? (uint32_t)(x + 127) << 23 : int_codes(x); }
 // Eight codes as fp16, times that: exact down to multiples of 2^-24 (integers to 2^-24, E4M3, whose codes reach 2^-9, to 2^-15), rounded to them below.
 template <bool E4M3>
-__device__ __forceinline__ half8_t expand(uint32_t a, uint32_t b, const Codes& c) {
+__device__ __forceinline__ half8_t expand(uint32_t a, uint32_t b, uint32_t by) {
   half2_t h[4];
   if constexpr (E4M3) {
-    const float by = __uint_as_float(c.by);
-    h[0] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, by, false));
-    h[1] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, by, true));
-    h[2] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, by, false));
-    h[3] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, by, true));
+    const float f = __uint_as_float(by);
+    h[0] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, f, false));
+    h[1] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, f, true));
+    h[2] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, f, false));
+    h[3] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, f, true));
   } else {
-    const half2_t both = __builtin_bit_cast(half2_t, c.by), f = {both.x, both.x}, bias = {both.y, both.y};
+    const half2_t both = __builtin_bit_cast(half2_t, by), f = {both.x, both.x}, bias = {both.y, both.y};
+    const uint32_t top = int_codes_top(by);
     a ^= 0x80808080u;
     b ^= 0x80808080u;
-    h[0] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(c.top, a, 0x04010400u)), f, bias);
-    h[1] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(c.top, a, 0x04030402u)), f, bias);
-    h[2] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(c.top, b, 0x04010400u)), f, bias);
-    h[3] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(c.top, b, 0x04030402u)), f, bias);
+    h[0] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(top, a, 0x04010400u)), f, bias);
+    h[1] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(top, a, 0x04030402u)), f, bias);
+    h[2] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(top, b, 0x04010400u)), f, bias);
+    h[3] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, __builtin_amdgcn_perm(top, b, 0x04030402u)), f, bias);
   }
   return half8_t{h[0].x, h[0].y, h[1].x, h[1].y, h[2].x, h[2].y, h[3].x, h[3].y};
 }
@@ -67,11 +63,14 @@ __device__ __forceinline__ float threshold(float m) { return __builtin_fmaf(-kFa
 
 // Scales.  That of a block of keys is a factor of its scores.  That of a block of values is a summand of the exponent, so that a weight carries it:
 //   w = 2^(s + log2 S - level),  O = sum w code,  l = sum w / S  (of the same rounded weights).
-// A block of far smaller values than the largest ones so far would have weights that fp16 does not hold, though they count in full in l; below 1/16
-// of that scale it is taken as S = 2^k S_v with codes times 2^-k.  Of that product fp16 holds multiples of 2^-24, so that every scale is taken 2^-kLift times and
-// codes 2^kLift times as large: what is rounded is off by 2^-25 at 2^-8 of the largest scale and less, 2^-39 of the largest value.
+// A token whose S is far below that of a stronger one would meet fp16's smallest step, 2^-24, the sooner, though it counts in full in l.  So the scale of a block
+// is taken as S = 2^k S_v, from half of the largest one so far up to all of it, with codes times 2^-k; and that of new and open rows, which is 1, as a power of
+// two not below half of the largest, with values divided by it.  Weights are then off by 2^-25 at a level of 2^10 below the largest one, and by one
+// factor of two for the scales: 2^-34 of the largest.  (Scales as they are down to 1/16 of the largest, and 1 for new rows: 2^-30, and 2^-25.)
+// Of the codes' products fp16 holds multiples of 2^-24, so that every S is taken 2^-kLift times and codes 2^kLift times as large: what is rounded is off by 2^-25
+// at 2^-5 of the largest scale and less, 2^-36 of the largest value; and new rows are divided by more than 1 only beside values above 2^11.
 constexpr int kLift = 5;                                 // (1152 2^5, which integers have taken away, is an fp16 number)
-struct Scales { float by, add, inv; Codes values; };     // factor of the scores, log2 S, 1 / S, 2^-k
+struct Scales { float by, add, inv; uint32_t values; };  // factor of the scores, log2 S, 1 / S, by what codes of values are multiplied
 
 constexpr float kScoreScale = 0.08838834764831845f * 1.4426950408889634f;        // log2(e) / sqrt(d)
 
@@ -80,7 +79,7 @@ template <bool E4M3>
 struct BlockUnits {
   long long at = 0;
   float by = 0.f, add = 0.f, inv = 0.f, largest = 0.f;
-  Codes values = {0u, 0u};
+  uint32_t values = 0u;
   int base = -1;
   // Tile u (not below an earlier one) is among them from now on; tiles end before u1.
   __device__ __forceinline__ void look(const BlockStore& s, int b, int h, int u, int u1, int lane) {
@@ -94,9 +93,8 @@ struct BlockUnits {
 #pragma unroll
     for (int i = 32; i > 0; i /= 2) most = fmaxf(most, __shfl_xor(most, i));
     largest = fmaxf(largest, most);
-    const float least = largest > 0.f ? largest * 0.0625f : 1.f;
-    const int k = vs < least && vs > 0.f ? __builtin_amdgcn_frexp_expf(least) - __builtin_amdgcn_frexp_expf(vs) + 1 : 0;
-    const float size = vs > 0.f ? __builtin_amdgcn_ldexpf(vs, k - kLift) : least;        // (no values but zeros: any)
+    const int e = largest > 0.f ? __builtin_amdgcn_frexp_expf(largest) : 1 + kLift, k = vs > 0.f ? e - __builtin_amdgcn_frexp_expf(vs) : 0;
+    const float size = __builtin_amdgcn_ldexpf(vs > 0.f ? vs : 0.5f, (vs > 0.f ? k : e) - kLift);      // (no values but zeros: any)
     values = codes_times<E4M3>(kLift - k);
     add = __builtin_amdgcn_logf(size);
     inv = 1.0f / size;
@@ -106,9 +104,20 @@ struct BlockUnits {
                        (unsigned)__builtin_amdgcn_readlane((int)at, u - base));
   }
   __device__ __forceinline__ Scales scales(int u) const {
-    return {lane_of(by, u - base), lane_of(add, u - base), lane_of(inv, u - base), {lane_of(values.by, u - base), lane_of(values.top, u - base)}};
+    return {lane_of(by, u - base), lane_of(add, u - base), lane_of(inv, u - base), lane_of(values, u - base)};
   }
 };
+
+// log2 of the divisor of fp16 rows behind blocks whose largest scale is `largest` (0: none).  The level and the sum of a row are brought to its unit before such rows
+// and back behind them, so that the rows' weights are what they would be with S = 1.
+__device__ __forceinline__ int plain_shift(float largest) {
+  const int e = __builtin_amdgcn_readfirstlane(largest > 0.f ? __builtin_amdgcn_frexp_expf(largest) : 0) - 1 - kLift;
+  return e < 0 ? 0 : e;
+}
+constexpr Scales kPlainScales = {kScoreScale, 0.f, 1.f, 0u};
+__device__ __forceinline__ uint32_t times(uint32_t pair, uint32_t by) {
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, pair) * __builtin_bit_cast(half2_t, by));
+}
 
 // What a work-group does.
 struct BlockWork { int b, h, row_block, split, n_splits; long long slot; };

@@ -17,16 +17,15 @@ constexpr long long kBlockMostCapacity = 1LL << 24;      // tokens and their pro
 constexpr long long block_packed(long long n, int block) { return n - n % block; }
 
 // Eight-bit integers as fp16 times 2^x, with one rounding.  A byte of two's complement with its sign bit flipped, code + 128, is put under the exponent of 1024
-// (`top`: the other byte): the number 1024 + 128 + code, which times 2^x, and 1152 2^x taken away, is one fused operation.  Below 2^-24 the factor is no
+// (the other byte is 0x64): the number 1024 + 128 + code, which times 2^x, and 1152 2^x taken away, is one fused operation.  Below 2^-24 the factor is no
 // fp16 number any more; there the byte stands alone, as (code + 128) 2^-24, with a factor of 2^(x + 24) and 128 2^x taken away.  Below 2^-31 every
 // product is less than half of the smallest step: zero.
-struct IntCodes { uint32_t factor_bias, top; };          // factor in the lower half
 constexpr uint32_t half_power(int x) { return x >= -14 ? (uint32_t)(x + 15) << 10 : 1u << (x + 24); }        // bits of 2^x, -24 <= x <= 15
-constexpr IntCodes int_codes(int x) {                    // x <= 5
-  return x >= -24 ? IntCodes{half_power(x) | (0x8080u | (uint32_t)(x + 25) << 10) << 16, 0x64646464u}
-       : x >= -31 ? IntCodes{half_power(x + 24) | (0x8000u | half_power(x + 7)) << 16, 0u}
-                  : IntCodes{0u, 0u};
+constexpr uint32_t int_codes(int x) {                    // x <= 5; the factor in the lower half, what is taken away (as a negative number) in the upper one
+  return x >= -24 ? half_power(x) | (0x8080u | (uint32_t)(x + 25) << 10) << 16 : x >= -31 ? half_power(x + 24) | (0x8000u | half_power(x + 7)) << 16 : 0u;
 }
+// (1152 is 1.125 x 1024: its bit stands for the case, since a power of two below 2^-17 has no bit there)
+constexpr uint32_t int_codes_top(uint32_t both) { return both >> 23 & 1u ? 0x64646464u : 0u; }
 
 // ---- attention.  A row: one query head of one new token; the rows of a kv head share its keys.
 constexpr int kBlockSplitMost = 256;    // most ranges the keys of a row are split into

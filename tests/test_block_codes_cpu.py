@@ -13,7 +13,7 @@ MAIN = r"""
 #include <stdio.h>
 #include "paper_2602_23200_amd/csrc/block_plan.h"
 int main() {
-  for (int x = -45; x <= 5; ++x) printf("%d %u %u\n", x, innerq::int_codes(x).factor_bias, innerq::int_codes(x).top);
+  for (int x = -45; x <= 5; ++x) printf("%d %u %u\n", x, innerq::int_codes(x), innerq::int_codes_top(innerq::int_codes(x)));
 }
 """
 
