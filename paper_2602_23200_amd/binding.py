@@ -618,7 +618,7 @@ def allocate_block_cache(cfg: innerq_block_config_t, device="cuda", page_table=N
         setattr(c, name, _ptr(bufs[name]))
     if cfg.page_pool_pages > 0:
         assert page_table is not None and page_table.dtype == torch.int32 and page_table.is_contiguous()
-        assert tuple(page_table.shape) == (cfg.batch, cfg.capacity_tokens // 64)
+        assert tuple(page_table.shape) == (cfg.batch, cfg.capacity_tokens // 64) and page_table.device == bufs["k_codes"].device
         bufs["page_table"] = page_table
         c.page_table = _ptr(page_table)
     return BlockCache(cfg, bufs, c)
@@ -644,23 +644,25 @@ def _strides(batch: int, head: int, token: int):
 
 
 def _block_rows(t, batch: int, heads: int, tokens: int, dim: int, dtype=None):
-    """_rows for the calls below (a third of the host's time in a call on short sequences went into it)."""
+    """_rows for the calls below (a third of the host's time in a call on short sequences went into it); on which device they lie is _block_stream's to check."""
     if dtype is None:
         import torch
         dtype = torch.float16
     b, h, n, one = t.stride()
-    assert t.is_cuda and t.dtype is dtype and t.shape == (batch, heads, tokens, dim) and one == 1
+    assert t.dtype is dtype and t.shape == (batch, heads, tokens, dim) and one == 1
     return t.data_ptr(), _strides(b if batch > 1 else 0, h if heads > 1 else 0, n if tokens > 1 else 0)
 
 
-def _block_stream(stream, t) -> Optional[int]:
-    """_stream for rows t, which lie on the current device: calls launch there."""
+def _block_stream(stream, cache: BlockCache, *tensors) -> Optional[int]:
+    """_stream for a call whose cache and tensors lie on the current device, where calls launch (the buffers of a cache lie on one)."""
     import torch
     try:
         device = torch._C._cuda_getDevice()
     except AttributeError:                                # (a private name, as in _stream)
         device = torch.cuda.current_device()
-    assert t.get_device() == device
+    assert cache.buffers["k_codes"].get_device() == device
+    for t in tensors:
+        assert t is None or t.get_device() == device
     return _stream(stream)
 
 
@@ -669,7 +671,7 @@ def innerq_block_append(cache: BlockCache, k_new, v_new, stream=None) -> None:
     cfg = cache.cfg
     B, H, T, d = cfg.batch, cfg.n_kv_heads, k_new.shape[2], cfg.head_dim
     _checked(lib().innerq_block_append(_byref(cfg), _byref(cache.c), *_block_rows(k_new, B, H, T, d), *_block_rows(v_new, B, H, T, d), T,
-                                       _block_stream(stream, k_new)), "innerq_block_append")
+                                       _block_stream(stream, cache, k_new, v_new)), "innerq_block_append")
 
 
 def innerq_block_append_ragged(cache: BlockCache, n_tokens_dev, t_new_dev, k_new, v_new, stream=None) -> None:
@@ -679,7 +681,7 @@ def innerq_block_append_ragged(cache: BlockCache, n_tokens_dev, t_new_dev, k_new
     B, H, T, d = cfg.batch, cfg.n_kv_heads, k_new.shape[2], cfg.head_dim
     _checked(lib().innerq_block_append_ragged(_byref(cfg), _byref(cache.c), _counts(n_tokens_dev, cfg), _counts(t_new_dev, cfg),
                                               *_block_rows(k_new, B, H, T, d), *_block_rows(v_new, B, H, T, d), T,
-                                              _block_stream(stream, k_new)),
+                                              _block_stream(stream, cache, k_new, v_new, n_tokens_dev, t_new_dev)),
              "innerq_block_append_ragged")
 
 
@@ -689,30 +691,31 @@ def _wanted_rows(t, cfg, count):
 
 def innerq_block_read(cache: BlockCache, first: int, k_out=None, v_out=None, stream=None):
     """Tokens first .. of every sequence into the fp16 rows k_out, v_out [B, Hk, T, d] (either may be None)."""
-    cfg, some = cache.cfg, v_out if k_out is None else k_out
-    T = some.shape[2]
+    cfg, T = cache.cfg, (v_out if k_out is None else k_out).shape[2]
     _checked(lib().innerq_block_read(_byref(cfg), _byref(cache.c), first, T, *_wanted_rows(k_out, cfg, T), *_wanted_rows(v_out, cfg, T),
-                                     _block_stream(stream, some)), "innerq_block_read")
+                                     _block_stream(stream, cache, k_out, v_out)), "innerq_block_read")
     return k_out, v_out
 
 
 def innerq_block_read_ragged(cache: BlockCache, n_tokens_dev, first_dev, k_out=None, v_out=None, stream=None):
     """innerq_block_read with counts and first tokens (None: 0) of every sequence in device memory; rows of tokens that are not there are
     left as they were."""
-    cfg, some = cache.cfg, v_out if k_out is None else k_out
-    T = some.shape[2]
+    cfg, T = cache.cfg, (v_out if k_out is None else k_out).shape[2]
     _checked(lib().innerq_block_read_ragged(_byref(cfg), _byref(cache.c), _counts(n_tokens_dev, cfg), _counts(first_dev, cfg), T,
-                                            *_wanted_rows(k_out, cfg, T), *_wanted_rows(v_out, cfg, T), _block_stream(stream, some)),
+                                            *_wanted_rows(k_out, cfg, T), *_wanted_rows(v_out, cfg, T),
+                                            _block_stream(stream, cache, k_out, v_out, n_tokens_dev, first_dev)),
              "innerq_block_read_ragged")
     return k_out, v_out
 
 
-def _block_result(out, q, B: int, H: int, T: int, d: int, workspace, stream):
-    """The arguments from the queries on, and the output."""
+def _block_result(cache: BlockCache, out, q, T: int, workspace, stream, *tensors):
+    """The arguments from the queries on, and the output.  tensors: the call's other ones."""
+    cfg = cache.cfg
+    B, H, d = cfg.batch, cfg.n_q_heads, cfg.head_dim
     out = _chunk_out(out, q)
-    assert workspace.is_cuda and workspace.is_contiguous()
+    assert workspace.is_contiguous()
     return out, (*_block_rows(q, B, H, T, d), T, *_block_rows(out, B, H, T, d, out.dtype), int(out.element_size() == 4),
-                 workspace.data_ptr(), workspace.nbytes, _block_stream(stream, q))
+                 workspace.data_ptr(), workspace.nbytes, _block_stream(stream, cache, q, out, workspace, *tensors))
 
 
 def innerq_block_attention(cache: BlockCache, k_new, v_new, q, workspace, out=None, stream=None):
@@ -720,7 +723,7 @@ def innerq_block_attention(cache: BlockCache, k_new, v_new, q, workspace, out=No
     -> out [B, Hq, T, d] (fp32 unless an fp16 `out` is passed)."""
     cfg = cache.cfg
     B, H, T, d = cfg.batch, cfg.n_kv_heads, q.shape[2], cfg.head_dim
-    out, rest = _block_result(out, q, B, cfg.n_q_heads, T, d, workspace, stream)
+    out, rest = _block_result(cache, out, q, T, workspace, stream, k_new, v_new)
     _checked(lib().innerq_block_attention(_byref(cfg), _byref(cache.c), *_block_rows(k_new, B, H, T, d), *_block_rows(v_new, B, H, T, d),
                                           *rest), "innerq_block_attention")
     return out
@@ -732,7 +735,7 @@ def innerq_block_attention_ragged(cache: BlockCache, n_tokens_dev, t_new_dev, ma
     new ones, at most T (None: T each); max_tokens bounds their sum."""
     cfg = cache.cfg
     B, H, T, d = cfg.batch, cfg.n_kv_heads, q.shape[2], cfg.head_dim
-    out, rest = _block_result(out, q, B, cfg.n_q_heads, T, d, workspace, stream)
+    out, rest = _block_result(cache, out, q, T, workspace, stream, k_new, v_new, n_tokens_dev, t_new_dev)
     _checked(lib().innerq_block_attention_ragged(_byref(cfg), _byref(cache.c), _counts(n_tokens_dev, cfg), _counts(t_new_dev, cfg),
                                                  max_tokens, *_block_rows(k_new, B, H, T, d), *_block_rows(v_new, B, H, T, d), *rest),
              "innerq_block_attention_ragged")
@@ -742,7 +745,7 @@ def innerq_block_attention_ragged(cache: BlockCache, n_tokens_dev, t_new_dev, ma
 def innerq_block_cross_attention(cache: BlockCache, q, workspace, out=None, stream=None):
     """q [B, Hq, T, d] attends to all cached tokens -> out [B, Hq, T, d] (fp32 unless an fp16 `out` is passed)."""
     cfg = cache.cfg
-    out, rest = _block_result(out, q, cfg.batch, cfg.n_q_heads, q.shape[2], cfg.head_dim, workspace, stream)
+    out, rest = _block_result(cache, out, q, q.shape[2], workspace, stream)
     _checked(lib().innerq_block_cross_attention(_byref(cfg), _byref(cache.c), *rest), "innerq_block_cross_attention")
     return out
 
@@ -750,7 +753,7 @@ def innerq_block_cross_attention(cache: BlockCache, q, workspace, out=None, stre
 def innerq_block_cross_attention_ragged(cache: BlockCache, n_tokens_dev, t_new_dev, max_tokens: int, q, workspace, out=None, stream=None):
     """innerq_block_cross_attention with the counts of every sequence in device memory; a sequence without a token has rows of zeros."""
     cfg = cache.cfg
-    out, rest = _block_result(out, q, cfg.batch, cfg.n_q_heads, q.shape[2], cfg.head_dim, workspace, stream)
+    out, rest = _block_result(cache, out, q, q.shape[2], workspace, stream, n_tokens_dev, t_new_dev)
     _checked(lib().innerq_block_cross_attention_ragged(_byref(cfg), _byref(cache.c), _counts(n_tokens_dev, cfg), _counts(t_new_dev, cfg),
                                                        max_tokens, *rest), "innerq_block_cross_attention_ragged")
     return out
