@@ -496,7 +496,8 @@ typedef enum {
   INNERQ_BLOCK_BUF_COUNT
 } innerq_block_buffer_t;
 
-/* Host-only: as innerq_validate_config, innerq_buffer_bytes and innerq_chunk_workspace_bytes (t_new: rows of a sequence). */
+/* Host-only: as innerq_validate_config, innerq_buffer_bytes and innerq_chunk_workspace_bytes (t_new: rows of a sequence; a workspace for
+ * so many serves calls of fewer, too). */
 int innerq_block_validate_config(const innerq_block_config_t *cfg);
 size_t innerq_block_buffer_bytes(const innerq_block_config_t *cfg, int which /* innerq_block_buffer_t */);
 size_t innerq_block_workspace_bytes(const innerq_block_config_t *cfg, int64_t t_new);

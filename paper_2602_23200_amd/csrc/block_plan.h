@@ -52,9 +52,11 @@ constexpr BlockKind kBlockFew = kBlockKinds[1], kBlockMany = kBlockKinds[3];    
 // Bytes of the cache a us.  (Up to 224 work-groups no CU has two while another has none.  8 sequences of 8 heads over 32k tokens, one token: in 3 ranges 84 us,
 // 4 93, 6 90, 8 93, 12 91; 5 tokens: 93, 96, 97, 98.)
 constexpr float block_rate(float groups) { return groups <= 224.f ? 6.5e6f : 6.0e6f; }
+// Fewest rows of a form.
+constexpr int block_least_rows(const BlockForm& f) { return f.rows == 16 ? 1 : f.rows / 2 + 1; }
 // Forms that come into question (of 16 rows a work-group for 17 and more reads the keys too often, of 64 for 129; wider ones would be empty for the most part).
 constexpr bool block_suits(const BlockForm& f, long long rows) {
-  return f.rows == 16 ? rows <= 16 : f.rows == 32 ? rows > 16 : f.rows == 64 ? rows > 32 && rows <= 128 : rows > f.rows / 2;
+  return rows >= block_least_rows(f) && (f.rows == 16 ? rows <= 16 : f.rows != 64 || rows <= 128);
 }
 // units: tiles of the longest row block; average: of one in the mean.
 inline float block_cost(const BlockKind& k, long long heads, long long row_blocks, float units, float average, int n) {
@@ -70,9 +72,10 @@ inline float block_cost(const BlockKind& k, long long heads, long long row_block
   us = std::sqrt(std::sqrt(us * us * us * us + bytes * bytes * bytes * bytes));      // (the larger of the two, and more where they are alike)
   return us + (n > 1 ? k.join + 0.85f * (float)((n + 7) / 8) + groups * (float)k.form.rows / k.partial : 0.f);
 }
-// Most ranges: partial results for one round of work-groups (many rows: two).
+// Most partial results: for one round of work-groups (many rows: two).
+constexpr int block_most_slots(const BlockForm& f) { return (f.rows > kBlockFewRows ? 2 : 1) * block_round(f); }
 inline int block_split_most(const BlockForm& f, long long heads, long long row_blocks) {
-  const long long most = (f.rows > kBlockFewRows ? 2 : 1) * block_round(f) / (heads * row_blocks);
+  const long long most = block_most_slots(f) / (heads * row_blocks);
   return (int)(most < 1 ? 1 : most > kBlockSplitMost ? kBlockSplitMost : most);
 }
 struct BlockPlan { BlockForm form; long long row_blocks; int n_splits; float us; };
@@ -185,14 +188,14 @@ constexpr BlockPlace block_place(int at, int units, int n_kv_heads, int splits) 
   return {h, rest % blocks, rest / blocks};
 }
 
-// (whatever the number of tokens)
+// Whatever the number of tokens, and enough for fewer rows, too.
 inline size_t block_workspace_bytes(const innerq_block_config_t& c, long long t_new) {
   const long long heads = (long long)c.batch * c.n_kv_heads, rows = t_new * (c.n_q_heads / c.n_kv_heads);
   size_t bytes = 0;
   for (const BlockKind& k : kBlockKinds) {
-    const long long row_blocks = ceil_div(rows, k.form.rows), most = block_split_most(k.form, heads, row_blocks);
-    if (!block_suits(k.form, rows) || most == 1) continue;
-    const size_t slots = (size_t)(heads * row_blocks * most) * block_slot_bytes(k.form.rows);
+    // (fewer row blocks may be split where these are not)
+    if (rows < block_least_rows(k.form) || block_split_most(k.form, heads, 1) == 1) continue;
+    const size_t slots = block_most_slots(k.form) * block_slot_bytes(k.form.rows);
     bytes = slots > bytes ? slots : bytes;
   }
   for (const bool all_few : {false, true}) {
