@@ -28,11 +28,12 @@ template <bool E4M3, int NR>
 __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(NR == 4 ? 1 : 2))) block_attention_kernel(BlockAttnArgs a) {
   __shared__ float lds[kFloats<NR>];
   BlockWork work;
-  if (a.table) {
-    if (!find_work<16 * NR, W>(a, 0, a.few_most, (int)blockIdx.x, work)) return;      // (uniform)
-  } else {
-    work = uniform_work(a);
+  bool listed = false;
+  if constexpr (NR <= 2) {                               // (lists have work-groups of 16 or 32 rows)
+    listed = a.table != nullptr;
+    if (listed && !find_work<16 * NR, W>(a, 0, a.few_most, (int)blockIdx.x, work)) return;      // (uniform)
   }
+  if (!listed) work = uniform_work(a);
   attend<E4M3, NR>(a, work, lds, a.ws, a.slots);
 }
 
@@ -119,7 +120,7 @@ hipError_t launch_rows(const BlockAttnArgs& a, const BlockForm& form, hipStream_
   switch (form.rows) {
     case 16: return launch_form<E4M3, 1>(a, stream);
     case 32: return launch_form<E4M3, 2>(a, stream);
-    case 64: return launch_form<E4M3, 4>(a, stream);
+    case 64: return a.table ? hipErrorInvalidValue : launch_form<E4M3, 4>(a, stream);
     default: return hipErrorInvalidValue;
   }
 }
