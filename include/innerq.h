@@ -513,7 +513,7 @@ int innerq_block_append(const innerq_block_config_t *cfg, innerq_block_cache_t *
  *                 read nor written.
  *   t_new_dev     int32 [B]: new tokens, clamped into 0 .. t_new; NULL: t_new each.  Rows beyond them are not read.
  * A sequence that would pass capacity_tokens takes the tokens that fit; one whose count is outside 0 .. capacity_tokens takes
- * none (its buffers and its count stay as they were).  One launch for up to `block` rows, else two. */
+ * none (its buffers and its count stay as they were).  One or two launches. */
 int innerq_block_append_ragged(const innerq_block_config_t *cfg, const innerq_block_cache_t *cache, int32_t *n_tokens_dev,
                                const int32_t *t_new_dev, const void *k_new, const innerq_strides_t *k_strides,
                                const void *v_new, const innerq_strides_t *v_strides, int64_t t_new, void *hip_stream);

@@ -184,7 +184,10 @@ __global__ void __launch_bounds__(256) block_append_kernel(BlockAppendArgs a, un
   append_unit<E4M3>(a, keys, b, h, j, take_of(a.s, b), lane);
 }
 
-// Few rows of a ragged batch: a work-group a sequence, which then advances its count.
+// Few rows of a ragged batch: a work-group a sequence, which then advances its count.  (Without the second launch a step takes 3.2 us in place of 4.2, but its 16
+// wavefronts pack the 2 H tensors' heads in turns.  In one launch and in two, us, a step that packs nothing, one that does, and 32 rows: 1 sequence of 8 heads 3.2
+// and 4.2, 6.2 and 5.9, 6.7 and 6.5; 1 of 16 3.6 and 4.2, 10.1 and 6.1, 10.9 and 6.9; 1 of 32 4.8 and 4.2, 19 and 6.1, 20 and 6.6; 64 of 32 the last two
+// 20.6 and 10.5, 22 and 11; 256 of 8 3.9 and 4.7, 8.2 and 10.6, 13.0 and 13.3.  Every 32nd step packs; so in one where there is one turn, and of few rows also in two.)
 template <bool E4M3>
 __global__ void __launch_bounds__(1024) block_append_step_kernel(BlockAppendArgs a, int* counts) {
   const int b = (int)blockIdx.x, lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -305,8 +308,12 @@ __global__ void __launch_bounds__(256) block_read_kernel(BlockReadArgs a, unsign
 
 }  // namespace
 
+// (up to a block of rows complete one block at most: a unit a head and tensor)
+static bool append_in_one(const BlockStore& s) {
+  return s.t_new <= s.block && (2 * s.n_kv_heads <= 16 || (2 * s.n_kv_heads <= 32 && 8 * s.t_new <= s.block));
+}
 hipError_t launch_block_append(const BlockAppendArgs& a, int* counts, bool e4m3, hipStream_t stream) {
-  if (counts && a.s.t_new <= a.s.block) {
+  if (counts && append_in_one(a.s)) {
     if (e4m3) block_append_step_kernel<true><<<a.s.batch, 1024, 0, stream>>>(a, counts);
     else block_append_step_kernel<false><<<a.s.batch, 1024, 0, stream>>>(a, counts);
     return hipGetLastError();
