@@ -544,7 +544,7 @@ int innerq_block_read_ragged(const innerq_block_config_t *cfg, const innerq_bloc
  *               same time need one each
  * Codes enter the products exactly (those of a block of values whose scale is below 2^-28 of the largest, with INNERQ_E4M3 below 2^-19: to 2^-35 of the
  * largest value), as do new and open rows (those beside a block with values above 2^11: to 2^-35 of the largest value); scales, statistics and sums are fp32.
- * Weights are rounded by at most 2^-22 of each where a kv head has up to 32 rows (query heads x new tokens), else, to fp16, by at most 2^-11 of
+ * Weights are rounded by at most 2^-22 of each where a kv head has up to 32 rows (query heads x new tokens of the sequence), else, to fp16, by at most 2^-11 of
  * each, and either way by up to 2^-34 of a row's largest one (2^-24 of it where scores, which fp32 then holds in steps of 2^-5 and more, are beyond 3 10^5).
  * Inputs finite. */
 int innerq_block_attention(const innerq_block_config_t *cfg, const innerq_block_cache_t *cache, const void *k_new,

@@ -145,11 +145,17 @@ int attention(const innerq_block_config_t& c, const innerq_block_cache_t& k, con
     return e == hipSuccess ? INNERQ_OK : INNERQ_E_HIP;
   }
   // (ragged: how many tokens the sequences have is not known here)
-  const BlockPlan plan = block_plan(c, t_new, tokens, causal && !n_dev ? 0.5f * (float)t_new : 0.f);
+  const bool both = n_dev && block_both_kinds(c, t_new);
+  const BlockPlan plan = both ? block_plan_both(c, t_new, tokens) : block_plan(c, t_new, tokens, causal && !n_dev ? 0.5f * (float)t_new : 0.f);
   a.row_blocks = (int)plan.row_blocks;
   a.n_splits = plan.n_splits;
   a.slots = heads * plan.row_blocks * plan.n_splits;
-  hipError_t e = launch(plan.form);
+  if (both) {
+    a.few_slots = a.slots;
+    a.few_rows = plan.form.rows;
+    a.few_most = kBlockFew.form.rows;
+  }
+  hipError_t e = both ? launch_block_list(a, e4m3, stream) : launch(plan.form);
   if (e == hipSuccess && a.n_splits > 1) e = launch_block_merge(a, plan.form, stream);
   return e == hipSuccess ? INNERQ_OK : INNERQ_E_HIP;
 }

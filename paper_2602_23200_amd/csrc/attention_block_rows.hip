@@ -374,19 +374,24 @@ __global__ void __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu
   attend<E4M3, WAVES>(a, uniform_work(a), lds);
 }
 
-// A ragged batch with sequences of many rows and of few: the first work-groups have the former, those behind them the latter, which wait for memory
-// while others compute.
+// A ragged batch with sequences of many rows and of few.  With lists: the first work-groups have the former, those behind them the latter, which wait for memory
+// while others compute.  Without: the same work-groups for every sequence, each in the form that its sequence's rows ask for.
 template <bool E4M3>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) block_list_kernel(BlockAttnArgs a) {
   constexpr int kFew = (int)sizeof(float) * block_few::kFloats<2>, kMany = kUnits * kUnitBytes;
   __shared__ __align__(16) char lds[kFew > kMany ? kFew : kMany];
   BlockWork w;
-  if ((int)blockIdx.x < a.list_many) {
-    if (find_work<128, 4>(a, a.few_most, 0x7fffffff, (int)blockIdx.x, w)) attend<E4M3, 4>(a, w, lds);
+  bool many = (int)blockIdx.x < a.list_many;
+  if (!a.table) {
+    w = uniform_work(a);
+    many = block_seq(a, w.b).t * a.heads_per_kv > a.few_most;
+  } else if (many) {
+    if (!find_work<128, 4>(a, a.few_most, 0x7fffffff, (int)blockIdx.x, w)) return;          // (uniform)
   } else {
-    if (find_work<32, 4>(a, 0, a.few_most, (int)blockIdx.x - a.list_many, w))
-      block_few::attend<E4M3, 2>(a, w, reinterpret_cast<float*>(lds), a.ws_few, a.few_slots);
+    if (!find_work<32, 4>(a, 0, a.few_most, (int)blockIdx.x - a.list_many, w)) return;
   }
+  if (many) attend<E4M3, 4>(a, w, lds);
+  else block_few::attend<E4M3, 2>(a, w, reinterpret_cast<float*>(lds), a.ws_few, a.few_slots, a.few_rows);
 }
 
 }  // namespace
@@ -407,9 +412,10 @@ hipError_t launch_block_rows(const BlockAttnArgs& a, bool e4m3, const BlockForm&
 }
 
 hipError_t launch_block_list(const BlockAttnArgs& a, bool e4m3, hipStream_t stream) {
-  const unsigned groups = (unsigned)(a.list_many + a.list_few);
-  if (e4m3) block_list_kernel<true><<<groups, 256, 0, stream>>>(a);
-  else block_list_kernel<false><<<groups, 256, 0, stream>>>(a);
+  const long long groups = a.table ? (long long)a.list_many + a.list_few : (long long)a.s.batch * a.s.n_kv_heads * a.row_blocks * a.n_splits;
+  if (groups >= (1LL << 31)) return hipErrorInvalidValue;
+  if (e4m3) block_list_kernel<true><<<(unsigned)groups, 256, 0, stream>>>(a);
+  else block_list_kernel<false><<<(unsigned)groups, 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 

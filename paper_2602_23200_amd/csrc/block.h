@@ -63,13 +63,13 @@ struct BlockAttnArgs {
   int list_few, list_many;             // work-groups of either kind
   float* ws;                           // slots: (level in the log2 domain, sum) of every row, then 128 sums of every row
   long long slots;                     // that ws holds
-  float* ws_few;                       // a list with both kinds: the slots of the sequences of few rows (ws: of the others)
+  float* ws_few;                       // a ragged batch with both kinds: the slots of the sequences of few rows (ws: of the others)
   long long few_slots;
   int few_rows, few_most;              // rows of such a slot; most rows of a sequence that has them
 };
 hipError_t launch_block_attention(const BlockAttnArgs& a, bool e4m3, const BlockForm& form, hipStream_t stream);
 hipError_t launch_block_rows(const BlockAttnArgs& a, bool e4m3, const BlockForm& form, hipStream_t stream);
-hipError_t launch_block_list(const BlockAttnArgs& a, bool e4m3, hipStream_t stream);     // both kinds
+hipError_t launch_block_list(const BlockAttnArgs& a, bool e4m3, hipStream_t stream);     // both kinds, with lists or without
 hipError_t launch_block_merge(const BlockAttnArgs& a, const BlockForm& form, hipStream_t stream);
 
 }  // namespace innerq

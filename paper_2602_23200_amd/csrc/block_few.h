@@ -138,9 +138,9 @@ constexpr int W = 4;                                    // wavefronts of a work-
 template <int NR>
 constexpr int kFloats = W * NR * (32 + 2) * 64;          // of LDS
 
-// ws, slots: where partial results go, and how many it holds.
+// ws, slots: where partial results go, and how many it holds, each of slot_rows rows.
 template <bool E4M3, int NR>
-__device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& work, float* lds, float* ws, long long slots) {
+__device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& work, float* lds, float* ws, long long slots, int slot_rows = 16 * NR) {
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
   const int b = work.b, h = work.h;
   const long long bh = (long long)b * a.s.n_kv_heads + h;
@@ -296,8 +296,8 @@ __device__ __forceinline__ void attend(const BlockAttnArgs& a, const BlockWork& 
     if (row >= rows) continue;
     const int channel = 32 * q + 8 * g + from;
     if (work.n_splits > 1) {
-      const long long slot_row = work.slot * (16 * NR) + 16 * n + c;
-      float* dst = ws + slots * (16 * NR * 2) + slot_row * D + channel;
+      const long long slot_row = work.slot * slot_rows + 16 * n + c;
+      float* dst = ws + slots * (slot_rows * 2) + slot_row * D + channel;
 #pragma unroll
       for (int i = 0; i < CH; i += 4) *reinterpret_cast<float4*>(dst + i) = float4{o[i], o[i + 1], o[i + 2], o[i + 3]};
       if (wave == 0 && g == 0) *reinterpret_cast<float2*>(ws + slot_row * 2) = float2{top, l};

@@ -142,6 +142,15 @@ inline BlockList block_list(const innerq_block_config_t& c, long long t_new, lon
   const bool all_few = rows <= kBlockFew.form.rows || block_plan_of(kBlockFew, heads, rows, units, units).us <= block_plan_of(kBlockMany, heads, rows, units, units).us;
   return block_list_of(c, t_new, all_few);
 }
+// Larger batches have no list.  Where a sequence may have more rows than few, all have the work-groups that the longest would have, as many ranges each, and every
+// work-group takes the form of its own sequence, so that what weights are rounded to does not depend on other sequences.
+inline bool block_both_kinds(const innerq_block_config_t& c, long long t_new) {
+  return c.batch > kBlockListMost && t_new * (c.n_q_heads / c.n_kv_heads) > kBlockFew.form.rows;
+}
+inline BlockPlan block_plan_both(const innerq_block_config_t& c, long long t_new, long long tokens) {
+  const float units = (float)ceil_div(tokens, kBlockTile);
+  return block_plan_of(kBlockMany, (long long)c.batch * c.n_kv_heads, t_new * (c.n_q_heads / c.n_kv_heads), units, units);
+}
 // What every work-group works out for itself (constexpr: device code, too).  A sequence's share of a list: units, each a kv head
 // and a block of `block` rows, and tiles of its keys (one, if there are none: zeros are written); none if its rows are not above `from` and up to `to`.
 struct BlockShare { int units, tiles; };
@@ -194,7 +203,8 @@ inline size_t block_workspace_bytes(const innerq_block_config_t& c, long long t_
   size_t bytes = 0;
   for (const BlockKind& k : kBlockKinds) {
     // (fewer row blocks may be split where these are not)
-    if (rows < block_least_rows(k.form) || block_split_most(k.form, heads, 1) == 1) continue;
+    const bool both = k.form.rows == kBlockMany.form.rows && block_both_kinds(c, t_new);
+    if ((rows < block_least_rows(k.form) && !both) || block_split_most(k.form, heads, 1) == 1) continue;
     const size_t slots = block_most_slots(k.form) * block_slot_bytes(k.form.rows);
     bytes = slots > bytes ? slots : bytes;
   }
