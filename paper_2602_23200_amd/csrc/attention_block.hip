@@ -12,7 +12,7 @@
 // the result is that of fp32 arithmetic on the values the cache stands for, and the kernel still waits for memory; for 64 rows that would cost
 // (8 sequences of 32k tokens, 48 rows: 133 us, with one piece 110), and weights are rounded to fp16 as they are for more rows.
 //
-// The softmax reference level is put 2^10 below the score that raises it and raised again only when a score passes it by 2^15, so outputs
+// The softmax reference level is put 2^10 below the score that raises it and raised again only when a score passes it by 2^15.9, so outputs
 // are scaled rarely; the statistics of a row are shared by its four lanes only then.
 //
 // What bounds it is the read of the cache: 8 sequences of 8 kv heads over 32k tokens, 538 MB, take 82 us for one token (6.5 TB/s; a copy of 2 GiB reaches 4.95

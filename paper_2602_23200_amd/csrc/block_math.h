@@ -11,8 +11,8 @@ typedef float float4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// log2 of the weight that the largest score has when it raises the level, and of the largest weight before the level is raised.
-constexpr float kTop = 10.0f, kRaise = 15.0f;
+// log2 of the weight that the largest score has when it raises the level, and of the largest weight before the level is raised (fp16 ends at 2^15.999).
+constexpr float kTop = 10.0f, kRaise = 15.9f;
 constexpr float kFar = 0x1p19f;                          // levels beyond: neighbours in fp32 are 2^-4 apart and more
 constexpr float kFarShare = 0x1p-16f;                    // of its own size, by which a level is raised the sooner
 
