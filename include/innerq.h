@@ -543,7 +543,7 @@ int innerq_block_read_ragged(const innerq_block_config_t *cfg, const innerq_bloc
  *   workspace   device scratch of innerq_block_workspace_bytes(cfg, t_new) bytes, content undefined; calls that may run at the
  *               same time need one each
  * Codes enter the products exactly (those of a block of values whose scale is below 2^-28 of the largest, with INNERQ_E4M3 below 2^-19: to 2^-35 of the
- * largest value), as do new and open rows (those beside a block with values above 2^11: to 2^-35 of the largest value); scales, statistics and sums are fp32.
+ * largest value), as do new and open rows (those beside a block with values above 2^12: to 2^-35 of the largest value); scales, statistics and sums are fp32.
  * Weights are rounded by at most 2^-22 of each where a kv head has up to 32 rows (query heads x new tokens of the sequence), else, to fp16, by at most 2^-11 of
  * each, and either way by up to 2^-34 of a row's largest one (2^-24 of it where scores, which fp32 then holds in steps of 2^-5 and more, are beyond 3 10^5).
  * Inputs finite. */

@@ -39,7 +39,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(NR 
 
 // The splits of a row joined: half a wavefront a row, a lane four channels, eight splits under way (only those that are there: with the last one read again in
 // place of the others, of a ragged batch with one to four, 15 us, now 11).  The launch is bounded, and its work-groups walk over the rows: of a padded
-// batch most rows are not there, and starting work-groups for them cost more than the joining (16 sequences of 1 to 256 new tokens 183 us with a
+// batch most rows are not there, and starting work-groups for them cost more than the joining (16 sequences of 2 to 256 new tokens 183 us with a
 // work-group for every eight rows, 177 with 4096 at most, 174 with 2048).  What bounds it is memory: three partial results of 9600 rows x 4 sequences
 // (60 MB) 15 us; of few rows the launch (4 us).
 constexpr int kMergeRows = 8;                            // of a work-group at once

@@ -14,7 +14,7 @@
 // Codes are exact in fp16 and scales are taken as block_math.h says.
 //
 // What bounds it is the matrix cores with the vector work beside them, and the power that both take: 2048 new tokens of 32 heads (8 of keys) over 32k,
-// 1134 GFLOP, take 1140 to 1180 us, 1000 to 960 TFLOP/s (a library product of two fp16 matrices 1330), matrix pipes 48 % and vector pipes 54 % busy; a
+// 1134 GFLOP, take 1140 to 1180 us, 1000 to 960 TFLOP/s (a library product of two fp16 matrices 1330), matrix pipes 46 % and vector pipes 52 % busy; a
 // form with 8 % fewer cycles took the same time at a lower clock.  Without one part at a time, in copies (of 1178 us): the first product 924, the second
 // 934, decoding and LDS writes 1037, exponentials 1118, barriers 1147, loads 1080.  Every wavefront with units of its own, decoded for itself: 2770;
 // units decoded once, in LDS, 64 rows a wavefront: 1534; the two products interleaved with what stands between them: 1196; keys read ahead of the barrier:

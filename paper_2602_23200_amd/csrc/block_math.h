@@ -68,7 +68,7 @@ __device__ __forceinline__ float threshold(float m) { return __builtin_fmaf(-kFa
 // two not below half of the largest, with values divided by it.  Weights are then off by 2^-25 at a level of 2^10 below the largest one, and by one
 // factor of two for the scales: 2^-34 of the largest.  (Scales as they are down to 1/16 of the largest, and 1 for new rows: 2^-30, and 2^-25.)
 // Of the codes' products fp16 holds multiples of 2^-24, so that every S is taken 2^-kLift times and codes 2^kLift times as large: what is rounded is off by 2^-25
-// at 2^-5 of the largest scale and less, 2^-36 of the largest value; and new rows are divided by more than 1 only beside values above 2^11.
+// at 2^-5 of the largest scale and less, 2^-36 of the largest value; and new rows are divided by more than 1 only beside values above 2^12.
 constexpr int kLift = 5;                                 // (1152 2^5, which integers have taken away, is an fp16 number)
 struct Scales { float by, add, inv; uint32_t values; };  // factor of the scores, log2 S, 1 / S, by what codes of values are multiplied
 

@@ -109,13 +109,14 @@ inline size_t block_slot_bytes(int group_rows) { return (size_t)group_rows * (kH
 
 // A ragged batch of up to kBlockListMost sequences: work-groups find their work in two lists made from the counts, of the sequences of few rows and of
 // those of more, each aimed at a number of work-groups.  With both they are one launch, the work-groups of many rows first: those of few rows find room
-// beside them and wait for memory while they compute (two launches and this one: 16 sequences of 1 to 256 new tokens over 1 to 16k 182 us, 167; 8 of 1 to
-// 40 over 1 to 4000 41.4, 32.2).  Sequences of few rows alone that fill half a round as they are have no list: it costs 4 us
-// in front of the first load, and a launch behind.  The second list's work-groups have 128 rows, not 256, and the first one's up to 32, not 64 (the
+// beside them and wait for memory while they compute (two launches and this one: 16 sequences of 2 to 256 new tokens over 1000 to 16000 182 us,
+// 167; 8 of 1 to 40 over 250 to 4000 41.4, 32.2).  Sequences of few rows alone that fill half a round as they are have no list: it costs 4 us
+// in front of the first load, and a launch behind.  (Without it one token of 64 sequences of 8 heads over 500 to 8000 tokens takes 75 us, 361 MB, of 64 over 2000 to
+// 32000 287, 1436 MB, of 32 of 16 heads over 500 to 8000 76, 365 MB: 4.8 to 5.0 TB/s, a copy's rate; with it 48 of 8 heads over 500 to 8000 59, 272 MB: 4.6.)  The second list's work-groups have 128 rows, not 256, and the first one's up to 32, not 64 (the
 // first of these cases, in two launches: 199 and 215 us; 187 and 199).
 constexpr int kBlockListMost = 256;
-// Ranges that a list aims at.  (As many as the chip holds, 768, 512 and 512: 8 sequences of 1 to 32k tokens, one new one 46.8 us, with these 43.8; of 1 to
-// 8000 22.7 and 21.2, 1 to 5 new ones 24.0 and 21.4; cross attention of 16 x 16 heads over 1 to 1437 17.7 and 18.7.)
+// Ranges that a list aims at.  (As many as the chip holds, 768, 512 and 512: 8 sequences of 2k to 32k tokens, one new one 46.8 us, with these 43.8; of 500 to
+// 8000 22.7 and 21.2, 1 to 5 new ones 24.0 and 21.4; cross attention of 16 x 16 heads over 89 to 1437 17.7 and 18.7.)
 constexpr int block_list_items(const BlockForm& f) { return f.rows == 32 ? 256 : 512; }
 constexpr int kBlockTableBytes = 2 * kBlockListMost * (int)sizeof(int);   // first slot and splits of every sequence, at the workspace's start
 struct BlockList {
@@ -177,7 +178,7 @@ constexpr int block_ranges(int tiles, int length) { return (tiles + length - 1) 
 constexpr bool block_length_fits(int length, int longest, int ranges, int items) { return length >= longest || ranges <= items; }
 // Which range a work-group takes.  Work-groups go to the eight dies in turn.  Where heads are a multiple of eight a die has an eighth of the heads, of every
 // sequence: a head's keys are read by one die, and sequences of any lengths are shared out evenly.  Otherwise a die has an eighth of the line.  (An eighth
-// of the line for each die, and this: 8 prompts of 16 to 2000 tokens 152 us, 97; 64 sequences of 1 to 512 new tokens over 250 to 4000 555, 313; the 16
+// of the line for each die, and this: 8 prompts of 15 to 2000 tokens 152 us, 97; 64 sequences of 4 to 512 new tokens over 250 to 4000 555, 313; the 16
 // above 157, 153.)  The last rows, which have the most keys, go first.
 constexpr bool block_by_head(int n_kv_heads) { return n_kv_heads % 8 == 0; }
 // Its place in the line (by head: in its die's line, an eighth of every sequence's ranges; none: -1).
